@@ -375,6 +375,128 @@ sl_status stacklstm_head_destroy(stacklstm_head_t h);
 /* One-line message for the last failure on the head ("" if none). */
 const char *stacklstm_head_last_error(stacklstm_head_t h);
 
+/*
+ * Output layers and beam search. What a model puts on the StackLSTM outputs y [T, B, H]
+ * (rows r = t B + b) beside the parser head, and the search that decodes it:
+ *   stacklstm_norm_*     layer norm, forward and backward
+ *   stacklstm_linear_*   linear layer with bias, activation and residual, and its backward
+ *   stacklstm_distill_*  loss and gradient against a teacher's top logits
+ *   stacklstm_beam_*     selection over hypotheses and classes, reordering of their stacks
+ * The conventions above hold: device pointers, C-ordered, 16-byte aligned; SL_FP32 / SL_BF16
+ * is the type of activations and weights (bf16 values as uint16 bit patterns), every gradient
+ * and statistic is float. Any width is accepted in either type. All sums are fp32 and run in
+ * a fixed order: results are bitwise reproducible.
+ * One handle type serves all of them; a handle takes only its own operator's calls
+ * (SL_ERR_ARG otherwise). Calls are ordered on the handle's stream and return after
+ * enqueueing; stacklstm_op_status reports what the device detected. `rows` may be anything
+ * from 0 to the R of create. A handle's workspace grows to the largest call so far (the first
+ * such call allocates and, where it replaces a smaller buffer, waits for the stream).
+ */
+typedef struct stacklstm_op *stacklstm_op_t;
+
+/* Replace the stream later calls are ordered on (waits for the old one: its work uses the
+ * handle's workspace). */
+sl_status stacklstm_op_set_stream(stacklstm_op_t op, void *stream);
+/* Synchronize the handle's stream; return (then clear) a device-detected error. */
+sl_status stacklstm_op_status(stacklstm_op_t op);
+/* Free the handle and its workspace (synchronizes its stream first). NULL is a no-op. */
+sl_status stacklstm_op_destroy(stacklstm_op_t op);
+/* One-line message for the last failure on the handle ("" if none). */
+const char *stacklstm_op_last_error(stacklstm_op_t op);
+
+/*
+ * Layer norm of rows of N: with m = mean(x), s = (mean((x - m)^2) + eps)^(-1/2),
+ *   y = (x - m) s gamma + beta.
+ * forward: x, y [rows, N] (dtype); gamma, beta [N] float (NULL: 1 and 0); mean, rstd [rows]
+ *   float outputs (NULL if no backward follows); eps >= 0.
+ * backward: dy [rows, N] float; x, gamma, mean, rstd as in the forward; outputs (each
+ *   nullable, overwritten) dx [rows, N], dgamma, dbeta [N]. rows = 0 gives zero sums.
+ */
+sl_status stacklstm_norm_create(stacklstm_op_t *out, int R, int N, sl_dtype dtype, int device, void *stream);
+sl_status stacklstm_norm_forward(stacklstm_op_t op, int rows, const void *x, const float *gamma, const float *beta,
+                                 float eps, void *y, float *mean, float *rstd);
+sl_status stacklstm_norm_backward(stacklstm_op_t op, int rows, const float *dy, const void *x, const float *gamma,
+                                  const float *mean, const float *rstd, float *dx, float *dgamma, float *dbeta);
+
+/* Activations: z; max(z, 0); tanh z; z Phi(z) (the normal distribution function); z sigmoid(z). */
+typedef enum { SL_ACT_NONE = 0, SL_ACT_RELU = 1, SL_ACT_TANH = 2, SL_ACT_GELU = 3, SL_ACT_SILU = 4 } sl_act;
+
+/*
+ * Linear layer y = act(pre) + residual, pre = x W^T + bias.
+ * forward: x [rows, K], W [N, K] (dtype); bias [N] float or NULL; residual [rows, N] (dtype)
+ *   or NULL; outputs y [rows, N] (dtype) and pre [rows, N] (dtype; NULL if not wanted: the
+ *   backward of an activation reads it). y may be residual.
+ * backward: dz = dy act'(pre) (relu: 0 at 0), dx = dz W + add, dW = dz^T x, dbias = sum of dz's rows.
+ *   dy [rows, N] float; x, W as in the forward; pre (unused for SL_ACT_NONE); add [rows, K]
+ *   float or NULL (the gradient a residual branch brings; may be dx); outputs (float, each
+ *   nullable, overwritten) dx [rows, K], dW [N, K], dbias [N]. The residual's gradient is dy.
+ * The contractions run on the tensor cores with fp32 accumulation. fp32 numbers (x and W of
+ * SL_FP32, dz always) enter as three bf16 parts each, 24 significant bits, and products below
+ * 2^-23 of the leading one are left out: results have fp32 accuracy. A value that is not
+ * finite makes the outputs it enters not finite (inf may become NaN).
+ * The first backward allocates 6 rows N bytes of workspace (and 4 rows N / 64 for dbias);
+ * SL_FP32 6 (rows + N) K for the parts.
+ */
+sl_status stacklstm_linear_create(stacklstm_op_t *out, int R, int K, int N, sl_dtype dtype, sl_act act, int device,
+                                  void *stream);
+sl_status stacklstm_linear_forward(stacklstm_op_t op, int rows, const void *x, const void *W, const float *bias,
+                                   const void *residual, void *y, void *pre);
+sl_status stacklstm_linear_backward(stacklstm_op_t op, int rows, const float *dy, const void *x, const void *W,
+                                    const void *pre, const float *add, float *dx, float *dW, float *dbias);
+
+/*
+ * Distillation from a teacher's top logits. Row r has logits z [V] (dtype), k teacher entries
+ * (t_idx int32: a class, or -1 for no entry; t_logit float) and a gold class (gold int32, -1
+ * for none; gold may be NULL). With q the softmax of t_logit / tau over the entries present,
+ * p = softmax(z / tau) and P = softmax(z):
+ *   loss = scale [ alpha tau^2 sum_j q_j (ln q_j - ln p_{i_j}) - (1 - alpha) ln P_gold ]
+ *   dz_v = scale [ alpha tau (p_v - sum of q_j over i_j = v) + (1 - alpha) (P_v - [v = gold]) ]
+ * A term whose teacher (gold class) is absent is 0, so a row with neither (padding) gives zero
+ * loss and gradient; so does a row whose every logit is -inf. A class listed twice counts with
+ * both weights; an entry with t_logit = -inf is as absent.
+ * loss_rows [rows], dlogits [rows, V]: float, each nullable. k <= 256, tau > 0, 0 <= alpha <= 1.
+ * An index outside its range is skipped and reported by stacklstm_op_status (SL_ERR_ARG).
+ */
+sl_status stacklstm_distill_create(stacklstm_op_t *out, int R, int V, int k, sl_dtype dtype, int device, void *stream);
+sl_status stacklstm_distill_run(stacklstm_op_t op, int rows, const void *logits, const int32_t *t_idx,
+                                const float *t_logit, const int32_t *gold, float tau, float alpha, float scale,
+                                float *loss_rows, float *dlogits);
+
+/*
+ * Beam search: B sentences with K hypotheses each (row n = b K + k), V classes (transitions or
+ * words), stacks of S slots and H units per row (S = T + 1 slots hold any T transitions).
+ * K <= 64, B <= 65535, K V <= 2^30.
+ * stacklstm_beam_lse: lse [B, K] (float) = ln sum_v exp(logits [B, K, V]) (dtype); -inf for a row
+ *   of -inf.
+ * stacklstm_beam_select: candidate (k, v) of sentence b scores
+ *   score[b, k] + (logits[b, k, v] - lse[b, k]), each operation rounded to fp32 (lse NULL: 0, the
+ *   logits are log-probabilities). A hypothesis with done[b, k] != 0 (done uint8, may be NULL) has
+ *   one candidate, itself, at its score. Candidates of -inf or NaN are none. Outputs [B, K], best
+ *   first, of equal scores the lowest k V + v first: new_score (float), parent (int32 k) and token
+ *   (int32 v, -1 for a done hypothesis); where candidates run out -inf, -1, -1. new_score must
+ *   not be score.
+ * stacklstm_beam_reorder: row (b, k) of the new stacks is row (b, parent[b, k]) of the old ones
+ *   (its own for parent -1): p_out [B K] = p, slots 0 .. p of h_out [S, B K, H] (dtype) and c_out
+ *   (float) copied, slots above the top left as they are, the top also to top_h, top_c [B K, H]
+ *   (each nullable). The new tensors must not overlap the old ones.
+ * stacklstm_beam_push: the step of Algorithm 1 on the reordered stacks, with dead writes skipped:
+ *   a push writes h_new, c_new [B K, H] to slot p + 1, then p += ops (int8 in {-1, 0, +1}); the
+ *   new top goes to top_h, top_c (each nullable). In place on p, h_stack, c_stack. The new state
+ *   of every row comes from a T = 1 stacklstm_forward whose h0, c0 are the tops.
+ * A parent, pointer or op out of range, a pop at depth 0 and a push on a full stack are
+ * treated as the row itself, the nearest slot and a hold, and reported by stacklstm_op_status.
+ */
+sl_status stacklstm_beam_create(stacklstm_op_t *out, int B, int K, int V, int S, int H, sl_dtype dtype, int device,
+                                void *stream);
+sl_status stacklstm_beam_lse(stacklstm_op_t op, const void *logits, float *lse);
+sl_status stacklstm_beam_select(stacklstm_op_t op, const void *logits, const float *lse, const float *score,
+                                const uint8_t *done, float *new_score, int32_t *parent, int32_t *token);
+sl_status stacklstm_beam_reorder(stacklstm_op_t op, const int32_t *parent, const int32_t *p, const void *h_stack,
+                                 const float *c_stack, int32_t *p_out, void *h_out, float *c_out, void *top_h,
+                                 float *top_c);
+sl_status stacklstm_beam_push(stacklstm_op_t op, const int8_t *ops, const void *h_new, const float *c_new, int32_t *p,
+                              void *h_stack, float *c_stack, void *top_h, float *top_c);
+
 #ifdef __cplusplus
 }
 #endif

@@ -75,6 +75,20 @@ def load(path: Optional[str] = None):
     lib.stacklstm_head_destroy.argtypes = [vp]
     lib.stacklstm_head_last_error.argtypes = [vp]
     lib.stacklstm_head_last_error.restype = ctypes.c_char_p
+    f32 = ctypes.c_float
+    op_args = {"op_set_stream": [vp, vp], "op_status": [vp], "op_destroy": [vp],
+               "norm_create": [ctypes.POINTER(vp), i, i, i, i, vp], "norm_forward": [vp, i, vp, vp, vp, f32, vp, vp, vp],
+               "norm_backward": [vp, i] + [vp] * 8, "linear_create": [ctypes.POINTER(vp)] + [i] * 6 + [vp],
+               "linear_forward": [vp, i] + [vp] * 6, "linear_backward": [vp, i] + [vp] * 8,
+               "distill_create": [ctypes.POINTER(vp)] + [i] * 5 + [vp],
+               "distill_run": [vp, i] + [vp] * 4 + [f32] * 3 + [vp] * 2,
+               "beam_create": [ctypes.POINTER(vp)] + [i] * 7 + [vp], "beam_lse": [vp] * 3, "beam_select": [vp] * 8,
+               "beam_reorder": [vp] * 10, "beam_push": [vp] * 9}
+    for name, types in op_args.items():
+        fn = getattr(lib, "stacklstm_" + name)
+        fn.argtypes, fn.restype = types, ctypes.c_int
+    lib.stacklstm_op_last_error.argtypes = [vp]
+    lib.stacklstm_op_last_error.restype = ctypes.c_char_p
     for fn in ("stacklstm_create", "stacklstm_forward", "stacklstm_backward", "stacklstm_set_stream",
                "stacklstm_set_async", "stacklstm_status", "stacklstm_destroy", "stacklstm_set_timing",
                "stacklstm_get_timing", "stacklstm_forward_group", "stacklstm_backward_group", "stacklstm_set_mode", "stacklstm_steps_run", "stacklstm_head_create", "stacklstm_head_run", "stacklstm_head_add_h0_grads",
@@ -362,3 +376,174 @@ def stacklstm_head_status(hh: StackLSTMHeadHandle):
 
 def stacklstm_head_destroy(hh: StackLSTMHeadHandle):
     hh.destroy()
+
+
+# ------------------------------------------------------------------ output layers and beam search
+SL_ACT_NONE, SL_ACT_RELU, SL_ACT_TANH, SL_ACT_GELU, SL_ACT_SILU = range(5)
+
+
+class StackLSTMOpHandle:
+    """Owns one operator handle (stacklstm_norm_*, _linear_*, _distill_* or _beam_*); ``destroy``
+    (or garbage collection) frees it."""
+
+    def __init__(self, h, device, dtype, **sizes):
+        self.h, self.device, self.dtype = h, device, dtype
+        self.__dict__.update(sizes)
+        import torch
+        self.tdtype = torch.bfloat16 if dtype == SL_BF16 else torch.float32
+
+    def destroy(self):
+        if self.h is not None and _lib is not None:
+            _lib.stacklstm_op_destroy(self.h)
+        self.h = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def _check_op(handle, st: int, where: str):
+    if st != 0:
+        msg = load().stacklstm_op_last_error(handle).decode() if handle else ""
+        raise StackLSTMError(st, where, msg)
+
+
+def _op_create(name, device, dtype, stream, args, **sizes):
+    import torch
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    raw = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+    h = ctypes.c_void_p()
+    _check_op(None, getattr(load(), name)(ctypes.byref(h), *args, device, ctypes.c_void_p(raw)), name)
+    return StackLSTMOpHandle(h, device, dtype, **sizes)
+
+
+def _rows(hd, t, name):
+    if t.dim() < 1 or t.shape[0] > hd.R:
+        raise ValueError("%s must have at most %d rows" % (name, hd.R))
+    return t.shape[0]
+
+
+def stacklstm_op_set_stream(hd: StackLSTMOpHandle, stream):
+    raw = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+    _check_op(hd.h, load().stacklstm_op_set_stream(hd.h, ctypes.c_void_p(raw)), "stacklstm_op_set_stream")
+
+
+def stacklstm_op_status(hd: StackLSTMOpHandle):
+    _check_op(hd.h, load().stacklstm_op_status(hd.h), "stacklstm_op_status")
+
+
+def stacklstm_op_destroy(hd: StackLSTMOpHandle):
+    hd.destroy()
+
+
+def stacklstm_norm_create(R: int, N: int, dtype: int, device: int = 0, stream=None):
+    """Layer norm of up to R rows of N; ``stream`` as for stacklstm_create."""
+    return _op_create("stacklstm_norm_create", device, dtype, stream, (R, N, dtype), R=R, N=N)
+
+
+def stacklstm_norm_forward(hd, x, gamma, beta, eps, y, mean=None, rstd=None):
+    """y = (x - mean) rstd gamma + beta, row by row; see include/stacklstm.h for layouts."""
+    import torch
+    r, N, d, dt, f = _rows(hd, x, "x"), hd.N, hd.device, hd.tdtype, torch.float32
+    args = [_ptr(x, d, dt, (r, N), "x"), _ptr(gamma, d, f, (N,), "gamma"), _ptr(beta, d, f, (N,), "beta"), eps,
+            _ptr(y, d, dt, (r, N), "y"), _ptr(mean, d, f, (r,), "mean"), _ptr(rstd, d, f, (r,), "rstd")]
+    _check_op(hd.h, load().stacklstm_norm_forward(hd.h, r, *args), "stacklstm_norm_forward")
+
+
+def stacklstm_norm_backward(hd, dy, x, gamma, mean, rstd, dx=None, dgamma=None, dbeta=None):
+    """Gradients of the layer norm; overwritten."""
+    import torch
+    r, N, d, f = _rows(hd, dy, "dy"), hd.N, hd.device, torch.float32
+    args = [_ptr(dy, d, f, (r, N), "dy"), _ptr(x, d, hd.tdtype, (r, N), "x"), _ptr(gamma, d, f, (N,), "gamma"),
+            _ptr(mean, d, f, (r,), "mean"), _ptr(rstd, d, f, (r,), "rstd"), _ptr(dx, d, f, (r, N), "dx"),
+            _ptr(dgamma, d, f, (N,), "dgamma"), _ptr(dbeta, d, f, (N,), "dbeta")]
+    _check_op(hd.h, load().stacklstm_norm_backward(hd.h, r, *args), "stacklstm_norm_backward")
+
+
+def stacklstm_linear_create(R: int, K: int, N: int, dtype: int, act: int = SL_ACT_NONE, device: int = 0, stream=None):
+    """A linear layer K -> N for up to R rows; ``stream`` as for stacklstm_create."""
+    return _op_create("stacklstm_linear_create", device, dtype, stream, (R, K, N, dtype, act), R=R, K=K, N=N, act=act)
+
+
+def stacklstm_linear_forward(hd, x, W, bias, residual, y, pre=None):
+    """y = act(x W^T + bias) + residual; see include/stacklstm.h for layouts."""
+    import torch
+    r, K, N, d, dt = _rows(hd, x, "x"), hd.K, hd.N, hd.device, hd.tdtype
+    args = [_ptr(x, d, dt, (r, K), "x"), _ptr(W, d, dt, (N, K), "W"), _ptr(bias, d, torch.float32, (N,), "bias"),
+            _ptr(residual, d, dt, (r, N), "residual"), _ptr(y, d, dt, (r, N), "y"), _ptr(pre, d, dt, (r, N), "pre")]
+    _check_op(hd.h, load().stacklstm_linear_forward(hd.h, r, *args), "stacklstm_linear_forward")
+
+
+def stacklstm_linear_backward(hd, dy, x, W, pre=None, add=None, dx=None, dW=None, dbias=None):
+    """Gradients of the linear layer; overwritten (dx includes ``add``)."""
+    import torch
+    r, K, N, d, dt, f = _rows(hd, dy, "dy"), hd.K, hd.N, hd.device, hd.tdtype, torch.float32
+    args = [_ptr(dy, d, f, (r, N), "dy"), _ptr(x, d, dt, (r, K), "x"), _ptr(W, d, dt, (N, K), "W"),
+            _ptr(pre, d, dt, (r, N), "pre"), _ptr(add, d, f, (r, K), "add"), _ptr(dx, d, f, (r, K), "dx"),
+            _ptr(dW, d, f, (N, K), "dW"), _ptr(dbias, d, f, (N,), "dbias")]
+    _check_op(hd.h, load().stacklstm_linear_backward(hd.h, r, *args), "stacklstm_linear_backward")
+
+
+def stacklstm_distill_create(R: int, V: int, k: int, dtype: int, device: int = 0, stream=None):
+    """Distillation of up to R rows of V logits from k teacher entries each."""
+    return _op_create("stacklstm_distill_create", device, dtype, stream, (R, V, k, dtype), R=R, V=V, k=k)
+
+
+def stacklstm_distill_run(hd, logits, t_idx, t_logit, gold, tau, alpha, scale, loss_rows=None, dlogits=None):
+    """Loss rows and the logits' gradient; see include/stacklstm.h for the formulas."""
+    import torch
+    r, V, k, d, f = _rows(hd, logits, "logits"), hd.V, hd.k, hd.device, torch.float32
+    args = [_ptr(logits, d, hd.tdtype, (r, V), "logits"), _ptr(t_idx, d, torch.int32, (r, k), "t_idx"),
+            _ptr(t_logit, d, f, (r, k), "t_logit"), _ptr(gold, d, torch.int32, (r,), "gold"), tau, alpha, scale,
+            _ptr(loss_rows, d, f, (r,), "loss_rows"), _ptr(dlogits, d, f, (r, V), "dlogits")]
+    _check_op(hd.h, load().stacklstm_distill_run(hd.h, r, *args), "stacklstm_distill_run")
+
+
+def stacklstm_beam_create(B: int, K: int, V: int, S: int, H: int, dtype: int, device: int = 0, stream=None):
+    """Beam search of B sentences, K hypotheses, V classes, stacks of S slots of H units."""
+    return _op_create("stacklstm_beam_create", device, dtype, stream, (B, K, V, S, H, dtype), B=B, K=K, V=V, S=S, H=H)
+
+
+def stacklstm_beam_lse(hd, logits, lse):
+    import torch
+    B, K, V, d = hd.B, hd.K, hd.V, hd.device
+    _check_op(hd.h, load().stacklstm_beam_lse(hd.h, _ptr(logits, d, hd.tdtype, (B, K, V), "logits"),
+                                              _ptr(lse, d, torch.float32, (B, K), "lse")), "stacklstm_beam_lse")
+
+
+def stacklstm_beam_select(hd, logits, lse, score, done, new_score, parent, token):
+    """The K best candidates of each sentence; see include/stacklstm.h."""
+    import torch
+    B, K, V, d, f, i = hd.B, hd.K, hd.V, hd.device, torch.float32, torch.int32
+    args = [_ptr(logits, d, hd.tdtype, (B, K, V), "logits"), _ptr(lse, d, f, (B, K), "lse"),
+            _ptr(score, d, f, (B, K), "score"), _ptr(done, d, torch.uint8, (B, K), "done"),
+            _ptr(new_score, d, f, (B, K), "new_score"), _ptr(parent, d, i, (B, K), "parent"),
+            _ptr(token, d, i, (B, K), "token")]
+    _check_op(hd.h, load().stacklstm_beam_select(hd.h, *args), "stacklstm_beam_select")
+
+
+def stacklstm_beam_reorder(hd, parent, p, h_stack, c_stack, p_out, h_out, c_out, top_h=None, top_c=None):
+    """The stacks of the chosen hypotheses' parents; see include/stacklstm.h."""
+    import torch
+    B, K, S, H, d, dt, f, i = hd.B, hd.K, hd.S, hd.H, hd.device, hd.tdtype, torch.float32, torch.int32
+    N = B * K
+    args = [_ptr(parent, d, i, (B, K), "parent"), _ptr(p, d, i, (N,), "p"), _ptr(h_stack, d, dt, (S, N, H), "h_stack"),
+            _ptr(c_stack, d, f, (S, N, H), "c_stack"), _ptr(p_out, d, i, (N,), "p_out"),
+            _ptr(h_out, d, dt, (S, N, H), "h_out"), _ptr(c_out, d, f, (S, N, H), "c_out"),
+            _ptr(top_h, d, dt, (N, H), "top_h"), _ptr(top_c, d, f, (N, H), "top_c")]
+    _check_op(hd.h, load().stacklstm_beam_reorder(hd.h, *args), "stacklstm_beam_reorder")
+
+
+def stacklstm_beam_push(hd, ops, h_new, c_new, p, h_stack, c_stack, top_h=None, top_c=None):
+    """One step of Algorithm 1 on the stacks, in place; see include/stacklstm.h."""
+    import torch
+    B, K, S, H, d, dt, f = hd.B, hd.K, hd.S, hd.H, hd.device, hd.tdtype, torch.float32
+    N = B * K
+    args = [_ptr(ops, d, torch.int8, (N,), "ops"), _ptr(h_new, d, dt, (N, H), "h_new"), _ptr(c_new, d, f, (N, H), "c_new"),
+            _ptr(p, d, torch.int32, (N,), "p"), _ptr(h_stack, d, dt, (S, N, H), "h_stack"),
+            _ptr(c_stack, d, f, (S, N, H), "c_stack"), _ptr(top_h, d, dt, (N, H), "top_h"),
+            _ptr(top_c, d, f, (N, H), "top_c")]
+    _check_op(hd.h, load().stacklstm_beam_push(hd.h, *args), "stacklstm_beam_push")
