@@ -380,6 +380,7 @@ def stacklstm_head_destroy(hh: StackLSTMHeadHandle):
 
 # ------------------------------------------------------------------ output layers and beam search
 SL_ACT_NONE, SL_ACT_RELU, SL_ACT_TANH, SL_ACT_GELU, SL_ACT_SILU = range(5)
+_f32 = _i32 = _i8 = _u8 = None  # torch's types, looked up when the first handle is made
 
 
 class StackLSTMOpHandle:
@@ -404,6 +405,20 @@ class StackLSTMOpHandle:
             pass
 
 
+def _arg(t, device, dtype, shape, name):
+    """The address of a tensor that is as it should be, by the cheapest checks that say so; anything
+    else goes through ``_ptr``, which names what is wrong. (Nine tensors a call: 18 us by ``_ptr``
+    on the host of a GB300, more than most kernels here take.)"""
+    if t is None:
+        return None
+    try:
+        if t.get_device() == device and t.dtype == dtype and t.shape == shape and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    return _ptr(t, device, dtype, shape, name)
+
+
 def _check_op(handle, st: int, where: str):
     if st != 0:
         msg = load().stacklstm_op_last_error(handle).decode() if handle else ""
@@ -411,7 +426,9 @@ def _check_op(handle, st: int, where: str):
 
 
 def _op_create(name, device, dtype, stream, args, **sizes):
+    global _f32, _i32, _i8, _u8
     import torch
+    _f32, _i32, _i8, _u8 = torch.float32, torch.int32, torch.int8, torch.uint8
     if stream is None:
         stream = torch.cuda.current_stream(device)
     raw = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
@@ -446,20 +463,18 @@ def stacklstm_norm_create(R: int, N: int, dtype: int, device: int = 0, stream=No
 
 def stacklstm_norm_forward(hd, x, gamma, beta, eps, y, mean=None, rstd=None):
     """y = (x - mean) rstd gamma + beta, row by row; see include/stacklstm.h for layouts."""
-    import torch
-    r, N, d, dt, f = _rows(hd, x, "x"), hd.N, hd.device, hd.tdtype, torch.float32
-    args = [_ptr(x, d, dt, (r, N), "x"), _ptr(gamma, d, f, (N,), "gamma"), _ptr(beta, d, f, (N,), "beta"), eps,
-            _ptr(y, d, dt, (r, N), "y"), _ptr(mean, d, f, (r,), "mean"), _ptr(rstd, d, f, (r,), "rstd")]
+    r, N, d, dt, f = _rows(hd, x, "x"), hd.N, hd.device, hd.tdtype, _f32
+    args = [_arg(x, d, dt, (r, N), "x"), _arg(gamma, d, f, (N,), "gamma"), _arg(beta, d, f, (N,), "beta"), eps,
+            _arg(y, d, dt, (r, N), "y"), _arg(mean, d, f, (r,), "mean"), _arg(rstd, d, f, (r,), "rstd")]
     _check_op(hd.h, load().stacklstm_norm_forward(hd.h, r, *args), "stacklstm_norm_forward")
 
 
 def stacklstm_norm_backward(hd, dy, x, gamma, mean, rstd, dx=None, dgamma=None, dbeta=None):
     """Gradients of the layer norm; overwritten."""
-    import torch
-    r, N, d, f = _rows(hd, dy, "dy"), hd.N, hd.device, torch.float32
-    args = [_ptr(dy, d, f, (r, N), "dy"), _ptr(x, d, hd.tdtype, (r, N), "x"), _ptr(gamma, d, f, (N,), "gamma"),
-            _ptr(mean, d, f, (r,), "mean"), _ptr(rstd, d, f, (r,), "rstd"), _ptr(dx, d, f, (r, N), "dx"),
-            _ptr(dgamma, d, f, (N,), "dgamma"), _ptr(dbeta, d, f, (N,), "dbeta")]
+    r, N, d, f = _rows(hd, dy, "dy"), hd.N, hd.device, _f32
+    args = [_arg(dy, d, f, (r, N), "dy"), _arg(x, d, hd.tdtype, (r, N), "x"), _arg(gamma, d, f, (N,), "gamma"),
+            _arg(mean, d, f, (r,), "mean"), _arg(rstd, d, f, (r,), "rstd"), _arg(dx, d, f, (r, N), "dx"),
+            _arg(dgamma, d, f, (N,), "dgamma"), _arg(dbeta, d, f, (N,), "dbeta")]
     _check_op(hd.h, load().stacklstm_norm_backward(hd.h, r, *args), "stacklstm_norm_backward")
 
 
@@ -470,20 +485,18 @@ def stacklstm_linear_create(R: int, K: int, N: int, dtype: int, act: int = SL_AC
 
 def stacklstm_linear_forward(hd, x, W, bias, residual, y, pre=None):
     """y = act(x W^T + bias) + residual; see include/stacklstm.h for layouts."""
-    import torch
     r, K, N, d, dt = _rows(hd, x, "x"), hd.K, hd.N, hd.device, hd.tdtype
-    args = [_ptr(x, d, dt, (r, K), "x"), _ptr(W, d, dt, (N, K), "W"), _ptr(bias, d, torch.float32, (N,), "bias"),
-            _ptr(residual, d, dt, (r, N), "residual"), _ptr(y, d, dt, (r, N), "y"), _ptr(pre, d, dt, (r, N), "pre")]
+    args = [_arg(x, d, dt, (r, K), "x"), _arg(W, d, dt, (N, K), "W"), _arg(bias, d, _f32, (N,), "bias"),
+            _arg(residual, d, dt, (r, N), "residual"), _arg(y, d, dt, (r, N), "y"), _arg(pre, d, dt, (r, N), "pre")]
     _check_op(hd.h, load().stacklstm_linear_forward(hd.h, r, *args), "stacklstm_linear_forward")
 
 
 def stacklstm_linear_backward(hd, dy, x, W, pre=None, add=None, dx=None, dW=None, dbias=None):
     """Gradients of the linear layer; overwritten (dx includes ``add``)."""
-    import torch
-    r, K, N, d, dt, f = _rows(hd, dy, "dy"), hd.K, hd.N, hd.device, hd.tdtype, torch.float32
-    args = [_ptr(dy, d, f, (r, N), "dy"), _ptr(x, d, dt, (r, K), "x"), _ptr(W, d, dt, (N, K), "W"),
-            _ptr(pre, d, dt, (r, N), "pre"), _ptr(add, d, f, (r, K), "add"), _ptr(dx, d, f, (r, K), "dx"),
-            _ptr(dW, d, f, (N, K), "dW"), _ptr(dbias, d, f, (N,), "dbias")]
+    r, K, N, d, dt, f = _rows(hd, dy, "dy"), hd.K, hd.N, hd.device, hd.tdtype, _f32
+    args = [_arg(dy, d, f, (r, N), "dy"), _arg(x, d, dt, (r, K), "x"), _arg(W, d, dt, (N, K), "W"),
+            _arg(pre, d, dt, (r, N), "pre"), _arg(add, d, f, (r, K), "add"), _arg(dx, d, f, (r, K), "dx"),
+            _arg(dW, d, f, (N, K), "dW"), _arg(dbias, d, f, (N,), "dbias")]
     _check_op(hd.h, load().stacklstm_linear_backward(hd.h, r, *args), "stacklstm_linear_backward")
 
 
@@ -494,11 +507,10 @@ def stacklstm_distill_create(R: int, V: int, k: int, dtype: int, device: int = 0
 
 def stacklstm_distill_run(hd, logits, t_idx, t_logit, gold, tau, alpha, scale, loss_rows=None, dlogits=None):
     """Loss rows and the logits' gradient; see include/stacklstm.h for the formulas."""
-    import torch
-    r, V, k, d, f = _rows(hd, logits, "logits"), hd.V, hd.k, hd.device, torch.float32
-    args = [_ptr(logits, d, hd.tdtype, (r, V), "logits"), _ptr(t_idx, d, torch.int32, (r, k), "t_idx"),
-            _ptr(t_logit, d, f, (r, k), "t_logit"), _ptr(gold, d, torch.int32, (r,), "gold"), tau, alpha, scale,
-            _ptr(loss_rows, d, f, (r,), "loss_rows"), _ptr(dlogits, d, f, (r, V), "dlogits")]
+    r, V, k, d, f = _rows(hd, logits, "logits"), hd.V, hd.k, hd.device, _f32
+    args = [_arg(logits, d, hd.tdtype, (r, V), "logits"), _arg(t_idx, d, _i32, (r, k), "t_idx"),
+            _arg(t_logit, d, f, (r, k), "t_logit"), _arg(gold, d, _i32, (r,), "gold"), tau, alpha, scale,
+            _arg(loss_rows, d, f, (r,), "loss_rows"), _arg(dlogits, d, f, (r, V), "dlogits")]
     _check_op(hd.h, load().stacklstm_distill_run(hd.h, r, *args), "stacklstm_distill_run")
 
 
@@ -508,42 +520,38 @@ def stacklstm_beam_create(B: int, K: int, V: int, S: int, H: int, dtype: int, de
 
 
 def stacklstm_beam_lse(hd, logits, lse):
-    import torch
     B, K, V, d = hd.B, hd.K, hd.V, hd.device
-    _check_op(hd.h, load().stacklstm_beam_lse(hd.h, _ptr(logits, d, hd.tdtype, (B, K, V), "logits"),
-                                              _ptr(lse, d, torch.float32, (B, K), "lse")), "stacklstm_beam_lse")
+    _check_op(hd.h, load().stacklstm_beam_lse(hd.h, _arg(logits, d, hd.tdtype, (B, K, V), "logits"),
+                                              _arg(lse, d, _f32, (B, K), "lse")), "stacklstm_beam_lse")
 
 
 def stacklstm_beam_select(hd, logits, lse, score, done, new_score, parent, token):
     """The K best candidates of each sentence; see include/stacklstm.h."""
-    import torch
-    B, K, V, d, f, i = hd.B, hd.K, hd.V, hd.device, torch.float32, torch.int32
-    args = [_ptr(logits, d, hd.tdtype, (B, K, V), "logits"), _ptr(lse, d, f, (B, K), "lse"),
-            _ptr(score, d, f, (B, K), "score"), _ptr(done, d, torch.uint8, (B, K), "done"),
-            _ptr(new_score, d, f, (B, K), "new_score"), _ptr(parent, d, i, (B, K), "parent"),
-            _ptr(token, d, i, (B, K), "token")]
+    B, K, V, d, f, i = hd.B, hd.K, hd.V, hd.device, _f32, _i32
+    args = [_arg(logits, d, hd.tdtype, (B, K, V), "logits"), _arg(lse, d, f, (B, K), "lse"),
+            _arg(score, d, f, (B, K), "score"), _arg(done, d, _u8, (B, K), "done"),
+            _arg(new_score, d, f, (B, K), "new_score"), _arg(parent, d, i, (B, K), "parent"),
+            _arg(token, d, i, (B, K), "token")]
     _check_op(hd.h, load().stacklstm_beam_select(hd.h, *args), "stacklstm_beam_select")
 
 
 def stacklstm_beam_reorder(hd, parent, p, h_stack, c_stack, p_out, h_out, c_out, top_h=None, top_c=None):
     """The stacks of the chosen hypotheses' parents; see include/stacklstm.h."""
-    import torch
-    B, K, S, H, d, dt, f, i = hd.B, hd.K, hd.S, hd.H, hd.device, hd.tdtype, torch.float32, torch.int32
+    B, K, S, H, d, dt, f, i = hd.B, hd.K, hd.S, hd.H, hd.device, hd.tdtype, _f32, _i32
     N = B * K
-    args = [_ptr(parent, d, i, (B, K), "parent"), _ptr(p, d, i, (N,), "p"), _ptr(h_stack, d, dt, (S, N, H), "h_stack"),
-            _ptr(c_stack, d, f, (S, N, H), "c_stack"), _ptr(p_out, d, i, (N,), "p_out"),
-            _ptr(h_out, d, dt, (S, N, H), "h_out"), _ptr(c_out, d, f, (S, N, H), "c_out"),
-            _ptr(top_h, d, dt, (N, H), "top_h"), _ptr(top_c, d, f, (N, H), "top_c")]
+    args = [_arg(parent, d, i, (B, K), "parent"), _arg(p, d, i, (N,), "p"), _arg(h_stack, d, dt, (S, N, H), "h_stack"),
+            _arg(c_stack, d, f, (S, N, H), "c_stack"), _arg(p_out, d, i, (N,), "p_out"),
+            _arg(h_out, d, dt, (S, N, H), "h_out"), _arg(c_out, d, f, (S, N, H), "c_out"),
+            _arg(top_h, d, dt, (N, H), "top_h"), _arg(top_c, d, f, (N, H), "top_c")]
     _check_op(hd.h, load().stacklstm_beam_reorder(hd.h, *args), "stacklstm_beam_reorder")
 
 
 def stacklstm_beam_push(hd, ops, h_new, c_new, p, h_stack, c_stack, top_h=None, top_c=None):
     """One step of Algorithm 1 on the stacks, in place; see include/stacklstm.h."""
-    import torch
-    B, K, S, H, d, dt, f = hd.B, hd.K, hd.S, hd.H, hd.device, hd.tdtype, torch.float32
+    B, K, S, H, d, dt, f = hd.B, hd.K, hd.S, hd.H, hd.device, hd.tdtype, _f32
     N = B * K
-    args = [_ptr(ops, d, torch.int8, (N,), "ops"), _ptr(h_new, d, dt, (N, H), "h_new"), _ptr(c_new, d, f, (N, H), "c_new"),
-            _ptr(p, d, torch.int32, (N,), "p"), _ptr(h_stack, d, dt, (S, N, H), "h_stack"),
-            _ptr(c_stack, d, f, (S, N, H), "c_stack"), _ptr(top_h, d, dt, (N, H), "top_h"),
-            _ptr(top_c, d, f, (N, H), "top_c")]
+    args = [_arg(ops, d, _i8, (N,), "ops"), _arg(h_new, d, dt, (N, H), "h_new"), _arg(c_new, d, f, (N, H), "c_new"),
+            _arg(p, d, _i32, (N,), "p"), _arg(h_stack, d, dt, (S, N, H), "h_stack"),
+            _arg(c_stack, d, f, (S, N, H), "c_stack"), _arg(top_h, d, dt, (N, H), "top_h"),
+            _arg(top_c, d, f, (N, H), "top_c")]
     _check_op(hd.h, load().stacklstm_beam_push(hd.h, *args), "stacklstm_beam_push")

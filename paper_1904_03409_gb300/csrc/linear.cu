@@ -18,6 +18,8 @@
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
+#include <cmath>
+
 #include "op.cuh"
 #include "tc.cuh"
 
@@ -154,41 +156,94 @@ struct Epilogue {
     float *part;            // split contraction: [split][rows][cols] sums, or null
 };
 
+constexpr int kMaxPairs = 6;
+
 struct GemmArgs {
     int chunks;             // 64-wide chunks of the contraction
-    int npair;
-    uint8_t pa[6], pb[6];   // parts of each partial product
-    int split, S;           // splits of the chunks; ring stages
+    int per_acc;            // chunks to an accumulator
+    int split;              // splits of the chunks
+    int mt, nt;             // tiles
+    int SA, SB;             // ring depths
+    int npair, PA, PB;      // partial products; parts of A and of B
+    struct Pair {
+        uint8_t a, b;       // parts
+        uint8_t at_a, at_b; // place of the part among the chunk's loads of A (B)
+        uint8_t load_a, load_b, free_a, free_b;  // first (last) use of the part in the chunk
+    } pair[kMaxPairs];
     int swapped;            // the output's rows are B's rows (few rows: A = W)
     Epilogue ep;
     long long limit;
     int32_t *err;
 };
 
+template <typename T>
+__device__ __forceinline__ void finish1(const Epilogue &ep, size_t at, int n, float v)
+{
+    if (ep.bias) v += ep.bias[n];
+    if (ep.pre) ((T *)ep.pre)[at] = from_f32<T>(v);
+    v = act_f(v, ep.act);
+    if (ep.residual) v += to_f32(((const T *)ep.residual)[at]);
+    ((T *)ep.y)[at] = from_f32<T>(v);
+}
+
+// One output element.
 __device__ __forceinline__ void finish(const Epilogue &ep, int r, int n, float v)
 {
     const size_t at = (size_t)r * ep.cols + n;
-    if (ep.out) {
+    if (ep.out)
         ep.out[at] = ep.add ? v + ep.add[at] : v;
+    else if (ep.bf16_out)
+        finish1<__nv_bfloat16>(ep, at, n, v);
+    else
+        finish1<float>(ep, at, n, v);
+}
+
+// Two neighbours of a row with an even number of columns: accesses of two elements.
+__device__ __forceinline__ void finish2(const Epilogue &ep, int r, int n, float2 v, float2 bias)
+{
+    const size_t at = (size_t)r * ep.cols + n;
+    if (ep.out) {
+        if (ep.add) {
+            const float2 a = *(const float2 *)(ep.add + at);
+            v.x += a.x;
+            v.y += a.y;
+        }
+        *(float2 *)(ep.out + at) = v;
         return;
     }
-    if (ep.bias) v += ep.bias[n];
-    float o = act_f(v, ep.act);
+    v.x += bias.x;
+    v.y += bias.y;
+    float2 o = make_float2(act_f(v.x, ep.act), act_f(v.y, ep.act));
     if (ep.bf16_out) {
-        if (ep.pre) ((__nv_bfloat16 *)ep.pre)[at] = __float2bfloat16(v);
-        if (ep.residual) o += __bfloat162float(((const __nv_bfloat16 *)ep.residual)[at]);
-        ((__nv_bfloat16 *)ep.y)[at] = __float2bfloat16(o);
+        if (ep.pre) *(__nv_bfloat162 *)((__nv_bfloat16 *)ep.pre + at) = __floats2bfloat162_rn(v.x, v.y);
+        if (ep.residual) {
+            const float2 q = __bfloat1622float2(*(const __nv_bfloat162 *)((const __nv_bfloat16 *)ep.residual + at));
+            o.x += q.x;
+            o.y += q.y;
+        }
+        *(__nv_bfloat162 *)((__nv_bfloat16 *)ep.y + at) = __floats2bfloat162_rn(o.x, o.y);
     } else {
-        if (ep.pre) ((float *)ep.pre)[at] = v;
-        if (ep.residual) o += ((const float *)ep.residual)[at];
-        ((float *)ep.y)[at] = o;
+        if (ep.pre) *(float2 *)((float *)ep.pre + at) = v;
+        if (ep.residual) {
+            const float2 q = *(const float2 *)((const float *)ep.residual + at);
+            o.x += q.x;
+            o.y += q.y;
+        }
+        *(float2 *)((float *)ep.y + at) = o;
     }
 }
 
-constexpr int kGemmThreads = 192;  // warps 0-3: epilogue; 4: TMA; 5: MMA
-constexpr int kMaxRing = 12;
+constexpr int kEpiWarps = 8;
+constexpr int kGemmThreads = (kEpiWarps + 2) * 32;  // then one warp for TMA, one for the MMAs
+constexpr int kMaxRing = 16;
 constexpr uint32_t kTileA = 128 * 128;  // 128 rows (or 2 x 64 columns) x 64 of the contraction
-constexpr long long kWaitLimit = 4000000000LL, kDrain = 4000000000LL;  // clock cycles of a bounded wait
+constexpr uint32_t kStageBytes = kEpiWarps * 32 * 32 * 4;
+constexpr uint32_t kRingBytes = 192 * 1024;
+constexpr uint32_t kGemmBars = (4 * kMaxRing + 5) * 8 + 16;
+constexpr uint32_t kGemmSmem = 1024 + kRingBytes + kStageBytes + kGemmBars;
+static_assert(kGemmSmem <= 227 * 1024, "shared memory of a CTA");
+constexpr int kGroupM = 16;             // m tiles that share their B tiles in L2
+constexpr long long kDrain = 4000000000LL;  // clock cycles: waits for a CTA's own copies and MMAs before it ends
 
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void *tmap, int c0, int c1, int c2, uint64_t *bar)
 {
@@ -198,46 +253,50 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void *tmap, int 
         : "memory");
 }
 
-__host__ __device__ constexpr uint32_t gemm_stage(int BN) { return kTileA + (uint32_t)BN * 128u; }
-__host__ __device__ constexpr uint32_t gemm_smem(int S, int BN) { return 1024 + S * gemm_stage(BN) + (2 * kMaxRing + 1) * 8 + 32; }
-
-// One 128 x BN tile (blockIdx.x: m tile fastest within a column of tiles) over the chunks of
-// split blockIdx.y. MN-major operands: blocks of 64 columns, each 64 rows of 128 bytes.
+// D [M][N] += sum over the pairs of A_i B_j^T. A CTA takes units (tile, split) blockIdx.x,
+// + gridDim.x, ...; a unit's chunks go through accumulators of per_acc chunks each, two of them
+// in turn in tensor memory: warps 0-7 add one up in registers (and after the last finish the
+// tile) while the MMAs fill the other. The tensor cores' fp32 additions cut, so an accumulator
+// that fp32 results come from takes few of them (1.7e-8 of the result each: 1e-4 after 6012).
+// A part is loaded once a chunk, whatever number of products it is in, small products first.
+// MN-major operands: blocks of 64 columns, each 64 rows of 128 bytes.
 template <int BN, bool A_MN, bool B_MN>
 __global__ void __launch_bounds__(kGemmThreads, 1)
-gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const GemmArgs g)
+gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
+           const __grid_constant__ GemmArgs g)
 {
-    constexpr uint32_t kStage = gemm_stage(BN);
-    constexpr uint32_t kCols = BN < 32 ? 32 : BN;
+    constexpr uint32_t kTileB = (uint32_t)BN * 128u;
+    constexpr int HALF = BN / 2, SEG = HALF < 32 ? HALF : 32;
+    constexpr uint32_t kCols = 2 * BN < 32 ? 32 : 2 * BN;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *base = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-    const int S = g.S;
-    const uint32_t ring0 = smem_u32(base);
-    uint64_t *full = (uint64_t *)(base + (size_t)S * kStage);
-    uint64_t *empty = full + kMaxRing;
-    uint64_t *done = empty + kMaxRing;
+    const int SA = g.SA, SB = g.SB;
+    const uint32_t ring_a = smem_u32(base), ring_b = ring_a + (uint32_t)SA * kTileA;
+    uint64_t *full_a = (uint64_t *)(base + kRingBytes + kStageBytes);
+    uint64_t *empty_a = full_a + kMaxRing, *full_b = empty_a + kMaxRing, *empty_b = full_b + kMaxRing;
+    uint64_t *acc_full = empty_b + kMaxRing, *acc_empty = acc_full + 2, *done = acc_empty + 2;
     uint32_t *tmem_slot = (uint32_t *)(done + 1);
-    int *n_issued = (int *)(tmem_slot + 1);
-    int *n_consumed = n_issued + 1;
-    volatile int *abort = (volatile int *)(n_consumed + 1);
+    volatile int *abort = (volatile int *)(tmem_slot + 1);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int mrows = g.swapped ? g.ep.cols : g.ep.rows, mt_n = (mrows + 127) / 128;
-    const int m0 = (int)(blockIdx.x % mt_n) * 128, n0 = (int)(blockIdx.x / mt_n) * BN, sp = blockIdx.y;
-    const int c_lo = (int)((long long)g.chunks * sp / g.split), c_hi = (int)((long long)g.chunks * (sp + 1) / g.split);
-    const int its = (c_hi - c_lo) * g.npair;
     if (tid == 0) {
-        for (int s = 0; s < S; ++s) {
-            tc::mbar_init(&full[s], 1);
-            tc::mbar_init(&empty[s], 1);
+        for (int s = 0; s < SA; ++s) {
+            tc::mbar_init(&full_a[s], 1);
+            tc::mbar_init(&empty_a[s], 1);
+        }
+        for (int s = 0; s < SB; ++s) {
+            tc::mbar_init(&full_b[s], 1);
+            tc::mbar_init(&empty_b[s], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            tc::mbar_init(&acc_full[i], 1);
+            tc::mbar_init(&acc_empty[i], kEpiWarps);
         }
         tc::mbar_init(done, 1);
-        *n_issued = 0;
-        *n_consumed = 0;
         *abort = 0;
         tc::fence_mbar_init();
     }
-    if (warp == 4) tc::tmem_alloc(tmem_slot, kCols);
+    if (warp == kEpiWarps) tc::tmem_alloc(tmem_slot, kCols);
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
@@ -246,97 +305,215 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
         *abort = 1;
         atomicCAS(g.err, 0, (int)SL_ERR_TIMEOUT);
     };
+    const long long limit = g.limit;
+    const int tiles = g.mt * g.nt;
+    const long long units = (long long)tiles * g.split;
+    // unit -> tile and chunks; tiles go down kGroupM m tiles, then to the next n tile, so that the
+    // CTAs running at one time share operands in L2
+    auto unit = [&](long long u, int &m0, int &n0, int &sp, int &c_lo, int &c_hi) {
+        sp = (int)(u / tiles);
+        const int t = (int)(u % tiles), group = t / (kGroupM * g.nt), in = t % (kGroupM * g.nt);
+        const int first = group * kGroupM, gm = min(kGroupM, g.mt - first);
+        m0 = (first + in % gm) * 128;
+        n0 = in / gm * BN;
+        c_lo = (int)((long long)g.chunks * sp / g.split);
+        c_hi = (int)((long long)g.chunks * (sp + 1) / g.split);
+    };
+    int m0, n0, sp, c_lo, c_hi;
 
-    if (warp == 4) {
+    // a ring's slots in use order: place i of the current chunk, its round's parity
+    struct Ring {
+        int S, at = 0;
+        uint32_t ph = 0;
+        __device__ int slot(int i) const { return at + i >= S ? at + i - S : at + i; }
+        __device__ uint32_t phase(int i) const { return at + i >= S ? ph ^ 1 : ph; }
+        __device__ void next(int parts)
+        {
+            at += parts;
+            if (at >= S) {
+                at -= S;
+                ph ^= 1;
+            }
+        }
+    };
+    Ring ra = {SA}, rb = {SB};
+
+    if (warp == kEpiWarps) {
         if (lane == 0) {
-            int it = 0;
-            for (; it < its; ++it) {
-                const int s = it % S;
-                if (it >= S && !tc::mbar_wait(&empty[s], (uint32_t)(it / S - 1) & 1, g.limit, abort)) {
-                    fail();
-                    break;
-                }
-                const uint32_t st = ring0 + s * kStage;
-                const int k0 = (c_lo + it / g.npair) * 64, pair = it % g.npair;
-                tc::mbar_arrive_expect_tx(&full[s], kStage);
-                if constexpr (A_MN) {
-                    tma_load_3d(st, &tm_a, m0, k0, g.pa[pair], &full[s]);
-                    tma_load_3d(st + 8192, &tm_a, m0 + 64, k0, g.pa[pair], &full[s]);
-                } else {
-                    tma_load_3d(st, &tm_a, k0, m0, g.pa[pair], &full[s]);
-                }
-                if constexpr (B_MN) {
+            long long na = 0, nb = 0;  // loads
+            bool ok = true;
+            for (long long u = blockIdx.x; ok && u < units; u += gridDim.x) {
+                unit(u, m0, n0, sp, c_lo, c_hi);
+                for (int c = c_lo; ok && c < c_hi; ++c) {
+                    const int k0 = c * 64;
+                    for (int p = 0; p < g.npair; ++p) {
+                        const GemmArgs::Pair &pr = g.pair[p];
+                        if (pr.load_b) {
+                            const int s = rb.slot(pr.at_b);
+                            ok = ok && tc::mbar_wait(&empty_b[s], rb.phase(pr.at_b) ^ 1, limit, abort);
+                            if (!ok) break;
+                            tc::mbar_arrive_expect_tx(&full_b[s], kTileB);
+                            ++nb;
+                            const uint32_t dst = ring_b + s * kTileB;
+                            if constexpr (B_MN) {
 #pragma unroll
-                    for (int nb = 0; nb < BN / 64; ++nb)
-                        tma_load_3d(st + kTileA + nb * 8192, &tm_b, n0 + nb * 64, k0, g.pb[pair], &full[s]);
-                } else {
-                    tma_load_3d(st + kTileA, &tm_b, k0, n0, g.pb[pair], &full[s]);
+                                for (int j = 0; j < BN / 64; ++j)
+                                    tma_load_3d(dst + j * 8192, &tm_b, n0 + j * 64, k0, pr.b, &full_b[s]);
+                            } else {
+                                tma_load_3d(dst, &tm_b, k0, n0, pr.b, &full_b[s]);
+                            }
+                        }
+                        if (pr.load_a) {
+                            const int s = ra.slot(pr.at_a);
+                            ok = ok && tc::mbar_wait(&empty_a[s], ra.phase(pr.at_a) ^ 1, limit, abort);
+                            if (!ok) break;
+                            tc::mbar_arrive_expect_tx(&full_a[s], kTileA);
+                            ++na;
+                            const uint32_t dst = ring_a + s * kTileA;
+                            if constexpr (A_MN) {
+                                tma_load_3d(dst, &tm_a, m0, k0, pr.a, &full_a[s]);
+                                tma_load_3d(dst + 8192, &tm_a, m0 + 64, k0, pr.a, &full_a[s]);
+                            } else {
+                                tma_load_3d(dst, &tm_a, k0, m0, pr.a, &full_a[s]);
+                            }
+                        }
+                    }
+                    ra.next(g.PA);
+                    rb.next(g.PB);
                 }
             }
-            *n_issued = it;
+            if (!ok) fail();
+            // no copy in flight when the CTA ends: the last load of every slot has landed
+            for (int s = 0; s < SA; ++s)
+                if (na > s) tc::mbar_wait(&full_a[s], (uint32_t)((na - 1 - s) / SA) & 1, kDrain, nullptr);
+            for (int s = 0; s < SB; ++s)
+                if (nb > s) tc::mbar_wait(&full_b[s], (uint32_t)((nb - 1 - s) / SB) & 1, kDrain, nullptr);
         }
         __syncwarp();
-    } else if (warp == 5) {
+    } else if (warp == kEpiWarps + 1) {
         if (lane == 0) {
             constexpr uint32_t idesc = tc::idesc_bf16(BN, A_MN, B_MN);
-            int it = 0;
-            for (; it < its && !*abort; ++it) {
-                const int s = it % S;
-                if (!tc::mbar_wait(&full[s], (uint32_t)(it / S) & 1, g.limit, abort)) {
-                    fail();
-                    break;
-                }
-                tc::tc_fence_after();
-                const uint32_t as = ring0 + s * kStage, bs = as + kTileA;
+            uint32_t acc = 0;  // accumulators filled so far
+            bool ok = true;
+            for (long long u = blockIdx.x; ok && u < units; u += gridDim.x) {
+                unit(u, m0, n0, sp, c_lo, c_hi);
+                for (int c = c_lo; ok && c < c_hi; ++acc) {
+                    const uint32_t d = tmem + (acc & 1) * BN;
+                    ok = tc::mbar_wait(&acc_empty[acc & 1], ((acc >> 1) & 1) ^ 1, limit, abort);
+                    if (!ok) break;
+                    tc::tc_fence_after();
+                    const int c_end = min(c_hi, c + g.per_acc);
+                    uint32_t more = 0;
+                    for (; ok && c < c_end; ++c) {
+                        for (int p = 0; p < g.npair; ++p) {
+                            const GemmArgs::Pair &pr = g.pair[p];
+                            const int sa = ra.slot(pr.at_a), sb = rb.slot(pr.at_b);
+                            if (pr.load_b) ok = tc::mbar_wait(&full_b[sb], rb.phase(pr.at_b), limit, abort);
+                            if (ok && pr.load_a) ok = tc::mbar_wait(&full_a[sa], ra.phase(pr.at_a), limit, abort);
+                            if (!ok) break;
+                            tc::tc_fence_after();
+                            const uint32_t as = ring_a + sa * kTileA, bs = ring_b + sb * kTileB;
 #pragma unroll
-                for (int k = 0; k < 4; ++k)  // 16 of the contraction: 32 bytes of a row, or 16 rows
-                    tc::mma_bf16(tmem, A_MN ? tc::smem_desc(as + k * 2048, 8192, 1024) : tc::smem_desc(as + k * 32, 16, 1024),
-                                 B_MN ? tc::smem_desc(bs + k * 2048, 8192, 1024) : tc::smem_desc(bs + k * 32, 16, 1024),
-                                 idesc, (it | k) != 0);
-                tc::mma_commit(&empty[s]);
+                            for (int k = 0; k < 4; ++k) {  // 16 of the contraction: 32 bytes of a row, or 16 rows
+                                tc::mma_bf16(d, A_MN ? tc::smem_desc(as + k * 2048, 8192, 1024) : tc::smem_desc(as + k * 32, 16, 1024),
+                                             B_MN ? tc::smem_desc(bs + k * 2048, 8192, 1024) : tc::smem_desc(bs + k * 32, 16, 1024),
+                                             idesc, more);
+                                more = 1;
+                            }
+                            if (pr.free_a) tc::mma_commit(&empty_a[sa]);
+                            if (pr.free_b) tc::mma_commit(&empty_b[sb]);
+                        }
+                        ra.next(g.PA);
+                        rb.next(g.PB);
+                    }
+                    if (ok) tc::mma_commit(&acc_full[acc & 1]);
+                }
             }
-            *n_consumed = it;
+            if (!ok) fail();
             tc::mma_commit(done);
+            tc::mbar_wait(done, 0, kDrain, nullptr);  // no MMA in flight when tensor memory is freed
         }
         __syncwarp();
     } else {
-        const bool ok = tc::mbar_wait(done, 0, g.limit, nullptr);
-        if (!ok) fail();
-        tc::tc_fence_after();
-        if (ok && !*abort) {
-            const int m = m0 + warp * 32 + lane;
-            const uint32_t trow = tmem + ((uint32_t)(warp * 32) << 16);
-            const Epilogue &ep = g.ep;
-            float *part = ep.part ? ep.part + (size_t)sp * ep.rows * ep.cols : nullptr;
-#pragma unroll 1
-            for (int c = 0; c < BN; c += 16) {
-                float v[16];
-                tc::tmem_ld16(trow + c, v);
+        // ------------------------------------------------------ sums and outputs
+        const int q = warp & 3, half = warp >> 2;  // a warp reads its quadrant of the lanes
+        float *stage = (float *)(base + kRingBytes) + warp * 1024;
+        const Epilogue &ep = g.ep;
+        uint32_t acc = 0;
+        bool ok = true;
+        for (long long u = blockIdx.x; ok && u < units; u += gridDim.x) {
+            unit(u, m0, n0, sp, c_lo, c_hi);
+            float sum[HALF];
+            for (int c = c_lo; c < c_hi; c += g.per_acc, ++acc) {
+                // (the whole warp: its reads of tensor memory are collective)
+                ok = __all_sync(0xffffffffu, tc::mbar_wait(&acc_full[acc & 1], (acc >> 1) & 1, limit, abort));
+                if (!ok) break;
+                tc::tc_fence_after();
+                const uint32_t at = tmem + ((uint32_t)(q * 32) << 16) + (acc & 1) * BN + half * HALF;
+                if (c == c_lo) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int n = n0 + c + i;
-                    const int r = g.swapped ? n : m, col = g.swapped ? m : n;
-                    if (r < ep.rows && col < ep.cols) {
-                        const float w = its ? v[i] : 0.0f;
-                        if (part)
-                            part[(size_t)r * ep.cols + col] = w;
-                        else
-                            finish(ep, r, col, w);
+                    for (int i = 0; i < HALF; i += 16) tc::tmem_ld16(at + i, *(float(*)[16])(sum + i));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < HALF; i += 16) {
+                        float v[16];
+                        tc::tmem_ld16(at + i, v);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) sum[i + j] += v[j];
                     }
                 }
+                tc::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&acc_empty[acc & 1]);
+            }
+            if (!ok) break;
+            // through shared memory, 32 rows x SEG columns at a time (16-byte pieces of row r at
+            // piece ^ (r mod 8)), so that a row's neighbours are a warp's
+            const int mm = m0 + q * 32, nn = n0 + half * HALF;
+            Epilogue o = ep;
+            if (ep.part) {  // plain sums
+                o.out = ep.part + (size_t)sp * ep.rows * ep.cols;
+                o.add = nullptr;
+            }
+            const bool pairs = ep.cols % 2 == 0;
+#pragma unroll
+            for (int s0 = 0; s0 < HALF; s0 += SEG) {
+#pragma unroll
+                for (int i = 0; i < SEG / 4; ++i)
+                    *(float4 *)(stage + lane * 32 + ((i ^ (lane & 7)) << 2)) =
+                        make_float4(sum[s0 + 4 * i], sum[s0 + 4 * i + 1], sum[s0 + 4 * i + 2], sum[s0 + 4 * i + 3]);
+                __syncwarp();
+                if (g.swapped) {
+                    const int n = mm + lane;
+                    for (int i = 0; i < SEG; ++i) {
+                        const int r = nn + s0 + i;
+                        if (n < ep.cols && r < ep.rows) finish(o, r, n, stage[lane * 32 + (((i >> 2) ^ (lane & 7)) << 2) + (i & 3)]);
+                    }
+                } else if (pairs && SEG == 32) {
+                    const int j = lane & 15, n = nn + s0 + 2 * j;
+                    float2 bias = make_float2(0.0f, 0.0f);
+                    if (n < ep.cols && !o.out && ep.bias) bias = *(const float2 *)(ep.bias + n);
+                    if (n < ep.cols)
+#pragma unroll 4
+                        for (int i = 0; i < 16; ++i) {
+                            const int rr = 2 * i + (lane >> 4), r = mm + rr;
+                            if (r < ep.rows)
+                                finish2(o, r, n, *(const float2 *)(stage + rr * 32 + (((j >> 1) ^ (rr & 7)) << 2) + ((j & 1) << 1)), bias);
+                        }
+                } else {
+                    const int j = lane, n = nn + s0 + j;
+                    if (j < SEG && n < ep.cols)
+                        for (int rr = 0; rr < 32; ++rr)
+                            if (mm + rr < ep.rows) finish(o, mm + rr, n, stage[rr * 32 + (((j >> 2) ^ (rr & 7)) << 2) + (j & 3)]);
+                }
+                __syncwarp();
             }
         }
+        if (!ok && lane == 0) fail();
     }
-    __syncthreads();
-    if (warp == 4 && lane == 0) {
-        // copies still in flight after an abort: issued, never seen landed
-        for (int it = *n_consumed; it < *n_issued; ++it)
-            tc::mbar_wait(&full[it % S], (uint32_t)(it / S) & 1, kDrain, nullptr);
-    }
-    if (warp == 5 && lane == 0) tc::mbar_wait(done, 0, kDrain, nullptr);
     tc::tc_fence_before();
     __syncthreads();
-    if (warp == 4) tc::tmem_dealloc(tmem, kCols);
+    if (warp == kEpiWarps) tc::tmem_dealloc(tmem, kCols);
 }
 
 // The splits' sums of each output added in split order, then its epilogue.
@@ -389,54 +566,111 @@ cudaError_t operand_map(CUtensorMap *tm, const Operand &o, int box_rows)
 }
 
 template <int BN, bool A_MN, bool B_MN>
-cudaError_t launch_gemm(const stacklstm_op *op, const Operand &a, const Operand &b, GemmArgs g, unsigned tiles)
+cudaError_t launch_gemm(const stacklstm_op *op, const Operand &a, const Operand &b, const GemmArgs &g)
 {
     CUtensorMap ta, tb;
     cudaError_t e = operand_map(&ta, a, A_MN ? 64 : 128);
     if (!e) e = operand_map(&tb, b, B_MN ? 64 : BN);
+    if (!e) e = smem_at_least((const void *)gemm_parts<BN, A_MN, B_MN>, kGemmSmem);
     if (e) return e;
-    g.S = std::min(kMaxRing, (int)((227 * 1024 - gemm_smem(0, BN)) / gemm_stage(BN)));
-    const size_t smem = gemm_smem(g.S, BN);
-    if ((e = smem_at_least((const void *)gemm_parts<BN, A_MN, B_MN>, smem))) return e;
-    gemm_parts<BN, A_MN, B_MN><<<dim3(tiles, g.split), kGemmThreads, smem, op->stream>>>(ta, tb, g);
+    const unsigned grid = (unsigned)std::min<long long>((long long)g.mt * g.nt * g.split, op->num_sms);
+    gemm_parts<BN, A_MN, B_MN><<<grid, kGemmThreads, kGemmSmem, op->stream>>>(ta, tb, g);
     return cudaGetLastError();
 }
 
 enum { kWsX = 0, kWsW, kWsDz, kWsSum, kWsPart };  // workspace buffers
 
-// D = sum over the parts' products of A B^T, kcols long, and its epilogue; the contraction is
-// split over more CTAs where its tiles leave SMs idle.
+constexpr size_t kMostPartBytes = (size_t)1 << 30;  // of the splits' sums
+
+// Tile width and splits: the least of waves x chunks x cycles a chunk (two cycles a column and
+// product, and no fewer than the operands' bytes take at 64 a cycle), a tile's start and end, and
+// for a split contraction its sums written and read again, and a second launch.
+void plan_gemm(GemmArgs &g, int M, int N, int bn_lo, int bn_hi, size_t out_elems, int sms, int *bn_out)
+{
+    double best = 1e300;
+    for (int bn = bn_lo; bn <= bn_hi; bn *= 2) {
+        const double mt = ceil_div(M, 128), nt = ceil_div(N, bn);
+        const double cyc = std::max(2.0 * bn * g.npair, (g.PA * (double)kTileA + g.PB * bn * 128.0) / 64.0);
+        for (int split = 1; split <= std::min(g.chunks, 64); ++split) {
+            if (split > 1 && (g.chunks / split < 2 || (double)split * out_elems * 4 > (double)kMostPartBytes)) break;
+            const double waves = std::ceil(mt * nt * split / sms), chunks = std::ceil((double)g.chunks / split);
+            double cost = waves * (chunks * cyc + 400.0) + 16.0 * bn + 2000.0;
+            if (split > 1) cost += 5000.0 + 2.0 * split * out_elems * 4 / 3500.0;
+            if (cost < best) {
+                best = cost;
+                g.mt = (int)mt;
+                g.nt = (int)nt;
+                g.split = split;
+                *bn_out = bn;
+            }
+        }
+    }
+}
+
+// D = sum over the parts' products of A B^T, kcols long, and its epilogue.
 template <bool A_MN, bool B_MN>
 cudaError_t contract(stacklstm_op *op, const Operand &a, const Operand &b, int kcols, bool swapped, Epilogue ep)
 {
     GemmArgs g = {};
     g.chunks = (int)ceil_div(kcols, 64);
+    g.PA = a.parts;
+    g.PB = b.parts;
+    // partial products, small ones first; a part's place is that of its first use
+    int next_a = 0, next_b = 0, place_a[3] = {-1, -1, -1}, place_b[3] = {-1, -1, -1};
+    for (int order = 2; order >= 0; --order)
+        for (int i = 0; i < a.parts; ++i) {
+            const int j = order - i;
+            if (j < 0 || j >= b.parts) continue;
+            GemmArgs::Pair &p = g.pair[g.npair++];
+            p.a = (uint8_t)i;
+            p.b = (uint8_t)j;
+            if ((p.load_a = place_a[i] < 0)) place_a[i] = next_a++;
+            if ((p.load_b = place_b[j] < 0)) place_b[j] = next_b++;
+            p.at_a = (uint8_t)place_a[i];
+            p.at_b = (uint8_t)place_b[j];
+        }
     for (int i = 0; i < a.parts; ++i)
-        for (int j = 0; j < b.parts; ++j)
-            if (i + j <= 2) {
-                g.pa[g.npair] = (uint8_t)i;
-                g.pb[g.npair++] = (uint8_t)j;
+        for (int p = g.npair - 1; p >= 0; --p)
+            if (g.pair[p].a == i) {
+                g.pair[p].free_a = 1;
+                break;
             }
+    for (int j = 0; j < b.parts; ++j)
+        for (int p = g.npair - 1; p >= 0; --p)
+            if (g.pair[p].b == j) {
+                g.pair[p].free_b = 1;
+                break;
+            }
+    // fp32 results: 24 MMAs to an accumulator
+    g.per_acc = ep.out || !ep.bf16_out ? std::max(1, 6 / g.npair) : g.chunks;
     g.swapped = swapped;
-    g.limit = kWaitLimit;
+    g.limit = op->wait_limit;
     g.err = op->err;
     const int M = swapped ? ep.cols : ep.rows, N = swapped ? ep.rows : ep.cols;
-    const int bn = N <= 64 ? 64 : N <= 128 ? 128 : 256;
-    const size_t tiles = (size_t)ceil_div(M, 128) * ceil_div(N, bn);
-    g.split = (int)std::max<size_t>(1, std::min<size_t>(g.chunks / 4, (size_t)op->num_sms / tiles));
-    // fp32 results: the tensor cores' fp32 additions cut instead of rounding, which costs about
-    // 1.7e-8 of the result an addition (measured: 1e-4 after 6012 of them); no accumulator takes
-    // more than 15 chunks' parts, the sums of which are added in fp32
-    if (ep.out || !ep.bf16_out) g.split = std::max(g.split, std::min(g.chunks, (int)ceil_div((size_t)g.chunks * g.npair, 15)));
+    // (three parts of a 256-wide B leave the rings no second chunk)
+    const int most = b.parts == 3 ? 128 : 256;
+    const int lo = swapped && N <= 32 ? 32 : 64, hi = N <= lo ? lo : N <= 64 ? 64 : N <= 128 ? 128 : most;
+    int bn = 64;
+    plan_gemm(g, M, N, lo, hi, (size_t)ep.rows * ep.cols, op->num_sms, &bn);
+    // rings: as many whole chunks as fit, what is left to B, then to A
+    const uint32_t tb = (uint32_t)bn * 128, per = g.PA * kTileA + g.PB * tb;
+    const int depth = (int)(kRingBytes / per);
+    g.SA = std::min(kMaxRing / g.PA, depth) * g.PA;
+    g.SB = std::min(kMaxRing / g.PB, depth) * g.PB;
+    while (g.SB < kMaxRing && g.SA * kTileA + (g.SB + 1) * tb <= kRingBytes && g.PB < g.PA) ++g.SB;
+    while (g.SA < kMaxRing && (g.SA + 1) * kTileA + g.SB * tb <= kRingBytes) ++g.SA;
     if (g.split > 1) {
         cudaError_t e = op_workspace(op, kWsPart, (size_t)g.split * ep.rows * ep.cols * 4);
         if (e) return e;
         ep.part = (float *)op->ws[kWsPart];
     }
     g.ep = ep;
-    cudaError_t e = bn == 64    ? launch_gemm<64, A_MN, B_MN>(op, a, b, g, (unsigned)tiles)
-                    : bn == 128 ? launch_gemm<128, A_MN, B_MN>(op, a, b, g, (unsigned)tiles)
-                                : launch_gemm<256, A_MN, B_MN>(op, a, b, g, (unsigned)tiles);
+    cudaError_t e = cudaErrorInvalidValue;
+    if constexpr (!A_MN && !B_MN)
+        if (bn == 32) e = launch_gemm<32, A_MN, B_MN>(op, a, b, g);
+    if (bn == 64) e = launch_gemm<64, A_MN, B_MN>(op, a, b, g);
+    if (bn == 128) e = launch_gemm<128, A_MN, B_MN>(op, a, b, g);
+    if (bn == 256) e = launch_gemm<256, A_MN, B_MN>(op, a, b, g);
     if (!e && g.split > 1) {
         join_splits<<<(unsigned)std::min<size_t>(ceil_div((size_t)ep.rows * ep.cols, 256), (size_t)op->num_sms * 8), 256, 0,
                       op->stream>>>(ep, g.split);

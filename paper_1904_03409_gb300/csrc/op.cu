@@ -1,5 +1,7 @@
 // op.cu -- what the output-layer and search operators have in common: the handle's life, its
 // stream, its status word and workspace, and their C ABI (include/stacklstm.h, stacklstm_op_*).
+#include <stdlib.h>
+
 #include "op.cuh"
 
 namespace sl {
@@ -25,6 +27,8 @@ stacklstm_op *op_new(int kind, sl_dtype dt, int device, void *stream, sl_status 
     op->dt = dt;
     op->device = device;
     op->stream = (cudaStream_t)stream;
+    const char *limit = getenv("STACKLSTM_WAIT_LIMIT_CYCLES");  // test hook (include/stacklstm.h)
+    op->wait_limit = limit ? atoll(limit) : 4000000000LL;
     int devices = 0;
     if (cudaGetDeviceCount(&devices) != cudaSuccess || device < 0 || device >= devices) {
         cudaGetLastError();

@@ -23,6 +23,7 @@ struct stacklstm_op {
     int V = 0, k = 0;                  // distill: classes, teacher entries a row; beam: V
     int B = 0, beams = 0, S = 0, H = 0;  // beam
     int32_t *err = nullptr;            // device-detected status (first error wins)
+    long long wait_limit = 0;          // clock cycles one bounded device-side wait may spin
     void *ws[8] = {};                  // workspace buffers, by kind
     size_t ws_bytes[8] = {};
     char last_error[192] = {};

@@ -131,7 +131,8 @@ def test_norm_gradient_is_that_of_differences():
 
 # ------------------------------------------------------------------ linear layer
 LINEAR = [(1, 1, 1), (1, 64, 40), (5, 100, 83), (8, 1024, 517), (17, 8, 300), (64, 200, 64), (65, 72, 130),
-          (128, 64, 256), (130, 75, 100), (200, 333, 257), (300, 600, 200), (513, 48, 513), (1000, 128, 32)]
+          (128, 64, 256), (130, 75, 100), (200, 333, 257), (300, 600, 200), (513, 48, 513), (1000, 128, 32),
+          (2100, 520, 300), (66, 1100, 2500)]
 
 
 @TYPES
@@ -250,6 +251,26 @@ def test_linear_on_its_own_stream():
     y2 = out(96, 56, dtype=torch.bfloat16)
     bd.stacklstm_linear_forward(op, xd, Wd, None, None, y2)
     assert torch.equal(y, y2)
+
+
+@TYPES
+@pytest.mark.parametrize("R,K,N", [(4, 200, 300), (300, 2000, 700)])
+def test_linear_wait_that_runs_out_is_reported(dt, R, K, N, monkeypatch):
+    """A wait budget of 0 cycles: the call ends, its status says so, and a handle with the usual
+    budget works after it."""
+    x, W = torch.ones(R, K, device="cuda", dtype=tdt(dt)), torch.ones(N, K, device="cuda", dtype=tdt(dt))
+    y = out(R, N, dtype=tdt(dt))
+    monkeypatch.setenv("STACKLSTM_WAIT_LIMIT_CYCLES", "0")
+    op = bd.stacklstm_linear_create(R, K, N, dt)
+    bd.stacklstm_linear_forward(op, x, W, None, None, y)
+    with pytest.raises(bd.StackLSTMError) as e:
+        bd.stacklstm_op_status(op)
+    assert e.value.status == 6
+    monkeypatch.delenv("STACKLSTM_WAIT_LIMIT_CYCLES")
+    op = bd.stacklstm_linear_create(R, K, N, dt)
+    bd.stacklstm_linear_forward(op, x, W, None, None, y)
+    bd.stacklstm_op_status(op)
+    assert y.eq(K).all()
 
 
 # ------------------------------------------------------------------ distillation
