@@ -19,6 +19,7 @@
 #include <cudaTypedefs.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "op.cuh"
 #include "tc.cuh"
@@ -92,32 +93,78 @@ pack_parts(size_t rows, int cols, int ld, const T *__restrict__ src, __nv_bfloat
     }
 }
 
-constexpr int kDzCols = 256, kDzRows = 64;
+constexpr int kDzCols = 128, kDzRows = 64, kDzSub = 8;
 
 // dz = dy act'(pre) as three parts [3][rows][ld], and this CTA's column sums of it over its rows,
-// part [row blocks][N]. A thread takes one column.
-template <typename T>
-__global__ void __launch_bounds__(kDzCols)
+// part [row blocks][N]. A lane takes four columns (one 8-byte store a part, from one 16-byte read
+// where the rows of dy start on 16 bytes), warp w the rows w, w + 8, ... of the block, four at a
+// time; the eight warps' sums are added in order. HBM-bound: 4 + 6 bytes an element.
+template <typename T, bool ALIGNED>
+__global__ void __launch_bounds__(32 * kDzSub)
 dz_parts(int rows, int N, int ld, int act, const float *__restrict__ dy, const T *__restrict__ pre,
          __nv_bfloat16 *__restrict__ out, float *__restrict__ part)
 {
-    const int c = blockIdx.y * kDzCols + threadIdx.x;
-    if (c >= N) return;
+    __shared__ float4 sm[kDzSub][32];
+    const int lane = threadIdx.x & 31, sub = threadIdx.x >> 5;
+    const int c = blockIdx.y * kDzCols + lane * 4, nc = min(4, N - c);
     const int r0 = blockIdx.x * kDzRows, r1 = min(rows, r0 + kDzRows);
     const size_t plane = (size_t)rows * ld;
-    float sum = 0.0f;
-    for (int r = r0; r < r1; ++r) {
-        float v = dy[(size_t)r * N + c];
-        if (act != kActNone) v = __fmul_rn(v, act_grad(to_f32(pre[(size_t)r * N + c]), act));  // (not fused with the sum)
-        sum += v;
-        if (out) {
-            __nv_bfloat16 p[3];
-            split3(v, p);
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (nc > 0) {
+        for (int r = r0 + sub; r < r1; r += 4 * kDzSub) {
+            float v[4][4], z[4][4];
 #pragma unroll
-            for (int i = 0; i < 3; ++i) out[i * plane + (size_t)r * ld + c] = p[i];
+            for (int i = 0; i < 4; ++i) {
+                const int ri = r + i * kDzSub;
+                const size_t at = (size_t)ri * N + c;
+                if constexpr (ALIGNED) {
+                    const float4 q = ri < r1 ? *(const float4 *)(dy + at) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    v[i][0] = q.x; v[i][1] = q.y; v[i][2] = q.z; v[i][3] = q.w;
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[i][j] = ri < r1 && j < nc ? dy[at + j] : 0.0f;
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) z[i][j] = act != kActNone && ri < r1 && j < nc ? to_f32(pre[at + j]) : 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int ri = r + i * kDzSub;
+                if (ri >= r1) break;
+                union {
+                    __nv_bfloat16 b[4];
+                    uint2 q;
+                } o[3];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float w = act != kActNone ? __fmul_rn(v[i][j], act_grad(z[i][j], act)) : v[i][j];  // (not fused with the sum)
+                    sum[j] += w;
+                    __nv_bfloat16 p[3];
+                    split3(w, p);
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) o[k].b[j] = p[k];
+                }
+                if (out)  // (a row has room for whole groups of eight: what is past N is never read)
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) *(uint2 *)(out + k * plane + (size_t)ri * ld + c) = o[k].q;
+            }
         }
     }
-    if (part) part[(size_t)blockIdx.x * N + c] = sum;
+    if (!part) return;
+    sm[sub][lane] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+    __syncthreads();
+    if (sub == 0 && nc > 0) {
+        float4 t = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int i = 0; i < kDzSub; ++i) {
+            const float4 q = sm[i][lane];
+            t.x += q.x; t.y += q.y; t.z += q.z; t.w += q.w;
+        }
+        const float w[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < nc) part[(size_t)blockIdx.x * N + c + j] = w[j];
+    }
 }
 
 // out[c] = the sum over s of part[s][c]: warp w adds parts w, w + 8, ..., then the eight in order.
@@ -156,85 +203,243 @@ struct Epilogue {
     float *part;            // split contraction: [split][rows][cols] sums, or null
 };
 
-constexpr int kMaxPairs = 6;
-
 struct GemmArgs {
     int chunks;             // 64-wide chunks of the contraction
     int per_acc;            // chunks to an accumulator
     int split;              // splits of the chunks
     int mt, nt;             // tiles
     int SA, SB;             // ring depths
-    int npair, PA, PB;      // partial products; parts of A and of B
-    struct Pair {
-        uint8_t a, b;       // parts
-        uint8_t at_a, at_b; // place of the part among the chunk's loads of A (B)
-        uint8_t load_a, load_b, free_a, free_b;  // first (last) use of the part in the chunk
-    } pair[kMaxPairs];
     int swapped;            // the output's rows are B's rows (few rows: A = W)
     Epilogue ep;
     long long limit;
     int32_t *err;
 };
 
-template <typename T>
-__device__ __forceinline__ void finish1(const Epilogue &ep, size_t at, int n, float v)
-{
-    if (ep.bias) v += ep.bias[n];
-    if (ep.pre) ((T *)ep.pre)[at] = from_f32<T>(v);
-    v = act_f(v, ep.act);
-    if (ep.residual) v += to_f32(((const T *)ep.residual)[at]);
-    ((T *)ep.y)[at] = from_f32<T>(v);
-}
-
-// One output element.
-__device__ __forceinline__ void finish(const Epilogue &ep, int r, int n, float v)
-{
-    const size_t at = (size_t)r * ep.cols + n;
-    if (ep.out)
-        ep.out[at] = ep.add ? v + ep.add[at] : v;
-    else if (ep.bf16_out)
-        finish1<__nv_bfloat16>(ep, at, n, v);
-    else
-        finish1<float>(ep, at, n, v);
-}
-
-// Two neighbours of a row with an even number of columns: accesses of two elements.
-__device__ __forceinline__ void finish2(const Epilogue &ep, int r, int n, float2 v, float2 bias)
-{
-    const size_t at = (size_t)r * ep.cols + n;
-    if (ep.out) {
-        if (ep.add) {
-            const float2 a = *(const float2 *)(ep.add + at);
-            v.x += a.x;
-            v.y += a.y;
+// The partial products of PA parts of A and PB of B: those of order i + j <= 2, small ones first.
+template <int PA, int PB>
+struct Pairs {
+    int n = 0, a[6] = {}, b[6] = {};
+    int at_a[3] = {}, at_b[3] = {};      // place of a part among the chunk's loads: that of its first use
+    bool load_a[6] = {}, load_b[6] = {}, free_a[6] = {}, free_b[6] = {};
+    constexpr Pairs()
+    {
+        int na = 0, nb = 0;
+        bool seen_a[3] = {}, seen_b[3] = {};
+        for (int order = 2; order >= 0; --order)
+            for (int i = 0; i < PA; ++i) {
+                const int j = order - i;
+                if (j < 0 || j >= PB) continue;
+                a[n] = i;
+                b[n] = j;
+                load_a[n] = !seen_a[i];
+                load_b[n] = !seen_b[j];
+                if (!seen_a[i]) at_a[i] = na++;
+                if (!seen_b[j]) at_b[j] = nb++;
+                seen_a[i] = seen_b[j] = true;
+                ++n;
+            }
+        for (int p = 0; p < n; ++p) {
+            free_a[p] = free_b[p] = true;
+            for (int q = p + 1; q < n; ++q) {
+                if (a[q] == a[p]) free_a[p] = false;
+                if (b[q] == b[p]) free_b[p] = false;
+            }
         }
-        *(float2 *)(ep.out + at) = v;
+    }
+};
+
+// What an output is made of, with the pointers of its kind: plain fp32 sums (and an addend), or
+// the forward's y and pre of type T.
+template <typename T>
+struct Forward {
+    const T *residual;
+    T *y, *pre;
+    int act;
+    __device__ explicit Forward(const Epilogue &ep) : residual((const T *)ep.residual), y((T *)ep.y), pre((T *)ep.pre), act(ep.act) {}
+    __device__ __forceinline__ float extra(size_t at) const { return residual ? to_f32(residual[at]) : 0.0f; }
+    __device__ __forceinline__ void put(size_t at, float v, float bias, float extra) const
+    {
+        v += bias;
+        if (pre) pre[at] = from_f32<T>(v);
+        y[at] = from_f32<T>(act_f(v, act) + extra);
+    }
+};
+struct Plain {
+    const float *add;
+    float *out;
+    __device__ __forceinline__ float extra(size_t at) const { return add ? add[at] : 0.0f; }
+    __device__ __forceinline__ void put(size_t at, float v, float, float extra) const { out[at] = v + extra; }
+};
+
+// Two neighbours in one access.
+__device__ __forceinline__ float2 load2(const float *p) { return *(const float2 *)p; }
+__device__ __forceinline__ float2 load2(const __nv_bfloat16 *p) { return __bfloat1622float2(*(const __nv_bfloat162 *)p); }
+__device__ __forceinline__ void store2(float *p, float x, float y) { *(float2 *)p = make_float2(x, y); }
+__device__ __forceinline__ void store2(__nv_bfloat16 *p, float x, float y) { *(__nv_bfloat162 *)p = __floats2bfloat162_rn(x, y); }
+
+// A warp's 32 rows x SEG columns of sums in shared memory: row r's 16-byte pieces at piece ^ (r mod 8).
+__device__ __forceinline__ const float *staged(const float *stage, int r, int c)
+{
+    return stage + r * 32 + (((c >> 2) ^ (r & 7)) << 2) + (c & 3);
+}
+
+// Those sums (row 0 = output row r0, column 0 = output column n0) to the output, a row's
+// neighbours by neighbouring lanes; what is added is read four rows ahead of the stores.
+template <int SEG, typename Out>
+__device__ __forceinline__ void put_rows(const Out &o, const float *stage, int lane, int r0, int n0, int rows, int cols,
+                                         const float *bias_p)
+{
+    const int n = n0 + lane;
+    if (lane >= SEG || n >= cols) return;
+    const float bias = bias_p ? bias_p[n] : 0.0f;
+    const int m = min(32, rows - r0);
+    for (int i0 = 0; i0 < m; i0 += 4) {
+        float extra[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) extra[i] = i0 + i < m ? o.extra((size_t)(r0 + i0 + i) * cols + n) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i0 + i < m) o.put((size_t)(r0 + i0 + i) * cols + n, *staged(stage, i0 + i, lane), bias, extra[i]);
+    }
+}
+
+// The same of an output that is D's transpose: stage row i is output column n0 + i.
+template <int SEG, typename Out>
+__device__ __forceinline__ void put_cols(const Out &o, const float *stage, int lane, int r0, int n0, int rows, int cols,
+                                         const float *bias_p)
+{
+    const int n = n0 + lane;
+    if (n >= cols) return;
+    const float bias = bias_p ? bias_p[n] : 0.0f;
+    const int m = min(SEG, rows - r0);
+    for (int i0 = 0; i0 < m; i0 += 4) {
+        float extra[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) extra[i] = i0 + i < m ? o.extra((size_t)(r0 + i0 + i) * cols + n) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i0 + i < m) o.put((size_t)(r0 + i0 + i) * cols + n, *staged(stage, lane, i0 + i), bias, extra[i]);
+    }
+}
+
+// A warp's 32 rows x 32 NSEG columns of an output with an even number of columns: two neighbours a
+// lane, two rows at a time; stage_in(seg) brings 32 columns of sums into `stage`. What is added to
+// a block of 32 columns (residual, add) is read while the block before it is worked on, and rows
+// are finished four at a time (more of them keep more activations in flight than there are
+// registers).
+template <typename T, bool FORWARD, int ACT, int NSEG, typename StageIn>
+__device__ __forceinline__ void put_pairs(const StageIn &stage_in, const float *stage, int lane, int r0, int n0, int rows,
+                                          int cols, const float *bias_p, const T *extra_p, T *y, T *pre)
+{
+    const int j = (lane & 15) * 2, half = lane >> 4, m = min(32, rows - r0);
+    const size_t step = 2 * (size_t)cols, first = (size_t)(r0 + half) * cols + n0 + j;
+    using Two = typename std::conditional<sizeof(T) == 2, uint32_t, float2>::type;
+    Two next[16] = {}, extra[16];
+    auto fetch = [&](int seg) {
+        if (n0 + seg * 32 + j < cols)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (half + 2 * i < m) next[i] = *(const Two *)(extra_p + first + seg * 32 + i * step);
+    };
+    if (extra_p) fetch(0);
+#pragma unroll 1
+    for (int seg = 0; seg < NSEG; ++seg) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) extra[i] = next[i];
+        if (extra_p && seg + 1 < NSEG) fetch(seg + 1);
+        const int n = n0 + seg * 32 + j;
+        float2 bias = make_float2(0.0f, 0.0f);
+        if (FORWARD && bias_p && n < cols) bias = *(const float2 *)(bias_p + n);
+        stage_in(seg);
+        __syncwarp();
+        if (n < cols) {
+            const size_t at = first + seg * 32;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                if (half + 2 * i < m) {
+                    float2 v = *(const float2 *)staged(stage, half + 2 * i, j), e;
+                    if constexpr (sizeof(T) == 2)
+                        e = __bfloat1622float2(*(const __nv_bfloat162 *)&extra[i]);
+                    else
+                        e = extra[i];
+                    if (FORWARD) {
+                        v.x += bias.x;
+                        v.y += bias.y;
+                        if (pre) store2(pre + at + i * step, v.x, v.y);
+                        v = make_float2(act_f(v.x, ACT), act_f(v.y, ACT));
+                    }
+                    store2(y + at + i * step, v.x + e.x, v.y + e.y);
+                }
+                if (i % 4 == 3) asm volatile("" ::: "memory");
+            }
+        }
+        __syncwarp();
+    }
+}
+template <typename T, int NSEG, typename StageIn>
+__device__ __forceinline__ void put_pairs_forward(const StageIn &in, const Epilogue &ep, const float *stage, int lane, int r0, int n0)
+{
+    const T *res = (const T *)ep.residual;
+    T *y = (T *)ep.y, *pre = (T *)ep.pre;
+    switch (ep.act) {
+    case kActRelu: put_pairs<T, true, kActRelu, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre); break;
+    case kActTanh: put_pairs<T, true, kActTanh, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre); break;
+    case kActGelu: put_pairs<T, true, kActGelu, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre); break;
+    case kActSilu: put_pairs<T, true, kActSilu, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre); break;
+    default: put_pairs<T, true, kActNone, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
+    }
+}
+
+// A warp's 32 rows x SEG NSEG columns of sums to the output.
+template <int SEG, int NSEG, bool GRADIENT, typename StageIn>
+__device__ __forceinline__ void put_tile(const StageIn &in, const Epilogue &ep, bool swapped, int sp, const float *stage,
+                                         int lane, int m0, int n0)
+{
+    const bool plain = GRADIENT || ep.part;
+    const Plain p = {ep.part ? nullptr : ep.add, ep.part ? ep.part + (size_t)sp * ep.rows * ep.cols : ep.out};
+    if (SEG == 32 && ep.cols % 2 == 0 && (GRADIENT || !swapped)) {
+        if (plain)
+            put_pairs<float, false, kActNone, NSEG>(in, stage, lane, m0, n0, ep.rows, ep.cols, nullptr, p.add, p.out, nullptr);
+        else if constexpr (!GRADIENT) {
+            if (ep.bf16_out)
+                put_pairs_forward<__nv_bfloat16, NSEG>(in, ep, stage, lane, m0, n0);
+            else
+                put_pairs_forward<float, NSEG>(in, ep, stage, lane, m0, n0);
+        }
         return;
     }
-    v.x += bias.x;
-    v.y += bias.y;
-    float2 o = make_float2(act_f(v.x, ep.act), act_f(v.y, ep.act));
-    if (ep.bf16_out) {
-        if (ep.pre) *(__nv_bfloat162 *)((__nv_bfloat16 *)ep.pre + at) = __floats2bfloat162_rn(v.x, v.y);
-        if (ep.residual) {
-            const float2 q = __bfloat1622float2(*(const __nv_bfloat162 *)((const __nv_bfloat16 *)ep.residual + at));
-            o.x += q.x;
-            o.y += q.y;
+#pragma unroll 1
+    for (int seg = 0; seg < NSEG; ++seg, n0 += SEG) {
+        in(seg);
+        __syncwarp();
+        if (!GRADIENT && swapped) {
+            if (plain)
+                put_cols<SEG>(p, stage, lane, n0, m0, ep.rows, ep.cols, nullptr);
+            else if (ep.bf16_out)
+                put_cols<SEG>(Forward<__nv_bfloat16>(ep), stage, lane, n0, m0, ep.rows, ep.cols, ep.bias);
+            else
+                put_cols<SEG>(Forward<float>(ep), stage, lane, n0, m0, ep.rows, ep.cols, ep.bias);
+        } else {
+            if (plain)
+                put_rows<SEG>(p, stage, lane, m0, n0, ep.rows, ep.cols, nullptr);
+            else if constexpr (!GRADIENT) {
+                if (ep.bf16_out)
+                    put_rows<SEG>(Forward<__nv_bfloat16>(ep), stage, lane, m0, n0, ep.rows, ep.cols, ep.bias);
+                else
+                    put_rows<SEG>(Forward<float>(ep), stage, lane, m0, n0, ep.rows, ep.cols, ep.bias);
+            }
         }
-        *(__nv_bfloat162 *)((__nv_bfloat16 *)ep.y + at) = __floats2bfloat162_rn(o.x, o.y);
-    } else {
-        if (ep.pre) *(float2 *)((float *)ep.pre + at) = v;
-        if (ep.residual) {
-            const float2 q = *(const float2 *)((const float *)ep.residual + at);
-            o.x += q.x;
-            o.y += q.y;
-        }
-        *(float2 *)((float *)ep.y + at) = o;
+        __syncwarp();
     }
 }
 
+// Three warpgroups: warp 0 for TMA, warp 1 for the MMAs (2 and 3 idle), warps 4-11 for the sums and
+// outputs. They are launched with 168 registers a thread (384 x 168 = 64512); the first group
+// keeps 56 of them and the others take 224 (128 x 56 + 256 x 224 = 64512), so that 128 sums and a
+// batch of reads stay in registers.
 constexpr int kEpiWarps = 8;
-constexpr int kGemmThreads = (kEpiWarps + 2) * 32;  // then one warp for TMA, one for the MMAs
+constexpr int kGemmThreads = (kEpiWarps + 4) * 32;
+static_assert(128 * 56 + kEpiWarps * 32 * 224 <= kGemmThreads * 168, "registers of a CTA");
 constexpr int kMaxRing = 16;
 constexpr uint32_t kTileA = 128 * 128;  // 128 rows (or 2 x 64 columns) x 64 of the contraction
 constexpr uint32_t kStageBytes = kEpiWarps * 32 * 32 * 4;
@@ -253,20 +458,28 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void *tmap, int 
         : "memory");
 }
 
+__device__ __forceinline__ void prefetch_map(const void *tmap)
+{
+    asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)tmap) : "memory");
+}
+
 // D [M][N] += sum over the pairs of A_i B_j^T. A CTA takes units (tile, split) blockIdx.x,
 // + gridDim.x, ...; a unit's chunks go through accumulators of per_acc chunks each, two of them
-// in turn in tensor memory: warps 0-7 add one up in registers (and after the last finish the
+// in turn in tensor memory: the output warps add one up in registers (and after the last finish the
 // tile) while the MMAs fill the other. The tensor cores' fp32 additions cut, so an accumulator
 // that fp32 results come from takes few of them (1.7e-8 of the result each: 1e-4 after 6012).
 // A part is loaded once a chunk, whatever number of products it is in, small products first.
 // MN-major operands: blocks of 64 columns, each 64 rows of 128 bytes.
-template <int BN, bool A_MN, bool B_MN>
+template <int BN, bool A_MN, bool B_MN, int PA, int PB>
 __global__ void __launch_bounds__(kGemmThreads, 1)
 gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
            const __grid_constant__ GemmArgs g)
 {
+    constexpr Pairs<PA, PB> P;
     constexpr uint32_t kTileB = (uint32_t)BN * 128u;
     constexpr int HALF = BN / 2, SEG = HALF < 32 ? HALF : 32;
+    constexpr bool JOINT = PA == 1 && PB == 1;      // A's and B's slots go together: one barrier for both
+    constexpr bool SUMS = A_MN || B_MN || PB == 3;  // fp32 results: several accumulators to a tile
     constexpr uint32_t kCols = 2 * BN < 32 ? 32 : 2 * BN;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *base = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -279,24 +492,26 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
     volatile int *abort = (volatile int *)(tmem_slot + 1);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    if (tid == 0) {
-        for (int s = 0; s < SA; ++s) {
-            tc::mbar_init(&full_a[s], 1);
-            tc::mbar_init(&empty_a[s], 1);
+    if (tid < kMaxRing) {  // (every ring's, used or not)
+        tc::mbar_init(&full_a[tid], 1);
+        tc::mbar_init(&empty_a[tid], 1);
+        tc::mbar_init(&full_b[tid], 1);
+        tc::mbar_init(&empty_b[tid], 1);
+        if (tid < 2) {
+            tc::mbar_init(&acc_full[tid], 1);
+            tc::mbar_init(&acc_empty[tid], kEpiWarps);
         }
-        for (int s = 0; s < SB; ++s) {
-            tc::mbar_init(&full_b[s], 1);
-            tc::mbar_init(&empty_b[s], 1);
+        if (tid == 0) {
+            tc::mbar_init(done, 1);
+            *abort = 0;
         }
-        for (int i = 0; i < 2; ++i) {
-            tc::mbar_init(&acc_full[i], 1);
-            tc::mbar_init(&acc_empty[i], kEpiWarps);
-        }
-        tc::mbar_init(done, 1);
-        *abort = 0;
         tc::fence_mbar_init();
     }
-    if (warp == kEpiWarps) tc::tmem_alloc(tmem_slot, kCols);
+    if (tid == 32) {
+        prefetch_map(&tm_a);
+        prefetch_map(&tm_b);
+    }
+    if (warp == 0) tc::tmem_alloc(tmem_slot, kCols);
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
@@ -338,48 +553,54 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
     };
     Ring ra = {SA}, rb = {SB};
 
-    if (warp == kEpiWarps) {
-        if (lane == 0) {
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if (warp == 0 && lane == 0) {
             long long na = 0, nb = 0;  // loads
             bool ok = true;
             for (long long u = blockIdx.x; ok && u < units; u += gridDim.x) {
                 unit(u, m0, n0, sp, c_lo, c_hi);
                 for (int c = c_lo; ok && c < c_hi; ++c) {
                     const int k0 = c * 64;
-                    for (int p = 0; p < g.npair; ++p) {
-                        const GemmArgs::Pair &pr = g.pair[p];
-                        if (pr.load_b) {
-                            const int s = rb.slot(pr.at_b);
-                            ok = ok && tc::mbar_wait(&empty_b[s], rb.phase(pr.at_b) ^ 1, limit, abort);
-                            if (!ok) break;
-                            tc::mbar_arrive_expect_tx(&full_b[s], kTileB);
-                            ++nb;
-                            const uint32_t dst = ring_b + s * kTileB;
-                            if constexpr (B_MN) {
 #pragma unroll
-                                for (int j = 0; j < BN / 64; ++j)
-                                    tma_load_3d(dst + j * 8192, &tm_b, n0 + j * 64, k0, pr.b, &full_b[s]);
-                            } else {
-                                tma_load_3d(dst, &tm_b, k0, n0, pr.b, &full_b[s]);
+                    for (int p = 0; p < P.n; ++p) {
+                        if (P.load_b[p] && ok) {
+                            const int at = P.at_b[P.b[p]], s = rb.slot(at);
+                            ok = tc::mbar_wait(&empty_b[s], rb.phase(at) ^ 1, limit, abort);
+                            if (ok) {
+                                tc::mbar_arrive_expect_tx(&full_b[s], JOINT ? kTileA + kTileB : kTileB);
+                                ++nb;
+                                const uint32_t dst = ring_b + s * kTileB;
+                                if constexpr (B_MN) {
+#pragma unroll
+                                    for (int j = 0; j < BN / 64; ++j)
+                                        tma_load_3d(dst + j * 8192, &tm_b, n0 + j * 64, k0, P.b[p], &full_b[s]);
+                                } else {
+                                    tma_load_3d(dst, &tm_b, k0, n0, P.b[p], &full_b[s]);
+                                }
                             }
                         }
-                        if (pr.load_a) {
-                            const int s = ra.slot(pr.at_a);
-                            ok = ok && tc::mbar_wait(&empty_a[s], ra.phase(pr.at_a) ^ 1, limit, abort);
-                            if (!ok) break;
-                            tc::mbar_arrive_expect_tx(&full_a[s], kTileA);
-                            ++na;
-                            const uint32_t dst = ring_a + s * kTileA;
-                            if constexpr (A_MN) {
-                                tma_load_3d(dst, &tm_a, m0, k0, pr.a, &full_a[s]);
-                                tma_load_3d(dst + 8192, &tm_a, m0 + 64, k0, pr.a, &full_a[s]);
-                            } else {
-                                tma_load_3d(dst, &tm_a, k0, m0, pr.a, &full_a[s]);
+                        if (P.load_a[p] && ok) {
+                            const int at = P.at_a[P.a[p]], s = ra.slot(at);
+                            uint64_t *full = JOINT ? &full_b[s] : &full_a[s];
+                            if (!JOINT) ok = tc::mbar_wait(&empty_a[s], ra.phase(at) ^ 1, limit, abort);
+                            if (ok) {
+                                if (!JOINT) {
+                                    tc::mbar_arrive_expect_tx(full, kTileA);
+                                    ++na;
+                                }
+                                const uint32_t dst = ring_a + s * kTileA;
+                                if constexpr (A_MN) {
+                                    tma_load_3d(dst, &tm_a, m0, k0, P.a[p], full);
+                                    tma_load_3d(dst + 8192, &tm_a, m0 + 64, k0, P.a[p], full);
+                                } else {
+                                    tma_load_3d(dst, &tm_a, k0, m0, P.a[p], full);
+                                }
                             }
                         }
                     }
-                    ra.next(g.PA);
-                    rb.next(g.PB);
+                    ra.next(PA);
+                    rb.next(PB);
                 }
             }
             if (!ok) fail();
@@ -389,10 +610,9 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
             for (int s = 0; s < SB; ++s)
                 if (nb > s) tc::mbar_wait(&full_b[s], (uint32_t)((nb - 1 - s) / SB) & 1, kDrain, nullptr);
         }
-        __syncwarp();
-    } else if (warp == kEpiWarps + 1) {
-        if (lane == 0) {
+        if (warp == 1 && lane == 0) {
             constexpr uint32_t idesc = tc::idesc_bf16(BN, A_MN, B_MN);
+            const uint64_t desc_a = tc::smem_desc(ring_a, A_MN ? 8192 : 16, 1024), desc_b = tc::smem_desc(ring_b, B_MN ? 8192 : 16, 1024);
             uint32_t acc = 0;  // accumulators filled so far
             bool ok = true;
             for (long long u = blockIdx.x; ok && u < units; u += gridDim.x) {
@@ -405,26 +625,23 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
                     const int c_end = min(c_hi, c + g.per_acc);
                     uint32_t more = 0;
                     for (; ok && c < c_end; ++c) {
-                        for (int p = 0; p < g.npair; ++p) {
-                            const GemmArgs::Pair &pr = g.pair[p];
-                            const int sa = ra.slot(pr.at_a), sb = rb.slot(pr.at_b);
-                            if (pr.load_b) ok = tc::mbar_wait(&full_b[sb], rb.phase(pr.at_b), limit, abort);
-                            if (ok && pr.load_a) ok = tc::mbar_wait(&full_a[sa], ra.phase(pr.at_a), limit, abort);
-                            if (!ok) break;
-                            tc::tc_fence_after();
-                            const uint32_t as = ring_a + sa * kTileA, bs = ring_b + sb * kTileB;
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) {  // 16 of the contraction: 32 bytes of a row, or 16 rows
-                                tc::mma_bf16(d, A_MN ? tc::smem_desc(as + k * 2048, 8192, 1024) : tc::smem_desc(as + k * 32, 16, 1024),
-                                             B_MN ? tc::smem_desc(bs + k * 2048, 8192, 1024) : tc::smem_desc(bs + k * 32, 16, 1024),
-                                             idesc, more);
-                                more = 1;
+                        for (int p = 0; p < P.n; ++p) {
+                            const int ia = P.at_a[P.a[p]], ib = P.at_b[P.b[p]], sa = ra.slot(ia), sb = rb.slot(ib);
+                            if (P.load_b[p] && ok) ok = tc::mbar_wait(&full_b[sb], rb.phase(ib), limit, abort);
+                            if (P.load_a[p] && ok && !JOINT) ok = tc::mbar_wait(&full_a[sa], ra.phase(ia), limit, abort);
+                            if (ok) {
+                                const uint64_t da = desc_a + (uint32_t)sa * (kTileA >> 4), db = desc_b + (uint32_t)sb * (kTileB >> 4);
+#pragma unroll
+                                for (int k = 0; k < 4; ++k)  // 16 of the contraction: 32 bytes of a row, or 16 rows
+                                    tc::mma_bf16(d, da + k * (A_MN ? 128 : 2), db + k * (B_MN ? 128 : 2), idesc, k || p ? 1 : more);
+                                if (P.free_a[p] && !JOINT) tc::mma_commit(&empty_a[sa]);
+                                if (P.free_b[p]) tc::mma_commit(&empty_b[sb]);
                             }
-                            if (pr.free_a) tc::mma_commit(&empty_a[sa]);
-                            if (pr.free_b) tc::mma_commit(&empty_b[sb]);
                         }
-                        ra.next(g.PA);
-                        rb.next(g.PB);
+                        more = 1;
+                        ra.next(PA);
+                        rb.next(PB);
                     }
                     if (ok) tc::mma_commit(&acc_full[acc & 1]);
                 }
@@ -435,97 +652,104 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
         }
         __syncwarp();
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         // ------------------------------------------------------ sums and outputs
-        const int q = warp & 3, half = warp >> 2;  // a warp reads its quadrant of the lanes
-        float *stage = (float *)(base + kRingBytes) + warp * 1024;
-        const Epilogue &ep = g.ep;
+        const int q = warp & 3, half = (warp >> 2) - 1;  // a warp reads its quadrant of the lanes
+        float *stage = (float *)(base + kRingBytes) + (warp - 4) * 1024;
         uint32_t acc = 0;
         bool ok = true;
         for (long long u = blockIdx.x; ok && u < units; u += gridDim.x) {
             unit(u, m0, n0, sp, c_lo, c_hi);
-            float sum[HALF];
-            for (int c = c_lo; c < c_hi; c += g.per_acc, ++acc) {
-                // (the whole warp: its reads of tensor memory are collective)
-                ok = __all_sync(0xffffffffu, tc::mbar_wait(&acc_full[acc & 1], (acc >> 1) & 1, limit, abort));
-                if (!ok) break;
+            const int mm = m0 + q * 32, nn = n0 + half * HALF;
+            float *mine = stage + lane * 32;
+            // (the whole warp waits together: its reads of tensor memory are collective)
+            auto filled = [&]() {
+                const bool got = __all_sync(0xffffffffu, tc::mbar_wait(&acc_full[acc & 1], (acc >> 1) & 1, limit, abort));
                 tc::tc_fence_after();
-                const uint32_t at = tmem + ((uint32_t)(q * 32) << 16) + (acc & 1) * BN + half * HALF;
-                if (c == c_lo) {
-#pragma unroll
-                    for (int i = 0; i < HALF; i += 16) tc::tmem_ld16(at + i, *(float(*)[16])(sum + i));
-                } else {
-#pragma unroll
-                    for (int i = 0; i < HALF; i += 16) {
-                        float v[16];
-                        tc::tmem_ld16(at + i, v);
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) sum[i + j] += v[j];
-                    }
-                }
+                return got;
+            };
+            auto release = [&]() {
                 tc::tc_fence_before();
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(&acc_empty[acc & 1]);
-            }
-            if (!ok) break;
-            // through shared memory, 32 rows x SEG columns at a time (16-byte pieces of row r at
-            // piece ^ (r mod 8)), so that a row's neighbours are a warp's
-            const int mm = m0 + q * 32, nn = n0 + half * HALF;
-            Epilogue o = ep;
-            if (ep.part) {  // plain sums
-                o.out = ep.part + (size_t)sp * ep.rows * ep.cols;
-                o.add = nullptr;
-            }
-            const bool pairs = ep.cols % 2 == 0;
+                ++acc;
+            };
+            auto read = [&](int col, uint32_t (&v)[SEG / 16][16]) {  // SEG columns, their reads in flight together
+                const uint32_t at = tmem + ((uint32_t)(q * 32) << 16) + (acc & 1) * BN + half * HALF + col;
 #pragma unroll
-            for (int s0 = 0; s0 < HALF; s0 += SEG) {
+                for (int j = 0; j < SEG / 16; ++j) tc::tmem_ld16_async(at + 16 * j, v[j]);
+                tc::tmem_wait_ld();
+            };
+            if constexpr (SUMS) {
+                float sum[HALF];
 #pragma unroll
-                for (int i = 0; i < SEG / 4; ++i)
-                    *(float4 *)(stage + lane * 32 + ((i ^ (lane & 7)) << 2)) =
-                        make_float4(sum[s0 + 4 * i], sum[s0 + 4 * i + 1], sum[s0 + 4 * i + 2], sum[s0 + 4 * i + 3]);
-                __syncwarp();
-                if (g.swapped) {
-                    const int n = mm + lane;
-                    for (int i = 0; i < SEG; ++i) {
-                        const int r = nn + s0 + i;
-                        if (n < ep.cols && r < ep.rows) finish(o, r, n, stage[lane * 32 + (((i >> 2) ^ (lane & 7)) << 2) + (i & 3)]);
+                for (int i = 0; i < HALF; ++i) sum[i] = 0.0f;
+#pragma unroll 1
+                for (int c = c_lo; c < c_hi; c += g.per_acc) {
+                    if (!(ok = filled())) break;
+#pragma unroll
+                    for (int i = 0; i < HALF; i += SEG) {
+                        uint32_t v[SEG / 16][16];
+                        read(i, v);
+#pragma unroll
+                        for (int j = 0; j < SEG; ++j) sum[i + j] += __uint_as_float(v[j / 16][j % 16]);
                     }
-                } else if (pairs && SEG == 32) {
-                    const int j = lane & 15, n = nn + s0 + 2 * j;
-                    float2 bias = make_float2(0.0f, 0.0f);
-                    if (n < ep.cols && !o.out && ep.bias) bias = *(const float2 *)(ep.bias + n);
-                    if (n < ep.cols)
-#pragma unroll 4
-                        for (int i = 0; i < 16; ++i) {
-                            const int rr = 2 * i + (lane >> 4), r = mm + rr;
-                            if (r < ep.rows)
-                                finish2(o, r, n, *(const float2 *)(stage + rr * 32 + (((j >> 1) ^ (rr & 7)) << 2) + ((j & 1) << 1)), bias);
-                        }
-                } else {
-                    const int j = lane, n = nn + s0 + j;
-                    if (j < SEG && n < ep.cols)
-                        for (int rr = 0; rr < 32; ++rr)
-                            if (mm + rr < ep.rows) finish(o, mm + rr, n, stage[rr * 32 + (((j >> 2) ^ (rr & 7)) << 2) + (j & 3)]);
+                    release();
                 }
-                __syncwarp();
+                if (!ok) break;
+                auto in = [&](int seg) {
+#pragma unroll
+                    for (int k = 0; k < HALF / SEG; ++k)
+                        if (seg == k)
+#pragma unroll
+                            for (int i = 0; i < SEG / 4; ++i) {
+                                const float *v = sum + k * SEG + 4 * i;
+                                *(float4 *)(mine + ((i ^ (lane & 7)) << 2)) = make_float4(v[0], v[1], v[2], v[3]);
+                            }
+                };
+                put_tile<SEG, HALF / SEG, A_MN || B_MN>(in, g.ep, g.swapped, sp, stage, lane, mm, nn);
+            } else {
+                if (!(ok = filled())) break;
+                auto in = [&](int seg) {
+                    uint32_t v[SEG / 16][16];
+                    read(seg * SEG, v);
+#pragma unroll
+                    for (int i = 0; i < SEG / 4; ++i)
+                        *(uint4 *)(mine + ((i ^ (lane & 7)) << 2)) =
+                            make_uint4(v[i / 4][i % 4 * 4], v[i / 4][i % 4 * 4 + 1], v[i / 4][i % 4 * 4 + 2], v[i / 4][i % 4 * 4 + 3]);
+                    if (seg == HALF / SEG - 1) release();
+                };
+                put_tile<SEG, HALF / SEG, false>(in, g.ep, g.swapped, sp, stage, lane, mm, nn);
             }
         }
         if (!ok && lane == 0) fail();
     }
     tc::tc_fence_before();
     __syncthreads();
-    if (warp == kEpiWarps) tc::tmem_dealloc(tmem, kCols);
+    if (warp == 0) tc::tmem_dealloc(tmem, kCols);
 }
 
 // The splits' sums of each output added in split order, then its epilogue.
-__global__ void __launch_bounds__(256)
-join_splits(const Epilogue ep, int split)
+template <typename Out>
+__device__ __forceinline__ void join(const Epilogue &ep, int split, const Out &o)
 {
     const size_t n = (size_t)ep.rows * ep.cols;
     for (size_t e = blockIdx.x * (size_t)256 + threadIdx.x; e < n; e += (size_t)gridDim.x * 256) {
         float v = 0.0f;
+#pragma unroll 4
         for (int s = 0; s < split; ++s) v += ep.part[(size_t)s * n + e];
-        finish(ep, (int)(e / ep.cols), (int)(e % ep.cols), v);
+        o.put(e, v, ep.bias ? ep.bias[e % ep.cols] : 0.0f, o.extra(e));
     }
+}
+__global__ void __launch_bounds__(256)
+join_splits(const __grid_constant__ Epilogue ep, int split)
+{
+    if (ep.out)
+        join(ep, split, Plain{ep.add, ep.out});
+    else if (ep.bf16_out)
+        join(ep, split, Forward<__nv_bfloat16>(ep));
+    else
+        join(ep, split, Forward<float>(ep));
 }
 
 // ------------------------------------------------------------------ host side
@@ -565,16 +789,16 @@ cudaError_t operand_map(CUtensorMap *tm, const Operand &o, int box_rows)
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-template <int BN, bool A_MN, bool B_MN>
+template <int BN, bool A_MN, bool B_MN, int PA, int PB>
 cudaError_t launch_gemm(const stacklstm_op *op, const Operand &a, const Operand &b, const GemmArgs &g)
 {
     CUtensorMap ta, tb;
     cudaError_t e = operand_map(&ta, a, A_MN ? 64 : 128);
     if (!e) e = operand_map(&tb, b, B_MN ? 64 : BN);
-    if (!e) e = smem_at_least((const void *)gemm_parts<BN, A_MN, B_MN>, kGemmSmem);
+    if (!e) e = smem_at_least((const void *)gemm_parts<BN, A_MN, B_MN, PA, PB>, kGemmSmem);
     if (e) return e;
     const unsigned grid = (unsigned)std::min<long long>((long long)g.mt * g.nt * g.split, op->num_sms);
-    gemm_parts<BN, A_MN, B_MN><<<grid, kGemmThreads, kGemmSmem, op->stream>>>(ta, tb, g);
+    gemm_parts<BN, A_MN, B_MN, PA, PB><<<grid, kGemmThreads, kGemmSmem, op->stream>>>(ta, tb, g);
     return cudaGetLastError();
 }
 
@@ -585,12 +809,12 @@ constexpr size_t kMostPartBytes = (size_t)1 << 30;  // of the splits' sums
 // Tile width and splits: the least of waves x chunks x cycles a chunk (two cycles a column and
 // product, and no fewer than the operands' bytes take at 64 a cycle), a tile's start and end, and
 // for a split contraction its sums written and read again, and a second launch.
-void plan_gemm(GemmArgs &g, int M, int N, int bn_lo, int bn_hi, size_t out_elems, int sms, int *bn_out)
+void plan_gemm(GemmArgs &g, int PA, int PB, int npair, int M, int N, int bn_lo, int bn_hi, size_t out_elems, int sms, int *bn_out)
 {
     double best = 1e300;
     for (int bn = bn_lo; bn <= bn_hi; bn *= 2) {
         const double mt = ceil_div(M, 128), nt = ceil_div(N, bn);
-        const double cyc = std::max(2.0 * bn * g.npair, (g.PA * (double)kTileA + g.PB * bn * 128.0) / 64.0);
+        const double cyc = std::max(2.0 * bn * npair, (PA * (double)kTileA + PB * bn * 128.0) / 64.0);
         for (int split = 1; split <= std::min(g.chunks, 64); ++split) {
             if (split > 1 && (g.chunks / split < 2 || (double)split * out_elems * 4 > (double)kMostPartBytes)) break;
             const double waves = std::ceil(mt * nt * split / sms), chunks = std::ceil((double)g.chunks / split);
@@ -608,57 +832,30 @@ void plan_gemm(GemmArgs &g, int M, int N, int bn_lo, int bn_hi, size_t out_elems
 }
 
 // D = sum over the parts' products of A B^T, kcols long, and its epilogue.
-template <bool A_MN, bool B_MN>
-cudaError_t contract(stacklstm_op *op, const Operand &a, const Operand &b, int kcols, bool swapped, Epilogue ep)
+template <bool A_MN, bool B_MN, int PA, int PB>
+cudaError_t contract_parts(stacklstm_op *op, const Operand &a, const Operand &b, int kcols, bool swapped, Epilogue ep)
 {
+    constexpr Pairs<PA, PB> P;
     GemmArgs g = {};
     g.chunks = (int)ceil_div(kcols, 64);
-    g.PA = a.parts;
-    g.PB = b.parts;
-    // partial products, small ones first; a part's place is that of its first use
-    int next_a = 0, next_b = 0, place_a[3] = {-1, -1, -1}, place_b[3] = {-1, -1, -1};
-    for (int order = 2; order >= 0; --order)
-        for (int i = 0; i < a.parts; ++i) {
-            const int j = order - i;
-            if (j < 0 || j >= b.parts) continue;
-            GemmArgs::Pair &p = g.pair[g.npair++];
-            p.a = (uint8_t)i;
-            p.b = (uint8_t)j;
-            if ((p.load_a = place_a[i] < 0)) place_a[i] = next_a++;
-            if ((p.load_b = place_b[j] < 0)) place_b[j] = next_b++;
-            p.at_a = (uint8_t)place_a[i];
-            p.at_b = (uint8_t)place_b[j];
-        }
-    for (int i = 0; i < a.parts; ++i)
-        for (int p = g.npair - 1; p >= 0; --p)
-            if (g.pair[p].a == i) {
-                g.pair[p].free_a = 1;
-                break;
-            }
-    for (int j = 0; j < b.parts; ++j)
-        for (int p = g.npair - 1; p >= 0; --p)
-            if (g.pair[p].b == j) {
-                g.pair[p].free_b = 1;
-                break;
-            }
     // fp32 results: 24 MMAs to an accumulator
-    g.per_acc = ep.out || !ep.bf16_out ? std::max(1, 6 / g.npair) : g.chunks;
+    g.per_acc = ep.out || !ep.bf16_out ? std::max(1, 6 / P.n) : g.chunks;
     g.swapped = swapped;
     g.limit = op->wait_limit;
     g.err = op->err;
     const int M = swapped ? ep.cols : ep.rows, N = swapped ? ep.rows : ep.cols;
     // (three parts of a 256-wide B leave the rings no second chunk)
-    const int most = b.parts == 3 ? 128 : 256;
+    constexpr int most = PB == 3 ? 128 : 256;
     const int lo = swapped && N <= 32 ? 32 : 64, hi = N <= lo ? lo : N <= 64 ? 64 : N <= 128 ? 128 : most;
     int bn = 64;
-    plan_gemm(g, M, N, lo, hi, (size_t)ep.rows * ep.cols, op->num_sms, &bn);
-    // rings: as many whole chunks as fit, what is left to B, then to A
-    const uint32_t tb = (uint32_t)bn * 128, per = g.PA * kTileA + g.PB * tb;
-    const int depth = (int)(kRingBytes / per);
-    g.SA = std::min(kMaxRing / g.PA, depth) * g.PA;
-    g.SB = std::min(kMaxRing / g.PB, depth) * g.PB;
-    while (g.SB < kMaxRing && g.SA * kTileA + (g.SB + 1) * tb <= kRingBytes && g.PB < g.PA) ++g.SB;
-    while (g.SA < kMaxRing && (g.SA + 1) * kTileA + g.SB * tb <= kRingBytes) ++g.SA;
+    plan_gemm(g, PA, PB, P.n, M, N, lo, hi, (size_t)ep.rows * ep.cols, op->num_sms, &bn);
+    // rings: as many whole chunks as fit, what is left to the single part of B, then to A
+    const uint32_t tb = (uint32_t)bn * 128;
+    const int depth = (int)(kRingBytes / (PA * kTileA + PB * tb));
+    g.SA = std::min(kMaxRing / PA, depth) * PA;
+    g.SB = std::min(kMaxRing / PB, depth) * PB;
+    while (g.SB < kMaxRing && g.SA * kTileA + (g.SB + 1) * tb <= kRingBytes && PB < PA) ++g.SB;
+    while (PA > 1 && g.SA < kMaxRing && (g.SA + 1) * kTileA + g.SB * tb <= kRingBytes) ++g.SA;
     if (g.split > 1) {
         cudaError_t e = op_workspace(op, kWsPart, (size_t)g.split * ep.rows * ep.cols * 4);
         if (e) return e;
@@ -667,16 +864,28 @@ cudaError_t contract(stacklstm_op *op, const Operand &a, const Operand &b, int k
     g.ep = ep;
     cudaError_t e = cudaErrorInvalidValue;
     if constexpr (!A_MN && !B_MN)
-        if (bn == 32) e = launch_gemm<32, A_MN, B_MN>(op, a, b, g);
-    if (bn == 64) e = launch_gemm<64, A_MN, B_MN>(op, a, b, g);
-    if (bn == 128) e = launch_gemm<128, A_MN, B_MN>(op, a, b, g);
-    if (bn == 256) e = launch_gemm<256, A_MN, B_MN>(op, a, b, g);
+        if (bn == 32) e = launch_gemm<32, A_MN, B_MN, PA, PB>(op, a, b, g);
+    if (bn == 64) e = launch_gemm<64, A_MN, B_MN, PA, PB>(op, a, b, g);
+    if (bn == 128) e = launch_gemm<128, A_MN, B_MN, PA, PB>(op, a, b, g);
+    if constexpr (PB == 1)
+        if (bn == 256) e = launch_gemm<256, A_MN, B_MN, PA, PB>(op, a, b, g);
     if (!e && g.split > 1) {
         join_splits<<<(unsigned)std::min<size_t>(ceil_div((size_t)ep.rows * ep.cols, 256), (size_t)op->num_sms * 8), 256, 0,
                       op->stream>>>(ep, g.split);
         e = cudaGetLastError();
     }
     return e;
+}
+
+// (x and W have the parts of their type, dz always three)
+template <bool A_MN, bool B_MN>
+cudaError_t contract(stacklstm_op *op, const Operand &a, const Operand &b, int kcols, bool swapped, const Epilogue &ep)
+{
+    if (b.parts == 3) return contract_parts<A_MN, B_MN, 3, 3>(op, a, b, kcols, swapped, ep);
+    if constexpr (A_MN || B_MN)
+        return contract_parts<A_MN, B_MN, 3, 1>(op, a, b, kcols, swapped, ep);
+    else
+        return contract_parts<A_MN, B_MN, 1, 1>(op, a, b, kcols, swapped, ep);
 }
 
 int row_ld(int cols) { return (cols + 7) / 8 * 8; }
@@ -776,12 +985,14 @@ sl_status stacklstm_linear_backward(stacklstm_op_t op, int rows, const float *dy
     if (dbias && (e = op_workspace(op, kWsSum, (size_t)blocks * N * 4))) return op_cuda(op, e, "stacklstm_linear_backward");
     const dim3 grid(blocks, ceil_div(N, kDzCols));
     float *sums = dbias ? (float *)op->ws[kWsSum] : nullptr;
+    auto launch = [&](auto kernel, auto *p) {
+        kernel<<<grid, 32 * kDzSub, 0, op->stream>>>(rows, N, ld, op->act, dy, p, (__nv_bfloat16 *)dz.p, sums);
+    };
+    const bool aligned = N % 4 == 0;
     if (op->dt == SL_BF16)
-        dz_parts<<<grid, kDzCols, 0, op->stream>>>(rows, N, ld, op->act, dy, (const __nv_bfloat16 *)pre,
-                                                   (__nv_bfloat16 *)dz.p, sums);
+        launch(aligned ? dz_parts<__nv_bfloat16, true> : dz_parts<__nv_bfloat16, false>, (const __nv_bfloat16 *)pre);
     else
-        dz_parts<<<grid, kDzCols, 0, op->stream>>>(rows, N, ld, op->act, dy, (const float *)pre, (__nv_bfloat16 *)dz.p,
-                                                   sums);
+        launch(aligned ? dz_parts<float, true> : dz_parts<float, false>, (const float *)pre);
     e = cudaGetLastError();
     if (!e && dbias) {
         sum_parts<<<ceil_div(N, 32), 256, 0, op->stream>>>(sums, (int)blocks, N, dbias);
