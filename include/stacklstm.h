@@ -465,7 +465,7 @@ sl_status stacklstm_distill_run(stacklstm_op_t op, int rows, const void *logits,
 /*
  * Beam search: B sentences with K hypotheses each (row n = b K + k), V classes (transitions or
  * words), stacks of S slots and H units per row (S = T + 1 slots hold any T transitions).
- * K <= 64, B <= 65535, K V <= 2^30.
+ * K <= 64, B <= 65535, K V <= 2^30, S <= 1048560.
  * stacklstm_beam_lse: lse [B, K] (float) = ln sum_v exp(logits [B, K, V]) (dtype); -inf for a row
  *   of -inf.
  * stacklstm_beam_select: candidate (k, v) of sentence b scores

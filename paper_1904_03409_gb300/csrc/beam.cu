@@ -20,55 +20,56 @@ constexpr int kSelThreads = 256;
 constexpr int kSelItems = 32;                          // candidates a thread
 constexpr int kSegment = kSelThreads * kSelItems;      // candidates a CTA
 constexpr int kMergeItems = 16;                        // keys a thread and pass of the merge
+constexpr int kWideRow = 1024;                         // classes from which a CTA keeps to one row
 constexpr int kMaxBeams = 64;
 
 // ------------------------------------------------------------------ normalisers
 template <typename T, int TPR, int NP>
-__global__ void __launch_bounds__(TPR == 32 ? 256 : TPR)
+__global__ void __launch_bounds__(row_cta(TPR), row_ctas_per_sm(TPR))
 lse_rows(int rows, int V, const T *__restrict__ z, float *__restrict__ lse)
 {
     constexpr int E = RowVec<T>::E, RPC = TPR == 32 ? 8 : 1;
-    __shared__ float sm[kRowThreads / 32];
+    __shared__ float sm[32];
     const int r = blockIdx.x * RPC + (TPR == 32 ? threadIdx.x / 32 : 0), t = threadIdx.x % TPR;
     if (r >= rows) return;
-    const RowVec<T> row(r, V, rows);
+    const RowVec<T> row(r, V);
     const int n = row.pieces();
-    float v[NP > 0 ? NP : 1][E];
-    float m = -INFINITY, s = 0.0f;
+    uint4 q[NP > 0 ? NP : 1];
     if constexpr (NP > 0) {
 #pragma unroll
         for (int j = 0; j < NP; ++j)
-            if (j * TPR + t < n) row.load(z, j * TPR + t, v[j]);
-#pragma unroll
-        for (int j = 0; j < NP; ++j)
-            if (j * TPR + t < n)
-#pragma unroll
-                for (int i = 0; i < E; ++i) m = max_nan(m, v[j][i]);
-    } else {
-        for (int p = t; p < n; p += TPR) {
-            row.load(z, p, v[0]);
-#pragma unroll
-            for (int i = 0; i < E; ++i) m = max_nan(m, v[0][i]);
-        }
+            if (j * TPR + t < n) q[j] = row.load(z, j * TPR + t);
     }
-    m = row_max<TPR>(m, sm);
-    const float base = m == -INFINITY ? 0.0f : m;  // a row of -inf sums to 0: its lse is -inf
-    auto add = [&](const float (&w)[E]) {
+    auto each = [&](auto f) {
+        if constexpr (NP > 0) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) s += exp2_hw((w[i] - base) * kLog2e);
+            for (int j = 0; j < NP; ++j)
+                if (j * TPR + t < n) {
+                    float v[E];
+                    unpack<T>(q[j], v);
+                    f(v);
+                }
+        } else {
+            for (int p = t; p < n; p += TPR) {
+                float v[E];
+                unpack<T>(row.load(z, p), v);
+                f(v);
+            }
+        }
     };
-    if constexpr (NP > 0) {
+    float m[1] = {-INFINITY}, s[1] = {0.0f};
+    each([&](const float (&v)[E]) {
 #pragma unroll
-        for (int j = 0; j < NP; ++j)
-            if (j * TPR + t < n) add(v[j]);
-    } else {
-        for (int p = t; p < n; p += TPR) {
-            row.load(z, p, v[0]);
-            add(v[0]);
-        }
-    }
-    s = row_sum<TPR>(s, sm);
-    if (t == 0) lse[r] = base + logf(s);
+        for (int i = 0; i < E; ++i) m[0] = max_nan(m[0], v[i]);
+    });
+    row_join<true, TPR>(m, sm);
+    const float base = m[0] == -INFINITY ? 0.0f : m[0];  // a row of -inf sums to 0: its lse is -inf
+    each([&](const float (&v)[E]) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) s[0] += exp2_hw((v[i] - base) * kLog2e);
+    });
+    row_join<false, TPR>(s, sm);
+    if (t == 0) lse[r] = base + logf(s[0]);
 }
 
 template <typename T>
@@ -78,10 +79,8 @@ cudaError_t launch_lse(int rows, int V, const void *z, float *lse, cudaStream_t 
     row_plan<T>(V, &tpr, &np);
     const unsigned grid = ceil_div(rows, tpr == 32 ? 8 : 1);
 #define SL_LSE(t, n) \
-    if (tpr == t && np == n) lse_rows<T, t, n><<<grid, t == 32 ? 256 : t, 0, st>>>(rows, V, (const T *)z, lse);
-    SL_LSE(32, 1) SL_LSE(32, 2) SL_LSE(32, 4)
-    SL_LSE(kRowThreads, 0) SL_LSE(kRowThreads, 1) SL_LSE(kRowThreads, 2) SL_LSE(kRowThreads, 4)
-    SL_LSE(kRowThreads, 8) SL_LSE(kRowThreads, 16)
+    if (tpr == t && np == n) lse_rows<T, t, n><<<grid, row_cta(t), 0, st>>>(rows, V, (const T *)z, lse);
+    SL_ROW_PLANS(SL_LSE)
 #undef SL_LSE
     return cudaGetLastError();
 }
@@ -100,46 +99,79 @@ __device__ __forceinline__ float key_score(u64 key)
     return __uint_as_float((o & 0x80000000u) ? o & 0x7FFFFFFFu : ~o);
 }
 
+constexpr int kList = 1024;  // keys that are ranked together, most times
+
 struct SelShared {
-    u64 top[kSelThreads];                // each thread's best key
-    u64 best[kMaxBeams];                 // the K best, sorted
+    u64 top[kSelThreads];  // the groups' (threads') best keys
+    u64 best[kMaxBeams];   // the K best, sorted
+    u64 list[kList];
     u64 kth;
     int count, last;
     float score[kMaxBeams], lse[kMaxBeams];
     uint8_t done[kMaxBeams];
 };
 
-// The K best of the CTA's keys (PT a thread; list: room for K PT keys), sorted, into s.best.
-// Each thread's best key is ranked among the threads': the K best keys are all in the K threads
-// with the best of these, and none is below the K-th of them.
-template <int PT>
-__device__ __forceinline__ void block_topk(const u64 (&key)[PT], int K, SelShared &s, u64 *list)
+// The K best of the CTA's keys into s.best, sorted. `mine` is the thread's best key and
+// push(bound, f) calls f with each of the thread's keys that are >= bound. Of any disjoint groups
+// of keys, the K-th best of the groups' best is no better than the K-th best of all: first the
+// threads' best are grouped (8 lanes a group, 4 for more than 32 hypotheses) and the keys from
+// that bound on are listed and ranked against one another. Where they are more than the list
+// holds (most of a row alike), the bound is the K-th of the threads' own best, from which on there
+// are at most K times a thread's keys, in `spill`.
+template <typename Push>
+__device__ __forceinline__ void block_topk(u64 mine, const Push &push, int K, SelShared &s, u64 *spill)
 {
-    const int tid = threadIdx.x;
-    u64 mine = 0;
-#pragma unroll
-    for (int i = 0; i < PT; ++i) mine = key[i] > mine ? key[i] : mine;
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int width = K <= 32 ? 8 : 4, groups = kSelThreads / width;
+    u64 g = mine;
+    for (int o = 1; o < width; o <<= 1) {
+        const u64 w = __shfl_xor_sync(0xffffffffu, g, o);
+        g = w > g ? w : g;
+    }
     __syncthreads();
-    s.top[tid] = mine;
+    if (lane % width == 0) s.top[tid / width] = g;
     if (tid == 0) {
         s.count = 0;
-        s.kth = 1;  // fewer than K threads with a candidate: every one counts
+        s.kth = 1;  // fewer than K groups with a candidate: every one counts
     }
     if (tid < K) s.best[tid] = 0;
     __syncthreads();
-    int rank = 0;
-    if (mine)
-        for (int i = 0; i < kSelThreads; ++i) rank += s.top[i] > mine;
-    if (mine && rank == K - 1) s.kth = mine;
-    __syncthreads();
-    const u64 kth = s.kth;
-    if (mine && rank < K) {
-#pragma unroll
-        for (int i = 0; i < PT; ++i)
-            if (key[i] >= kth) list[atomicAdd(&s.count, 1)] = key[i];  // any order: they are ranked below
+    if (tid < groups) {
+        const u64 k = s.top[tid];
+        int above = 0;
+#pragma unroll 8
+        for (int i = 0; i < groups; ++i) above += s.top[i] > k;
+        if (k && above == K - 1) s.kth = k;
     }
     __syncthreads();
-    const int n = s.count;
+    const u64 bound = s.kth;
+    if (mine >= bound)
+        push(bound, [&](u64 k) {
+            const int at = atomicAdd(&s.count, 1);  // any order: they are ranked below
+            if (at < kList) s.list[at] = k;
+        });
+    __syncthreads();
+    int n = s.count;
+    u64 *list = s.list;
+    if (n > kList) {
+        list = spill;
+        __syncthreads();
+        s.top[tid] = mine;
+        if (tid == 0) {
+            s.count = 0;
+            s.kth = 1;
+        }
+        __syncthreads();
+        int above = 0;
+        if (mine)
+            for (int i = 0; i < kSelThreads; ++i) above += s.top[i] > mine;
+        if (mine && above == K - 1) s.kth = mine;
+        __syncthreads();
+        const u64 tight = s.kth;
+        if (mine >= tight) push(tight, [&](u64 k) { list[atomicAdd(&s.count, 1)] = k; });
+        __syncthreads();
+        n = s.count;
+    }
     for (int e = tid; e < n; e += kSelThreads) {
         const u64 k = list[e];
         int above = 0;
@@ -149,24 +181,97 @@ __device__ __forceinline__ void block_topk(const u64 (&key)[PT], int K, SelShare
     __syncthreads();
 }
 
-template <typename T>
+// Keys that a thread has at hand.
+template <int PT>
+__device__ __forceinline__ void keys_topk(const u64 (&key)[PT], int K, SelShared &s, u64 *spill)
+{
+    u64 mine = 0;
+#pragma unroll
+    for (int i = 0; i < PT; ++i) mine = key[i] > mine ? key[i] : mine;
+    block_topk(mine, [&](u64 bound, auto f) {
+#pragma unroll
+        for (int i = 0; i < PT; ++i)
+            if (key[i] >= bound) f(key[i]);
+    }, K, s, spill);
+}
+
+// Sentence blockIdx.y; the candidates of segment blockIdx.x: kSegment of the sentence's K V
+// (ROWS = false), or kSegment of the V of hypothesis blockIdx.x / per_row. The K best of each
+// segment go to `part`, and the sentence's last CTA joins them.
+template <typename T, bool ROWS>
 __global__ void __launch_bounds__(kSelThreads)
-beam_select(int K, int V, int nseg, const T *__restrict__ z, const float *__restrict__ lse, const float *__restrict__ score,
-            const uint8_t *__restrict__ done, u64 *__restrict__ part, int *__restrict__ arrived,
-            float *__restrict__ out_score, int32_t *__restrict__ parent, int32_t *__restrict__ token)
+beam_select(int K, int V, int nseg, int per_row, const T *__restrict__ z, const float *__restrict__ lse,
+            const float *__restrict__ score, const uint8_t *__restrict__ done, u64 *__restrict__ part,
+            int *__restrict__ arrived, float *__restrict__ out_score, int32_t *__restrict__ parent,
+            int32_t *__restrict__ token)
 {
     __shared__ SelShared s;
-    extern __shared__ u64 list[];
+    extern __shared__ u64 spill[];
     const int tid = threadIdx.x, b = blockIdx.y, seg = blockIdx.x;
     if (tid < K) {
         s.score[tid] = score[(size_t)b * K + tid];
         s.lse[tid] = lse ? lse[(size_t)b * K + tid] : 0.0f;
         s.done[tid] = done ? done[(size_t)b * K + tid] : 0;
     }
-    __syncthreads();
-    const uint32_t n = (uint32_t)K * (uint32_t)V;
-    const T *zb = z + (size_t)b * n;
-    {
+    if constexpr (ROWS) {
+        constexpr int E = RowVec<T>::E, NP = kSelItems / E;
+        const int k = seg / per_row, piece0 = seg % per_row * (kSegment / E) + tid;
+        const RowVec<T> row((size_t)b * K + k, V);
+        const int n = row.pieces();
+        uint4 q[NP];
+#pragma unroll
+        for (int j = 0; j < NP; ++j)
+            if (piece0 + j * kSelThreads < n) q[j] = row.load(z, piece0 + j * kSelThreads);
+        __syncthreads();
+        const float add = s.score[k], sub = s.lse[k];
+        const bool is_done = s.done[k];
+        const uint32_t place0 = (uint32_t)k * (uint32_t)V;
+        u64 mine = 0;
+        if (is_done) {
+            if (seg % per_row == 0 && tid == 0) mine = make_key(add, place0);
+        } else {
+            float top = -INFINITY;
+            uint32_t at = 0;
+#pragma unroll
+            for (int j = 0; j < NP; ++j)
+                if (piece0 + j * kSelThreads < n) {
+                    float v[E];
+                    unpack<T>(q[j], v);
+#pragma unroll
+                    for (int i = 0; i < E; ++i) {  // places go up: of equal scores the first stays
+                        const float c = __fadd_rn(add, __fsub_rn(v[i], sub));
+                        if (c > top) {
+                            top = c;
+                            at = (uint32_t)(row.column(piece0 + j * kSelThreads) + i);
+                        }
+                    }
+                }
+            if (top > -INFINITY) mine = make_key(top, place0 + at);
+        }
+        block_topk(mine, [&](u64 bound, auto f) {
+            if (is_done) {
+                f(mine);
+                return;
+            }
+            const float least = bound > 1 ? key_score(bound) : -INFINITY;
+#pragma unroll
+            for (int j = 0; j < NP; ++j)
+                if (piece0 + j * kSelThreads < n) {
+                    float v[E];
+                    unpack<T>(q[j], v);
+#pragma unroll
+                    for (int i = 0; i < E; ++i) {
+                        const float c = __fadd_rn(add, __fsub_rn(v[i], sub));
+                        if (c >= least) {
+                            const u64 key = make_key(c, place0 + (uint32_t)(row.column(piece0 + j * kSelThreads) + i));
+                            if (key >= bound) f(key);
+                        }
+                    }
+                }
+        }, K, s, spill);
+    } else {
+        const uint32_t n = (uint32_t)K * (uint32_t)V;
+        const T *zb = z + (size_t)b * n;
         float v[kSelItems];
         const uint32_t e0 = (uint32_t)seg * kSegment + tid;
 #pragma unroll
@@ -174,6 +279,7 @@ beam_select(int K, int V, int nseg, const T *__restrict__ z, const float *__rest
             const uint32_t e = e0 + i * kSelThreads;
             v[i] = e < n ? to_f32(zb[e]) : -INFINITY;
         }
+        __syncthreads();
         u64 key[kSelItems];
 #pragma unroll
         for (int i = 0; i < kSelItems; ++i) {
@@ -187,7 +293,7 @@ beam_select(int K, int V, int nseg, const T *__restrict__ z, const float *__rest
                     key[i] = make_key(s.score[k], e);
             }
         }
-        block_topk<kSelItems>(key, K, s, list);
+        keys_topk<kSelItems>(key, K, s, spill);
     }
     if (nseg > 1) {  // the sentence's last CTA joins the segments
         if (tid < K) part[((size_t)b * nseg + seg) * K + tid] = s.best[tid];
@@ -210,7 +316,7 @@ beam_select(int K, int V, int nseg, const T *__restrict__ z, const float *__rest
                 key[i] = e < total ? __ldcg(mine + e) : 0;
             }
             key[kMergeItems - 1] = tid < K ? s.best[tid] : 0;  // the best so far
-            block_topk<kMergeItems>(key, K, s, list);
+            keys_topk<kMergeItems>(key, K, s, spill);
         }
     }
     if (tid < K) {
@@ -226,6 +332,23 @@ beam_select(int K, int V, int nseg, const T *__restrict__ z, const float *__rest
             token[o] = s.done[k] ? -1 : (int)(e - k * (uint32_t)V);
         }
     }
+}
+
+// Segments of a sentence: by rows where a row fills most of a CTA's threads, else across the rows
+// (8 x 83 candidates are one CTA's; by rows they would be eight, and their join).
+struct SelPlan {
+    bool rows;
+    int per_row, nseg;
+};
+template <typename T>
+SelPlan select_plan(int K, int V)
+{
+    SelPlan p;
+    p.rows = V >= kWideRow;
+    constexpr size_t E = RowVec<T>::E;
+    p.per_row = (int)ceil_div(((size_t)V + E - 1) / E + 1, kSegment / E);
+    p.nseg = p.rows ? K * p.per_row : (int)ceil_div((size_t)K * V, kSegment);
+    return p;
 }
 
 // ------------------------------------------------------------------ stacks
@@ -250,32 +373,53 @@ __device__ __forceinline__ int source_row(int n, int K, int S, const int32_t *pa
 }
 
 // Row n (blockIdx.x) of the new stacks: the slots 0 .. p of its source row, and its top. PH and
-// PC pieces (type Q) of h and c a slot; a CTA's threads take the pieces of its slots in order.
+// PC pieces (types QH, QC) of h and c a slot. A CTA takes kSlots slots, its threads their pieces in
+// order, four copies in flight each (a CTA a slot kept 75 of 256 threads busy at H = 200).
+constexpr int kSlots = 16;
 template <typename QH, typename QC>
 __global__ void __launch_bounds__(256)
 reorder_rows(int N, int K, int S, int PH, int PC, const int32_t *__restrict__ parent, const int32_t *__restrict__ p,
              const QH *__restrict__ h, const QC *__restrict__ c, int32_t *__restrict__ p_out, QH *__restrict__ h_out,
              QC *__restrict__ c_out, QH *__restrict__ top_h, QC *__restrict__ top_c, int32_t *err)
 {
-    const int n = blockIdx.x;
+    const int n = blockIdx.x, s0 = blockIdx.y * kSlots;
     int top;
     const int src = source_row(n, K, S, parent, p, &top, err);
-    const int per = PH + PC;
-    for (int s = blockIdx.y; s <= top; s += gridDim.y) {
-        const size_t from = (size_t)s * N + src, to = (size_t)s * N + n;
-        for (int i = threadIdx.x; i < per; i += blockDim.x) {
-            if (i < PH) {
-                const QH v = h[from * PH + i];
-                h_out[to * PH + i] = v;
-                if (s == top && top_h) top_h[(size_t)n * PH + i] = v;
+    if (blockIdx.y == 0 && threadIdx.x == 0) p_out[n] = top;
+    const int slots = min(kSlots, top + 1 - s0);
+    if (slots <= 0) return;
+    const int per = PH + PC, total = slots * per;
+    for (int i0 = threadIdx.x; i0 < total; i0 += 4 * 256) {
+        QH vh[4];
+        QC vc[4];
+        int slot[4], at[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int i = i0 + u * 256;
+            slot[u] = i / per;
+            at[u] = i - slot[u] * per;
+            if (i < total) {
+                const size_t from = (size_t)(s0 + slot[u]) * N + src;
+                if (at[u] < PH)
+                    vh[u] = h[from * PH + at[u]];
+                else
+                    vc[u] = c[from * PC + (at[u] - PH)];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (i0 + u * 256 >= total) break;
+            const int s = s0 + slot[u];
+            const size_t to = (size_t)s * N + n;
+            if (at[u] < PH) {
+                h_out[to * PH + at[u]] = vh[u];
+                if (s == top && top_h) top_h[(size_t)n * PH + at[u]] = vh[u];
             } else {
-                const QC v = c[from * PC + i - PH];
-                c_out[to * PC + i - PH] = v;
-                if (s == top && top_c) top_c[(size_t)n * PC + i - PH] = v;
+                c_out[to * PC + (at[u] - PH)] = vc[u];
+                if (s == top && top_c) top_c[(size_t)n * PC + (at[u] - PH)] = vc[u];
             }
         }
     }
-    if (blockIdx.y == 0 && threadIdx.x == 0) p_out[n] = top;
 }
 
 // Row n: the new state into slot p + 1 of a push, p moved by the op, the new top out.
@@ -336,18 +480,16 @@ sl_status stacklstm_beam_create(stacklstm_op_t *out, int B, int K, int V, int S,
     if (!out) return SL_ERR_ARG;
     *out = nullptr;
     if (B < 1 || K < 1 || V < 1 || S < 1 || H < 1 || (dtype != SL_FP32 && dtype != SL_BF16)) return SL_ERR_ARG;
-    if (K > kMaxBeams || B > 65535 || (long long)K * V > (1LL << 30) || H > (1 << 24)) return SL_ERR_UNSUPPORTED;
+    if (K > kMaxBeams || B > 65535 || (long long)K * V > (1LL << 30) || H > (1 << 24) || S > kSlots * 65535) return SL_ERR_UNSUPPORTED;
     sl_status st;
     stacklstm_op *op = op_new(SL_OP_BEAM, dtype, device, stream, &st);
     if (!op) return st;
     op->R = B * K; op->B = B; op->beams = K; op->V = V; op->S = S; op->H = H;
     OpDevice guard(device);
-    const size_t nseg = ceil_div((size_t)K * V, kSegment);
+    const size_t nseg = dtype == SL_BF16 ? select_plan<__nv_bfloat16>(K, V).nseg : select_plan<float>(K, V).nseg;
     cudaError_t e = op_workspace(op, 0, (size_t)B * nseg * K * 8);
     if (!e) e = op_workspace(op, 1, (size_t)B * 4);
     if (!e) e = cudaMemset(op->ws[1], 0, (size_t)B * 4);
-    if (!e) e = smem_at_least((const void *)beam_select<float>, (size_t)kMaxBeams * kSelItems * 8);
-    if (!e) e = smem_at_least((const void *)beam_select<__nv_bfloat16>, (size_t)kMaxBeams * kSelItems * 8);
     if (e) {
         stacklstm_op_destroy(op);
         return SL_ERR_OOM;
@@ -376,15 +518,19 @@ sl_status stacklstm_beam_select(stacklstm_op_t op, const void *logits, const flo
         return op_fail(op, SL_ERR_ARG, m);
     if (new_score == score) return op_fail(op, SL_ERR_ARG, "new_score must not be score: it is read by the whole sentence");
     OpDevice guard(op->device);
-    const int K = op->beams, V = op->V, nseg = (int)ceil_div((size_t)K * V, kSegment);
-    const dim3 grid(nseg, op->B);
-    const size_t smem = (size_t)K * kSelItems * 8;
-    if (op->dt == SL_BF16)
-        beam_select<<<grid, kSelThreads, smem, op->stream>>>(K, V, nseg, (const __nv_bfloat16 *)logits, lse, score, done,
-                                                             (u64 *)op->ws[0], (int *)op->ws[1], new_score, parent, token);
-    else
-        beam_select<<<grid, kSelThreads, smem, op->stream>>>(K, V, nseg, (const float *)logits, lse, score, done,
-                                                             (u64 *)op->ws[0], (int *)op->ws[1], new_score, parent, token);
+    const int K = op->beams, V = op->V;
+    const size_t smem = (size_t)K * kSelItems * 8;  // at most 16 KB
+    auto launch = [&](auto kernel, const SelPlan &p, auto *z) {
+        kernel<<<dim3(p.nseg, op->B), kSelThreads, smem, op->stream>>>(K, V, p.nseg, p.per_row, z, lse, score, done, (u64 *)op->ws[0],
+                                                                       (int *)op->ws[1], new_score, parent, token);
+    };
+    if (op->dt == SL_BF16) {
+        const SelPlan p = select_plan<__nv_bfloat16>(K, V);
+        launch(p.rows ? beam_select<__nv_bfloat16, true> : beam_select<__nv_bfloat16, false>, p, (const __nv_bfloat16 *)logits);
+    } else {
+        const SelPlan p = select_plan<float>(K, V);
+        launch(p.rows ? beam_select<float, true> : beam_select<float, false>, p, (const float *)logits);
+    }
     const cudaError_t e = cudaGetLastError();
     return e ? op_cuda(op, e, "stacklstm_beam_select") : SL_OK;
 }
@@ -401,7 +547,7 @@ sl_status stacklstm_beam_reorder(stacklstm_op_t op, const int32_t *parent, const
     OpDevice guard(op->device);
     const int N = op->R, K = op->beams, S = op->S, H = op->H;
     const bool bf = op->dt == SL_BF16;
-    const dim3 grid(N, std::min(S, 64));
+    const dim3 grid(N, ceil_div(S, kSlots));
     if (H % 8 == 0)
         reorder_rows<<<grid, 256, 0, op->stream>>>(N, K, S, H / (bf ? 8 : 4), H / 4, parent, p, (const uint4 *)h_stack,
                                                    (const uint4 *)c_stack, p_out, (uint4 *)h_out, (uint4 *)c_out,

@@ -29,19 +29,21 @@ struct DistillArgs {
     int32_t *err;
 };
 
-// NP pieces a thread in registers (0: read again in each pass); RPC rows a CTA.
+// NP pieces a thread in registers, as they lie in memory (0: read again in each pass); RPC rows a
+// CTA. With l_j = (t_j - max t) / tau, w_j = exp(l_j) and x_v = z_v - max z, four sums are joined
+// at once: sum_j w_j, sum_j w_j (l_j - x_{i_j} / tau), sum_v exp(x_v / tau), sum_v exp(x_v).
 template <typename T, int TPR, int NP>
-__global__ void __launch_bounds__(TPR == 32 ? 256 : TPR)
-distill_rows(const DistillArgs a)
+__global__ void __launch_bounds__(row_cta(TPR), row_ctas_per_sm(TPR))
+distill_rows(const __grid_constant__ DistillArgs a)
 {
     constexpr int E = RowVec<T>::E, RPC = TPR == 32 ? 8 : 1;
-    __shared__ float sm[kRowThreads / 32];
+    __shared__ float sm[4 * 32];
     extern __shared__ uint8_t dyn[];
     const int sub = TPR == 32 ? threadIdx.x / 32 : 0, t = threadIdx.x % TPR;
     const int r = blockIdx.x * RPC + sub;
     if (r >= a.rows) return;  // (TPR = 32: no barrier of the CTA below)
-    int *ci = (int *)dyn + (size_t)sub * (a.k + 1);                           // classes of the entries
-    float *cw = (float *)(dyn + (size_t)RPC * (a.k + 1) * 4) + (size_t)sub * (a.k + 1);  // their weights in the gradient
+    int *ci = (int *)dyn + (size_t)sub * (a.k + 1);                                      // classes of the entries
+    float *cw = (float *)(dyn + (size_t)RPC * (a.k + 1) * 4) + (size_t)sub * (a.k + 1);  // their logits, then weights
     auto sync = [] {
         if constexpr (TPR == 32)
             __syncwarp();
@@ -49,31 +51,37 @@ distill_rows(const DistillArgs a)
             __syncthreads();
     };
     const T *z = (const T *)a.z;
-    const RowVec<T> row(r, a.V, a.rows);
+    const RowVec<T> row(r, a.V);
+    const T *zr = z + row.first();
     const int n = row.pieces();
-    float v[NP > 0 ? NP : 1][E];
-    float m = -INFINITY;
+    uint4 q[NP > 0 ? NP : 1];
     if constexpr (NP > 0) {
 #pragma unroll
         for (int j = 0; j < NP; ++j)
-            if (j * TPR + t < n) row.load(z, j * TPR + t, v[j]);
-#pragma unroll
-        for (int j = 0; j < NP; ++j)
-            if (j * TPR + t < n)
-#pragma unroll
-                for (int i = 0; i < E; ++i) m = max_nan(m, v[j][i]);
-    } else {
-        for (int p = t; p < n; p += TPR) {
-            row.load(z, p, v[0]);
-#pragma unroll
-            for (int i = 0; i < E; ++i) m = max_nan(m, v[0][i]);
-        }
+            if (j * TPR + t < n) q[j] = row.load(z, j * TPR + t);
     }
-    // the teacher, by the row's first warp (each warp when it is the row)
-    float tmax = -INFINITY, tsum = 0.0f;
+    // f(piece, its elements) over this thread's pieces
+    auto each = [&](auto f) {
+        if constexpr (NP > 0) {
+#pragma unroll
+            for (int j = 0; j < NP; ++j)
+                if (j * TPR + t < n) {
+                    float v[E];
+                    unpack<T>(q[j], v);
+                    f(j * TPR + t, v);
+                }
+        } else {
+            for (int p = t; p < n; p += TPR) {
+                float v[E];
+                unpack<T>(row.load(z, p), v);
+                f(p, v);
+            }
+        }
+    };
+    float top[2] = {-INFINITY, -INFINITY};  // of z, of the teacher's logits
     for (int j = t; j < a.k; j += TPR) {
         int c = a.t_idx[(size_t)r * a.k + j];
-        float l = a.t_logit[(size_t)r * a.k + j];
+        const float l = a.t_logit[(size_t)r * a.k + j];
         if (c < -1 || c >= a.V) {
             atomicCAS(a.err, 0, (int)SL_ERR_ARG);  // the entry is skipped
             c = -1;
@@ -81,95 +89,89 @@ distill_rows(const DistillArgs a)
         if (l == -INFINITY) c = -1;
         ci[j] = c;
         cw[j] = l;
+        if (c >= 0) top[1] = max_nan(top[1], l);
     }
-    sync();
-    for (int j = (int)(threadIdx.x & 31); j < a.k; j += 32)
-        if (ci[j] >= 0) tmax = fmaxf(tmax, cw[j]);
-    tmax = warp_max(tmax);
-    for (int j = (int)(threadIdx.x & 31); j < a.k; j += 32)
-        if (ci[j] >= 0) tsum += expf((cw[j] - tmax) / a.tau);
-    tsum = warp_sum(tsum);
     int gold = a.gold ? a.gold[r] : -1;
     if (gold < -1 || gold >= a.V) {
         if (t == 0) atomicCAS(a.err, 0, (int)SL_ERR_ARG);
         gold = -1;
     }
-    m = row_max<TPR>(m, sm);
+    each([&](int, const float (&v)[E]) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) top[0] = max_nan(top[0], v[i]);
+    });
+    row_join<true, TPR>(top, sm);
+    const float m = top[0], rtau = 1.0f / a.tau;
     const bool some = m > -INFINITY || isnan(m);
-    // (a teacher whose logits are all -inf, or absent, has tsum = 0)
-    const bool soft = some && a.alpha > 0.0f && tsum != 0.0f, hard = some && a.alpha < 1.0f && gold >= 0;
+    const bool taught = top[1] > -INFINITY || isnan(top[1]);
+    const bool soft = some && taught && a.alpha > 0.0f, hard = some && a.alpha < 1.0f && gold >= 0;
     const float k2 = kLog2e / a.tau;
-    float st = 0.0f, s1 = 0.0f;
-    auto add = [&](const float (&w)[E]) {
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-            const float d = w[i] - m;
-            if (soft) st += exp2_hw(d * k2);
-            if (hard) s1 += exp2_hw(d * kLog2e);
-        }
-    };
-    if (soft || hard) {
-        if constexpr (NP > 0) {
-#pragma unroll
-            for (int j = 0; j < NP; ++j)
-                if (j * TPR + t < n) add(v[j]);
-        } else {
-            for (int p = t; p < n; p += TPR) {
-                row.load(z, p, v[0]);
-                add(v[0]);
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (soft)
+        for (int j = t; j < a.k; j += TPR)
+            if (ci[j] >= 0) {
+                const float l = (cw[j] - top[1]) * rtau, w = expf(l);
+                s[0] += w;
+                if (w > 0.0f) s[1] += w * (l - (to_f32(zr[ci[j]]) - m) * rtau);  // (0 on a class of -inf is 0)
+                else if (isnan(w)) s[1] = w;
             }
-        }
+    if (soft && hard)
+        each([&](int, const float (&v)[E]) {
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const float d = v[i] - m;
+                s[2] += exp2_hw(d * k2);
+                s[3] += exp2_hw(d * kLog2e);
+            }
+        });
+    else if (soft || hard) {
+        const float kk = soft ? k2 : kLog2e;
+        float one = 0.0f;
+        each([&](int, const float (&v)[E]) {
+#pragma unroll
+            for (int i = 0; i < E; ++i) one += exp2_hw((v[i] - m) * kk);
+        });
+        s[soft ? 2 : 3] = one;
     }
-    st = row_sum<TPR>(st, sm);
-    s1 = row_sum<TPR>(s1, sm);
-    const float lse_t = logf(st), lse_1 = logf(s1);  // of (z - m) / tau and z - m
+    row_join<false, TPR>(s, sm);
     const float ct = soft ? a.scale * a.alpha * a.tau : 0.0f, c1 = hard ? a.scale * (1.0f - a.alpha) : 0.0f;
-    const float wt = soft ? ct / st : 0.0f, w1 = hard ? c1 / s1 : 0.0f;
-    auto grad = [&](float zv) {
-        const float d = zv - m;
-        float g = 0.0f;
-        if (soft) g = wt * exp2_hw(d * k2);
-        if (hard) g = fmaf(w1, exp2_hw(d * kLog2e), g);
-        return g;
-    };
-    if (a.dz) {
-        auto put = [&](int p, const float (&w)[E]) {
+    const float wt = soft ? ct / s[2] : 0.0f, w1 = hard ? c1 / s[3] : 0.0f;
+    if (t == 0 && a.loss) {
+        float loss = 0.0f;
+        if (soft) loss = a.alpha * a.tau * a.tau * (s[1] / s[0] - logf(s[0]) + logf(s[2]));
+        if (hard) loss += (1.0f - a.alpha) * (logf(s[3]) - (to_f32(zr[gold]) - m));
+        a.loss[r] = a.scale * loss;
+    }
+    if (!a.dz) return;
+    if (soft && hard)
+        each([&](int p, const float (&v)[E]) {
             float g[E];
 #pragma unroll
-            for (int i = 0; i < E; ++i) g[i] = grad(w[i]);
+            for (int i = 0; i < E; ++i) {
+                const float d = v[i] - m;
+                g[i] = fmaf(w1, exp2_hw(d * kLog2e), wt * exp2_hw(d * k2));
+            }
             row.store_f32(a.dz, p, g);
-        };
-        if constexpr (NP > 0) {
+        });
+    else {
+        const float kk = soft ? k2 : kLog2e, w = soft ? wt : w1;
+        const bool any = soft || hard;
+        each([&](int p, const float (&v)[E]) {
+            float g[E];
 #pragma unroll
-            for (int j = 0; j < NP; ++j)
-                if (j * TPR + t < n) put(j * TPR + t, v[j]);
-        } else {
-            for (int p = t; p < n; p += TPR) {
-                row.load(z, p, v[0]);
-                put(p, v[0]);
-            }
-        }
+            for (int i = 0; i < E; ++i) g[i] = any ? w * exp2_hw((v[i] - m) * kk) : 0.0f;
+            row.store_f32(a.dz, p, g);
+        });
     }
-    // the loss, and the entries' weights; entry k is the gold class
-    float loss = 0.0f;
-    if (soft)
-        for (int j = (int)(threadIdx.x & 31); j < a.k; j += 32)
-            if (ci[j] >= 0) {
-                const float l = (cw[j] - tmax) / a.tau, q = expf(l) / tsum;
-                if (q > 0.0f) loss += q * ((l - logf(tsum)) - ((to_f32(z[row.first + ci[j]]) - m) / a.tau - lse_t));
-            }
-    loss = warp_sum(loss) * a.alpha * a.tau * a.tau;
-    if (hard) loss += (1.0f - a.alpha) * (lse_1 - (to_f32(z[row.first + gold]) - m));
-    if (t == 0 && a.loss) a.loss[r] = a.scale * loss;
-    if (!a.dz) return;
     sync();
+    // the entries' weights in the gradient; entry k is the gold class
     for (int j = t; j <= a.k; j += TPR) {
         if (j == a.k) {
             ci[j] = hard ? gold : -1;
             cw[j] = c1;
         } else if (ci[j] >= 0) {
             if (soft)
-                cw[j] = ct * (expf((cw[j] - tmax) / a.tau) / tsum);
+                cw[j] = ct * (expf((cw[j] - top[1]) * rtau) / s[0]);
             else
                 ci[j] = -1;
         }
@@ -184,7 +186,11 @@ distill_rows(const DistillArgs a)
         float w = 0.0f;
         for (int i = j; i <= a.k; ++i)
             if (ci[i] == c) w += cw[i];
-        a.dz[row.first + c] = grad(to_f32(z[row.first + c])) - w;
+        const float d = to_f32(zr[c]) - m;
+        float g = 0.0f;
+        if (soft) g = wt * exp2_hw(d * k2);
+        if (hard) g = fmaf(w1, exp2_hw(d * kLog2e), g);
+        a.dz[row.first() + c] = g - w;
     }
 }
 
@@ -197,10 +203,8 @@ cudaError_t launch_distill(const DistillArgs &a, cudaStream_t st)
     const unsigned grid = ceil_div(a.rows, rpc);
     const size_t smem = (size_t)rpc * (a.k + 1) * 8;
 #define SL_DIST(t, n) \
-    if (tpr == t && np == n) distill_rows<T, t, n><<<grid, t == 32 ? 256 : t, smem, st>>>(a);
-    SL_DIST(32, 1) SL_DIST(32, 2) SL_DIST(32, 4)
-    SL_DIST(kRowThreads, 0) SL_DIST(kRowThreads, 1) SL_DIST(kRowThreads, 2) SL_DIST(kRowThreads, 4)
-    SL_DIST(kRowThreads, 8) SL_DIST(kRowThreads, 16)
+    if (tpr == t && np == n) distill_rows<T, t, n><<<grid, row_cta(t), smem, st>>>(a);
+    SL_ROW_PLANS(SL_DIST)
 #undef SL_DIST
     return cudaGetLastError();
 }

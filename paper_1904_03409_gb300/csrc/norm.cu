@@ -6,53 +6,99 @@
 //   dx = s (a - mean(a) - xh mean(a xh)),  dgamma = sum_r dy xh,  dbeta = sum_r dy.
 // Both are bound by HBM: each tensor is read or written once. A row's elements stay in the
 // registers of its threads (a warp, or a CTA of 256), so the variance is taken of the centred
-// values and nothing is read twice; only rows wider than the registers hold (norm_*_wide) are
-// read again, from the caches. The backward's CTAs keep their columns' sums of dgamma and dbeta
+// values and nothing is read twice, and the next row's are read while one is worked on; only rows
+// wider than the registers hold (norm_*_wide) are read again, from the caches. The backward's CTAs keep their columns' sums of dgamma and dbeta
 // in registers over all their rows and write them once; a second launch adds the CTAs' sums in
 // CTA order, so the gradients are bitwise reproducible. (Products that a sum follows are rounded
 // by __fmul_rn where a null output would otherwise let the compiler fuse the two, and change bits.)
-#include "op.cuh"
+#include "rowvec.cuh"
 
 namespace sl {
 namespace {
 
-constexpr int kNormThreads = 256;
+// A row's TPR threads (a warp: CTAs of four rows, or a CTA of 256) hold CH pieces of VEC elements
+// each: piece j of thread t is at column (j TPR + t) VEC. VEC = 16 bytes of the type where every
+// row starts on 16 bytes, else 1.
+constexpr int kWideThreads = 256;
+__host__ __device__ constexpr int norm_threads(int tpr) { return tpr == 32 ? 128 : 256; }
+// CTAs an SM: as many as their registers allow (the next row's pieces, and in the backward the
+// column sums, stay in them), and no more than leave the parts few
+__host__ __device__ constexpr int norm_ctas(int tpr, int elems, bool bwd)
+{
+    return tpr == 32 ? (elems <= 8 ? 8 : elems <= 16 ? (bwd ? 5 : 8) : bwd ? 3 : 6)
+                     : (elems <= 8 ? 4 : elems <= 16 ? (bwd ? 2 : 4) : bwd ? 1 : 3);
+}
 
-// The TPR threads of a row hold CH pieces of VEC elements each: piece j of thread t is at column
-// (j TPR + t) VEC.
+// A piece as it lies in memory.
+template <typename T, int VEC>
+struct Piece {
+    uint4 q[VEC * sizeof(T) / 16];
+    __device__ __forceinline__ void load(const T *p)
+    {
+#pragma unroll
+        for (int i = 0; i < (int)(VEC * sizeof(T) / 16); ++i) q[i] = ((const uint4 *)p)[i];
+    }
+    __device__ __forceinline__ void get(float (&v)[VEC]) const
+    {
+        constexpr int E = 16 / sizeof(T);
+#pragma unroll
+        for (int i = 0; i < VEC / E; ++i) {
+            float w[E];
+            unpack<T>(q[i], w);
+#pragma unroll
+            for (int k = 0; k < E; ++k) v[i * E + k] = w[k];
+        }
+    }
+};
+template <typename T>
+struct Piece<T, 1> {
+    T e;
+    __device__ __forceinline__ void load(const T *p) { e = *p; }
+    __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = to_f32(e); }
+};
+
 template <typename T, int VEC, int CH, int TPR>
-__global__ void __launch_bounds__(kNormThreads)
+__global__ void __launch_bounds__(norm_threads(TPR), norm_ctas(TPR, CH * VEC, false))
 norm_fwd(int rows, int N, const T *__restrict__ x, const float *__restrict__ gamma, const float *__restrict__ beta,
          float eps, T *__restrict__ y, float *__restrict__ mean, float *__restrict__ rstd)
 {
-    constexpr int RPB = kNormThreads / TPR;
-    __shared__ float sm[kNormThreads / 32];
-    const int t = threadIdx.x % TPR;
+    constexpr int RPB = norm_threads(TPR) / TPR;
+    __shared__ float sm[32];
+    const int t = threadIdx.x % TPR, step = gridDim.x * RPB;
     const float inv = 1.0f / (float)N;
-    for (int r = blockIdx.x * RPB + threadIdx.x / TPR; r < rows; r += gridDim.x * RPB) {
+    int r = blockIdx.x * RPB + threadIdx.x / TPR;
+    Piece<T, VEC> next[CH];
+    auto fetch = [&](int row) {
+        if (row < rows)
+#pragma unroll
+            for (int j = 0; j < CH; ++j)
+                if ((j * TPR + t) * VEC < N) next[j].load(x + (size_t)row * N + (j * TPR + t) * VEC);
+    };
+    fetch(r);
+    for (; r < rows; r += step) {
         const size_t at = (size_t)r * N;
         float v[CH][VEC];
-        float sum = 0.0f;
+        float sum[1] = {0.0f}, sq[1] = {0.0f};
 #pragma unroll
-        for (int j = 0; j < CH; ++j) {
-            const int c = (j * TPR + t) * VEC;
-            if (c < N) {
-                load_vec<T, VEC>(x + at + c, v[j]);
+        for (int j = 0; j < CH; ++j)
+            if ((j * TPR + t) * VEC < N) {
+                next[j].get(v[j]);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) sum += v[j][i];
+                for (int i = 0; i < VEC; ++i) sum[0] += v[j][i];
             }
-        }
-        const float m = __fmul_rn(row_sum<TPR>(sum, sm), inv);
-        float sq = 0.0f;
+        fetch(r + step);  // on its way while this row is worked on
+        row_join<false, TPR>(sum, sm);
+        const float m = __fmul_rn(sum[0], inv);
 #pragma unroll
         for (int j = 0; j < CH; ++j)
             if ((j * TPR + t) * VEC < N)
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
                     v[j][i] -= m;
-                    sq = fmaf(v[j][i], v[j][i], sq);
+                    sq[0] = fmaf(v[j][i], v[j][i], sq[0]);
                 }
-        const float s = 1.0f / sqrtf(row_sum<TPR>(sq, sm) * inv + eps);
+        row_join<false, TPR>(sq, sm);
+        const float s = 1.0f / sqrtf(sq[0] * inv + eps);
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
             const int c = (j * TPR + t) * VEC;
@@ -79,24 +125,24 @@ norm_fwd(int rows, int N, const T *__restrict__ x, const float *__restrict__ gam
 
 // Rows of any width: a CTA a row, three passes over it (the last two from the caches).
 template <typename T>
-__global__ void __launch_bounds__(kNormThreads)
+__global__ void __launch_bounds__(kWideThreads)
 norm_fwd_wide(int rows, int N, const T *__restrict__ x, const float *__restrict__ gamma,
               const float *__restrict__ beta, float eps, T *__restrict__ y, float *__restrict__ mean,
               float *__restrict__ rstd)
 {
-    __shared__ float sm[kNormThreads / 32];
+    __shared__ float sm[kWideThreads / 32];
     const float inv = 1.0f / (float)N;
     for (int r = blockIdx.x; r < rows; r += gridDim.x) {
         const T *xr = x + (size_t)r * N;
         float sum = 0.0f, sq = 0.0f;
-        for (int c = threadIdx.x; c < N; c += kNormThreads) sum += to_f32(xr[c]);
-        const float m = __fmul_rn(row_sum<kNormThreads>(sum, sm), inv);
-        for (int c = threadIdx.x; c < N; c += kNormThreads) {
+        for (int c = threadIdx.x; c < N; c += kWideThreads) sum += to_f32(xr[c]);
+        const float m = __fmul_rn(row_sum<kWideThreads>(sum, sm), inv);
+        for (int c = threadIdx.x; c < N; c += kWideThreads) {
             const float d = to_f32(xr[c]) - m;
             sq = fmaf(d, d, sq);
         }
-        const float s = 1.0f / sqrtf(row_sum<kNormThreads>(sq, sm) * inv + eps);
-        for (int c = threadIdx.x; c < N; c += kNormThreads)
+        const float s = 1.0f / sqrtf(row_sum<kWideThreads>(sq, sm) * inv + eps);
+        for (int c = threadIdx.x; c < N; c += kWideThreads)
             y[(size_t)r * N + c] = from_f32<T>(fmaf((to_f32(xr[c]) - m) * s, gamma ? gamma[c] : 1.0f, beta ? beta[c] : 0.0f));
         if (threadIdx.x == 0) {
             if (mean) mean[r] = m;
@@ -107,33 +153,52 @@ norm_fwd_wide(int rows, int N, const T *__restrict__ x, const float *__restrict_
 
 // part [gridDim.x][2][N]: this CTA's sums of dy xh and dy over its rows.
 template <typename T, int VEC, int CH, int TPR>
-__global__ void __launch_bounds__(kNormThreads)
+__global__ void __launch_bounds__(norm_threads(TPR), norm_ctas(TPR, CH * VEC, true))
 norm_bwd(int rows, int N, const float *__restrict__ dy, const T *__restrict__ x, const float *__restrict__ gamma,
          const float *__restrict__ mean, const float *__restrict__ rstd, float *__restrict__ dx,
          float *__restrict__ part)
 {
-    constexpr int RPB = kNormThreads / TPR;
-    __shared__ float sm[kNormThreads / 32];
+    constexpr int RPB = norm_threads(TPR) / TPR;
+    __shared__ float sm[2 * 32];
     extern __shared__ float cols[];  // [RPB][N] when RPB > 1: the warps' column sums
-    const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+    const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR, step = gridDim.x * RPB;
     const float inv = 1.0f / (float)N;
     float dg[CH][VEC], db[CH][VEC];
 #pragma unroll
     for (int j = 0; j < CH; ++j)
 #pragma unroll
         for (int i = 0; i < VEC; ++i) dg[j][i] = db[j][i] = 0.0f;
-    for (int r = blockIdx.x * RPB + sub; r < rows; r += gridDim.x * RPB) {
+    Piece<float, VEC> nd[CH];
+    Piece<T, VEC> nx[CH];
+    float nm = 0.0f, ns = 0.0f;
+    auto fetch = [&](int row) {
+        if (row < rows) {
+            nm = mean[row];
+            ns = rstd[row];
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                const size_t o = (size_t)row * N + (j * TPR + t) * VEC;
+                if ((j * TPR + t) * VEC < N) {
+                    nd[j].load(dy + o);
+                    nx[j].load(x + o);
+                }
+            }
+        }
+    };
+    int r = blockIdx.x * RPB + sub;
+    fetch(r);
+    for (; r < rows; r += step) {
         const size_t at = (size_t)r * N;
-        const float m = mean[r], s = rstd[r];
+        const float m = nm, s = ns;
         float a[CH][VEC], xh[CH][VEC];
-        float sa = 0.0f, sx = 0.0f;
+        float sums[2] = {0.0f, 0.0f};  // of a and of a xh
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
             const int c = (j * TPR + t) * VEC;
             if (c < N) {
                 float g[VEC];
-                load_vec<float, VEC>(dy + at + c, a[j]);
-                load_vec<T, VEC>(x + at + c, xh[j]);
+                nd[j].get(a[j]);
+                nx[j].get(xh[j]);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) g[i] = 1.0f;
                 if (gamma) load_vec<float, VEC>(gamma + c, g);
@@ -143,13 +208,15 @@ norm_bwd(int rows, int N, const float *__restrict__ dy, const T *__restrict__ x,
                     dg[j][i] = fmaf(a[j][i], xh[j][i], dg[j][i]);
                     db[j][i] += a[j][i];
                     a[j][i] = __fmul_rn(a[j][i], g[i]);
-                    sa += a[j][i];
-                    sx = fmaf(a[j][i], xh[j][i], sx);
+                    sums[0] += a[j][i];
+                    sums[1] = fmaf(a[j][i], xh[j][i], sums[1]);
                 }
             }
         }
+        fetch(r + step);  // on its way while this row is worked on
         if (dx) {
-            const float ma = __fmul_rn(row_sum<TPR>(sa, sm), inv), mx = __fmul_rn(row_sum<TPR>(sx, sm), inv);
+            row_join<false, TPR>(sums, sm);
+            const float ma = __fmul_rn(sums[0], inv), mx = __fmul_rn(sums[1], inv);
 #pragma unroll
             for (int j = 0; j < CH; ++j) {
                 const int c = (j * TPR + t) * VEC;
@@ -169,19 +236,14 @@ norm_bwd(int rows, int N, const float *__restrict__ dy, const T *__restrict__ x,
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
             const int c = (j * TPR + t) * VEC;
-            if (c < N)
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    const float v = which ? db[j][i] : dg[j][i];
-                    if constexpr (RPB > 1)
-                        cols[(size_t)sub * N + c + i] = v;
-                    else
-                        out[(size_t)which * N + c + i] = v;
-                }
+            if (c < N) {
+                float *to = RPB > 1 ? cols + (size_t)sub * N + c : out + (size_t)which * N + c;
+                store_vec<float, VEC>(to, which ? db[j] : dg[j]);
+            }
         }
         if constexpr (RPB > 1) {
             __syncthreads();
-            for (int c = threadIdx.x; c < N; c += kNormThreads) {
+            for (int c = threadIdx.x; c < N; c += norm_threads(TPR)) {
                 float acc = 0.0f;
 #pragma unroll
                 for (int w = 0; w < RPB; ++w) acc += cols[(size_t)w * N + c];
@@ -192,29 +254,29 @@ norm_bwd(int rows, int N, const float *__restrict__ dy, const T *__restrict__ x,
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kNormThreads)
+__global__ void __launch_bounds__(kWideThreads)
 norm_bwd_wide(int rows, int N, const float *__restrict__ dy, const T *__restrict__ x, const float *__restrict__ gamma,
               const float *__restrict__ mean, const float *__restrict__ rstd, float *__restrict__ dx,
               float *__restrict__ part)
 {
-    __shared__ float sm[kNormThreads / 32];
+    __shared__ float sm[kWideThreads / 32];
     const float inv = 1.0f / (float)N;
     float *out = part ? part + (size_t)blockIdx.x * 2 * N : nullptr;
     if (out)
-        for (int c = threadIdx.x; c < 2 * N; c += kNormThreads) out[c] = 0.0f;
+        for (int c = threadIdx.x; c < 2 * N; c += kWideThreads) out[c] = 0.0f;
     __syncthreads();
     for (int r = blockIdx.x; r < rows; r += gridDim.x) {
         const float *dr = dy + (size_t)r * N;
         const T *xr = x + (size_t)r * N;
         const float m = mean[r], s = rstd[r];
         float sa = 0.0f, sx = 0.0f;
-        for (int c = threadIdx.x; c < N; c += kNormThreads) {
+        for (int c = threadIdx.x; c < N; c += kWideThreads) {
             const float a = dr[c] * (gamma ? gamma[c] : 1.0f);
             sa += a;
             sx = fmaf(a, (to_f32(xr[c]) - m) * s, sx);
         }
-        const float ma = row_sum<kNormThreads>(sa, sm) * inv, mx = row_sum<kNormThreads>(sx, sm) * inv;
-        for (int c = threadIdx.x; c < N; c += kNormThreads) {
+        const float ma = row_sum<kWideThreads>(sa, sm) * inv, mx = row_sum<kWideThreads>(sx, sm) * inv;
+        for (int c = threadIdx.x; c < N; c += kWideThreads) {
             const float d = dr[c], xh = (to_f32(xr[c]) - m) * s;
             if (dx) dx[(size_t)r * N + c] = s * (d * (gamma ? gamma[c] : 1.0f) - ma - xh * mx);
             if (out) {  // a thread owns its columns: no other thread of the CTA touches them
@@ -226,42 +288,50 @@ norm_bwd_wide(int rows, int N, const float *__restrict__ dy, const T *__restrict
     }
 }
 
-// dgamma, dbeta = the parts' sums in part order: warp w of a CTA adds parts w, w + 8, ... of 32
-// columns, then the eight sums are added in order.
-__global__ void __launch_bounds__(256)
+// dgamma, dbeta = the parts' sums in a fixed order: warp w of a CTA adds parts w, w + 32, ... of 32
+// columns, then the 32 sums are added in order. (Eight warps: 10 us for 608 parts of 400 columns.)
+__global__ void __launch_bounds__(1024)
 norm_reduce(const float *__restrict__ part, int n, int N, float *__restrict__ dgamma, float *__restrict__ dbeta)
 {
-    __shared__ float sm[8][32];
+    __shared__ float sm[32][33];
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     const size_t c = blockIdx.x * (size_t)32 + lane, W = 2 * (size_t)N;
     float acc = 0.0f;
     if (c < W) {
-#pragma unroll 8
-        for (int s = w; s < n; s += 8) acc += part[(size_t)s * W + c];
+#pragma unroll 10
+        for (int s = w; s < n; s += 32) acc += part[(size_t)s * W + c];
     }
     sm[w][lane] = acc;
     __syncthreads();
-    if (w == 0 && c < W) {
-        float v = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v += sm[i][lane];
-        if (c < (size_t)N) {
-            if (dgamma) dgamma[c] = v;
+    acc = warp_sum(sm[lane][w]);  // column w of the 32: a butterfly over the warps' sums
+    const size_t cc = blockIdx.x * (size_t)32 + w;
+    if (lane == 0 && cc < W) {
+        if (cc < (size_t)N) {
+            if (dgamma) dgamma[cc] = acc;
         } else if (dbeta) {
-            dbeta[c - N] = v;
+            dbeta[cc - N] = acc;
         }
     }
 }
 
-// Pieces a thread holds for a row of N elements over TPR threads (0: more than 4).
-int pieces(int N, int vec, int tpr)
+// How a call runs: elements of a piece, pieces a thread (0: the wide kernels), threads a row, CTAs.
+struct NormPlan {
+    int vec, ch, tpr, grid;
+};
+NormPlan norm_plan(const stacklstm_op *op, int rows, bool bwd)
 {
-    const int n = (int)ceil_div((size_t)N, (size_t)vec * tpr);
-    return n <= 1 ? 1 : n <= 2 ? 2 : n <= 4 ? 4 : 0;
+    const int vmax = op->dt == SL_BF16 ? 8 : 4, N = op->N;
+    NormPlan p;
+    p.vec = N % vmax == 0 ? vmax : 1;
+    const int most = p.vec == 1 ? 16 : 4;
+    p.tpr = ceil_div(N, p.vec * 32) <= (unsigned)most ? 32 : 256;
+    const int n = (int)ceil_div(N, p.vec * p.tpr);
+    p.ch = p.vec == 1 ? (n <= 4 ? 4 : n <= 16 ? 16 : 0) : n <= 1 ? 1 : n <= 2 ? 2 : n <= 4 ? 4 : 0;
+    const int per_sm = p.ch ? std::min(norm_ctas(p.tpr, p.ch * p.vec, bwd), bwd ? 4 : 8) : 4;
+    const int rpb = p.ch ? norm_threads(p.tpr) / p.tpr : 1;
+    p.grid = (int)std::min<size_t>(ceil_div((size_t)rows, (size_t)rpb), (size_t)op->num_sms * per_sm);
+    return p;
 }
-
-template <typename T>
-constexpr int kVec = 16 / (int)sizeof(T);
 
 struct NormCall {
     stacklstm_op *op;
@@ -274,58 +344,37 @@ struct NormCall {
     // backward
     const float *dy;
     float *dx, *part;
-    int grid;
 };
 
 template <typename T, int VEC, int CH, int TPR>
-cudaError_t launch_norm(const NormCall &c)
+void launch_norm(const NormCall &c, int grid)
 {
-    constexpr int RPB = kNormThreads / TPR;
+    constexpr int NT = norm_threads(TPR), RPB = NT / TPR;
     const int N = c.op->N;
-    if (!c.dy) {
-        norm_fwd<T, VEC, CH, TPR><<<c.grid, kNormThreads, 0, c.op->stream>>>(c.rows, N, (const T *)c.x, c.gamma, c.beta,
-                                                                             c.eps, (T *)c.y, c.mean, c.rstd);
-    } else {
-        const size_t smem = RPB > 1 ? (size_t)RPB * N * 4 : 0;
-        norm_bwd<T, VEC, CH, TPR><<<c.grid, kNormThreads, smem, c.op->stream>>>(
+    if (!c.dy)
+        norm_fwd<T, VEC, CH, TPR><<<grid, NT, 0, c.op->stream>>>(c.rows, N, (const T *)c.x, c.gamma, c.beta, c.eps, (T *)c.y,
+                                                                 c.mean, c.rstd);
+    else  // (RPB > 1: N <= 1024, 16 KB)
+        norm_bwd<T, VEC, CH, TPR><<<grid, NT, RPB > 1 ? (size_t)RPB * N * 4 : 0, c.op->stream>>>(
             c.rows, N, c.dy, (const T *)c.x, c.gamma, c.mean, c.rstd, c.dx, c.part);
-    }
-    return cudaGetLastError();
 }
 
 template <typename T>
-cudaError_t dispatch_norm(const NormCall &c, int vec, int ch, int tpr)
+cudaError_t run_norm(const NormCall &c, const NormPlan &p)
 {
-    constexpr int V = kVec<T>;
+    constexpr int V = 16 / (int)sizeof(T);
 #define SL_NORM(v, n, t) \
-    if (vec == v && ch == n && tpr == t) return launch_norm<T, v, n, t>(c);
+    if (p.vec == v && p.ch == n && p.tpr == t) launch_norm<T, v, n, t>(c, p.grid);
     SL_NORM(V, 1, 32) SL_NORM(V, 2, 32) SL_NORM(V, 4, 32) SL_NORM(V, 1, 256) SL_NORM(V, 2, 256) SL_NORM(V, 4, 256)
-    SL_NORM(1, 1, 32) SL_NORM(1, 2, 32) SL_NORM(1, 4, 32) SL_NORM(1, 1, 256) SL_NORM(1, 2, 256) SL_NORM(1, 4, 256)
+    SL_NORM(1, 4, 32) SL_NORM(1, 16, 32) SL_NORM(1, 4, 256) SL_NORM(1, 16, 256)
 #undef SL_NORM
-    if (!c.dy)
-        norm_fwd_wide<T><<<c.grid, kNormThreads, 0, c.op->stream>>>(c.rows, c.op->N, (const T *)c.x, c.gamma, c.beta, c.eps,
+    if (!p.ch && !c.dy)
+        norm_fwd_wide<T><<<p.grid, kWideThreads, 0, c.op->stream>>>(c.rows, c.op->N, (const T *)c.x, c.gamma, c.beta, c.eps,
                                                                     (T *)c.y, c.mean, c.rstd);
-    else
-        norm_bwd_wide<T><<<c.grid, kNormThreads, 0, c.op->stream>>>(c.rows, c.op->N, c.dy, (const T *)c.x, c.gamma,
+    if (!p.ch && c.dy)
+        norm_bwd_wide<T><<<p.grid, kWideThreads, 0, c.op->stream>>>(c.rows, c.op->N, c.dy, (const T *)c.x, c.gamma,
                                                                     c.mean, c.rstd, c.dx, c.part);
     return cudaGetLastError();
-}
-
-// Pieces of 16 bytes where every row starts on 16 bytes of all its tensors, else single
-// elements; a warp a row where four pieces a lane hold it, else a CTA.
-cudaError_t run_norm(NormCall c)
-{
-    const stacklstm_op *op = c.op;
-    const int vmax = op->dt == SL_BF16 ? 8 : 4;
-    const int vec = op->N % vmax == 0 ? vmax : 1;
-    int tpr = 32, ch = pieces(op->N, vec, 32);
-    if (!ch) {
-        tpr = 256;
-        ch = pieces(op->N, vec, 256);
-    }
-    const int rpb = kNormThreads / tpr;
-    c.grid = (int)std::min<size_t>(ceil_div((size_t)c.rows, (size_t)rpb), (size_t)op->num_sms * 4);
-    return op->dt == SL_BF16 ? dispatch_norm<__nv_bfloat16>(c, vec, ch, tpr) : dispatch_norm<float>(c, vec, ch, tpr);
 }
 
 }  // namespace
@@ -369,7 +418,8 @@ sl_status stacklstm_norm_forward(stacklstm_op_t op, int rows, const void *x, con
     OpDevice guard(op->device);
     NormCall c = {};
     c.op = op; c.rows = rows; c.x = x; c.gamma = gamma; c.beta = beta; c.eps = eps; c.y = y; c.mean = mean; c.rstd = rstd;
-    const cudaError_t e = run_norm(c);
+    const NormPlan p = norm_plan(op, rows, false);
+    const cudaError_t e = op->dt == SL_BF16 ? run_norm<__nv_bfloat16>(c, p) : run_norm<float>(c, p);
     return e ? op_cuda(op, e, "stacklstm_norm_forward") : SL_OK;
 }
 
@@ -393,12 +443,10 @@ sl_status stacklstm_norm_backward(stacklstm_op_t op, int rows, const float *dy, 
     c.rstd = const_cast<float *>(rstd); c.dy = dy; c.dx = dx;
     const bool sums = dgamma || dbeta;
     c.part = sums ? (float *)op->ws[0] : nullptr;
-    e = run_norm(c);
+    const NormPlan p = norm_plan(op, rows, true);
+    e = op->dt == SL_BF16 ? run_norm<__nv_bfloat16>(c, p) : run_norm<float>(c, p);
     if (!e && sums) {
-        const int vmax = op->dt == SL_BF16 ? 8 : 4, vec = op->N % vmax == 0 ? vmax : 1;
-        const int rpb = pieces(op->N, vec, 32) ? kNormThreads / 32 : 1;
-        const int n = (int)std::min<size_t>(ceil_div((size_t)rows, (size_t)rpb), (size_t)op->num_sms * 4);
-        norm_reduce<<<ceil_div(2 * (size_t)op->N, 32), 256, 0, op->stream>>>((const float *)op->ws[0], n, op->N, dgamma, dbeta);
+        norm_reduce<<<ceil_div(2 * (size_t)op->N, 32), 1024, 0, op->stream>>>((const float *)op->ws[0], p.grid, op->N, dgamma, dbeta);
         e = cudaGetLastError();
     }
     return e ? op_cuda(op, e, "stacklstm_norm_backward") : SL_OK;

@@ -9,38 +9,68 @@
 
 namespace sl {
 
+// The elements of a piece as fp32.
+template <typename T>
+__device__ __forceinline__ void unpack(const uint4 &q, float (&v)[16 / sizeof(T)])
+{
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (sizeof(T) == 4) {
+            v[j] = __uint_as_float(w[j]);
+        } else {
+            v[2 * j] = __uint_as_float(w[j] << 16);
+            v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+        }
+    }
+}
+
 template <typename T>
 struct RowVec {
     static constexpr int E = 16 / (int)sizeof(T);
-    size_t first;  // the row's first flat element
-    size_t total;  // elements of the whole tensor: nothing is read beyond them
+    size_t at;   // the row's first piece's first flat element
+    int lead;    // elements of that piece that come before the row
     int V;
-    __device__ __forceinline__ RowVec(int r, int V_, size_t rows) : first((size_t)r * V_), total(rows * V_), V(V_) {}
-    // pieces the row touches, and the column of a piece's element 0 (negative before the row)
-    __device__ __forceinline__ int pieces() const { return (int)((first + V - 1) / E - first / E) + 1; }
-    __device__ __forceinline__ int column(int p) const { return p * E - (int)(first % E); }
-    // piece p in v, what is outside the row as -inf
-    __device__ __forceinline__ void load(const T *base, int p, float (&v)[E]) const
+    __device__ __forceinline__ RowVec(size_t r, int V_) : V(V_)
     {
-        const size_t at = (first / E + p) * E;
+        const size_t first = r * V_;
+        lead = (int)(first % E);
+        at = first - lead;
+    }
+    // pieces the row touches, and the column of a piece's element 0 (negative before the row)
+    __device__ __forceinline__ int pieces() const { return (lead + V + E - 1) / E; }
+    __device__ __forceinline__ int column(int p) const { return p * E - lead; }
+    __device__ __forceinline__ bool whole(int p) const
+    {
         const int c = column(p);
-        if (c >= 0 && c + E <= V) {
-            load_vec<T, E>(base + at, v);
-        } else {
+        return c >= 0 && c + E <= V;
+    }
+    __device__ __forceinline__ size_t first() const { return at + lead; }
+    // piece p as it lies in memory, with -inf in the place of what is outside the row (which is
+    // not read)
+    __device__ __forceinline__ uint4 load(const T *base, int p) const
+    {
+        const size_t o = at + (size_t)p * E;
+        if (whole(p)) return *(const uint4 *)(base + o);
+        union {
+            T e[E];
+            uint4 q;
+        } u;
+        const int c = column(p);
 #pragma unroll
-            for (int i = 0; i < E; ++i) v[i] = c + i >= 0 && c + i < V ? to_f32(base[at + i]) : -INFINITY;
-        }
+        for (int i = 0; i < E; ++i) u.e[i] = c + i >= 0 && c + i < V ? base[o + i] : from_f32<T>(-INFINITY);
+        return u.q;
     }
     __device__ __forceinline__ void store_f32(float *base, int p, const float (&v)[E]) const
     {
-        const size_t at = (first / E + p) * E;
-        const int c = column(p);
-        if (c >= 0 && c + E <= V) {
-            store_vec<float, E>(base + at, v);
+        const size_t o = at + (size_t)p * E;
+        if (whole(p)) {
+            store_vec<float, E>(base + o, v);
         } else {
+            const int c = column(p);
 #pragma unroll
             for (int i = 0; i < E; ++i)
-                if (c + i >= 0 && c + i < V) base[at + i] = v[i];
+                if (c + i >= 0 && c + i < V) base[o + i] = v[i];
         }
     }
 };
@@ -52,25 +82,39 @@ __device__ __forceinline__ float max_nan(float a, float b)
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
     return m;
 }
-__device__ __forceinline__ float warp_max(float v)
+
+// A warp's sums (maxima) of NV values at once: their shuffles in flight together.
+template <bool MAX, int NV>
+__device__ __forceinline__ void warp_join(float (&v)[NV])
 {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = max_nan(v, __shfl_xor_sync(0xffffffffu, v, o));
-    return v;
+    for (int o = 16; o > 0; o >>= 1) {
+        float w[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) w[i] = __shfl_xor_sync(0xffffffffu, v[i], o);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] = MAX ? max_nan(v[i], w[i]) : v[i] + w[i];
+    }
 }
-template <int TPR>
-__device__ __forceinline__ float row_max(float v, float *sm)
+// The same over the TPR threads of a row: a warp, or the whole CTA through `sm` (NV TPR / 32
+// floats, free again after the call).
+template <bool MAX, int TPR, int NV>
+__device__ __forceinline__ void row_join(float (&v)[NV], float *sm)
 {
-    v = warp_max(v);
+    warp_join<MAX>(v);
     if constexpr (TPR > 32) {
-        if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = v;
-        __syncthreads();
-        v = sm[0];
+        constexpr int W = TPR / 32;
+        const int lane = threadIdx.x & 31;
+        if (lane == 0)
 #pragma unroll
-        for (int i = 1; i < TPR / 32; ++i) v = max_nan(v, sm[i]);
+            for (int i = 0; i < NV; ++i) sm[i * W + (threadIdx.x >> 5)] = v[i];
+        __syncthreads();
+        // every warp joins the warps' values, lane by lane and then in a butterfly
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] = lane < W ? sm[i * W + lane] : MAX ? -INFINITY : 0.0f;
+        warp_join<MAX>(v);
         __syncthreads();
     }
-    return v;
 }
 
 __device__ __forceinline__ float exp2_hw(float x)
@@ -81,20 +125,27 @@ __device__ __forceinline__ float exp2_hw(float x)
 }
 constexpr float kLog2e = 1.4426950408889634f;
 
-// How a row of V elements is spread: a warp or a CTA of kRowThreads, its pieces in the threads'
-// registers (NP a thread) or, for the widest rows, read again in each pass (NP = 0).
-constexpr int kRowThreads = 512;
+// How a row of V elements is spread: over a warp where four pieces a lane hold it, else over the
+// least of 128, 512 and 1024 threads with up to eight pieces in the registers of each; the widest
+// rows are read again in each pass (NP = 0).
 template <typename T>
 inline void row_plan(int V, int *tpr, int *np)
 {
     const int n = (int)(((size_t)V + RowVec<T>::E - 1) / RowVec<T>::E) + 1;  // most pieces of a row
-    auto up = [](int v) { return v <= 1 ? 1 : v <= 2 ? 2 : v <= 4 ? 4 : v <= 8 ? 8 : v <= 16 ? 16 : 0; };
+    auto up = [](unsigned v) { return v <= 1 ? 1 : v <= 2 ? 2 : v <= 4 ? 4 : v <= 8 ? 8 : 0; };
     *tpr = 32;
-    *np = up((int)ceil_div(n, 32));
-    if (*np == 0 || *np > 4) {
-        *tpr = kRowThreads;
-        *np = up((int)ceil_div(n, kRowThreads));
+    *np = up(ceil_div(n, 32));
+    if (*np && *np <= 4) return;
+    for (int t : {128, 512, 1024}) {
+        *tpr = t;
+        *np = up(ceil_div(n, t));
+        if (*np) return;
     }
 }
+// the kernels that row_plan can ask for: X(threads, pieces)
+#define SL_ROW_PLANS(X) \
+    X(32, 1) X(32, 2) X(32, 4) X(128, 2) X(128, 4) X(128, 8) X(512, 4) X(512, 8) X(1024, 8) X(1024, 0)
+__host__ __device__ constexpr int row_cta(int tpr) { return tpr == 32 ? 256 : tpr; }
+__host__ __device__ constexpr int row_ctas_per_sm(int tpr) { return tpr == 32 ? 5 : tpr == 128 ? 8 : tpr == 512 ? 2 : 1; }
 
 }  // namespace sl
