@@ -16,9 +16,7 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int kSelThreads = 256;
-constexpr int kSelItems = 32;                          // candidates a thread
-constexpr int kSegment = kSelThreads * kSelItems;      // candidates a CTA
+// A CTA of NT threads looks at NI candidates a thread: 256 x 32, or 512 x 64 where there are many.
 constexpr int kMergeItems = 16;                        // keys a thread and pass of the merge
 constexpr int kWideRow = 1024;                         // classes from which a CTA keeps to one row
 constexpr int kMaxBeams = 64;
@@ -28,12 +26,11 @@ template <typename T, int TPR, int NP>
 __global__ void __launch_bounds__(row_cta(TPR), row_ctas_per_sm(TPR))
 lse_rows(int rows, int V, const T *__restrict__ z, float *__restrict__ lse)
 {
-    constexpr int E = RowVec<T>::E, RPC = TPR == 32 ? 8 : 1;
+    constexpr int E = RowVec<T>::E;
     __shared__ float sm[32];
-    const int r = blockIdx.x * RPC + (TPR == 32 ? threadIdx.x / 32 : 0), t = threadIdx.x % TPR;
-    if (r >= rows) return;
+    const int r = blockIdx.x * rows_per_cta(TPR) + (TPR <= 32 ? threadIdx.x / TPR : 0), t = threadIdx.x % TPR;
     const RowVec<T> row(r, V);
-    const int n = row.pieces();
+    const int n = r < rows ? row.pieces() : 0;  // (a row past the end has no pieces: its lanes stay for the joins)
     uint4 q[NP > 0 ? NP : 1];
     if constexpr (NP > 0) {
 #pragma unroll
@@ -58,10 +55,13 @@ lse_rows(int rows, int V, const T *__restrict__ z, float *__restrict__ lse)
         }
     };
     float m[1] = {-INFINITY}, s[1] = {0.0f};
-    each([&](const float (&v)[E]) {
+    if constexpr (NP > 0) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) m[0] = max_nan(m[0], v[i]);
-    });
+        for (int j = 0; j < NP; ++j)
+            if (j * TPR + t < n) m[0] = max_nan(m[0], piece_max<T, true>(q[j]));
+    } else {
+        for (int p = t; p < n; p += TPR) m[0] = max_nan(m[0], piece_max<T, true>(row.load(z, p)));
+    }
     row_join<true, TPR>(m, sm);
     const float base = m[0] == -INFINITY ? 0.0f : m[0];  // a row of -inf sums to 0: its lse is -inf
     each([&](const float (&v)[E]) {
@@ -69,7 +69,7 @@ lse_rows(int rows, int V, const T *__restrict__ z, float *__restrict__ lse)
         for (int i = 0; i < E; ++i) s[0] += exp2_hw((v[i] - base) * kLog2e);
     });
     row_join<false, TPR>(s, sm);
-    if (t == 0) lse[r] = base + logf(s[0]);
+    if (t == 0 && r < rows) lse[r] = base + logf(s[0]);
 }
 
 template <typename T>
@@ -77,7 +77,7 @@ cudaError_t launch_lse(int rows, int V, const void *z, float *lse, cudaStream_t 
 {
     int tpr, np;
     row_plan<T>(V, &tpr, &np);
-    const unsigned grid = ceil_div(rows, tpr == 32 ? 8 : 1);
+    const unsigned grid = ceil_div(rows, rows_per_cta(tpr));
 #define SL_LSE(t, n) \
     if (tpr == t && np == n) lse_rows<T, t, n><<<grid, row_cta(t), 0, st>>>(rows, V, (const T *)z, lse);
     SL_ROW_PLANS(SL_LSE)
@@ -102,51 +102,50 @@ __device__ __forceinline__ float key_score(u64 key)
 constexpr int kList = 1024;  // keys that are ranked together, most times
 
 struct SelShared {
-    u64 top[kSelThreads];  // the groups' (threads') best keys
+    u64 top[512];          // the threads' best keys
+    float group[64];       // the groups' best scores
     u64 best[kMaxBeams];   // the K best, sorted
     u64 list[kList];
     u64 kth;
+    float least;
     int count, last;
     float score[kMaxBeams], lse[kMaxBeams];
     uint8_t done[kMaxBeams];
 };
 
-// The K best of the CTA's keys into s.best, sorted. `mine` is the thread's best key and
-// push(bound, f) calls f with each of the thread's keys that are >= bound. Of any disjoint groups
-// of keys, the K-th best of the groups' best is no better than the K-th best of all: first the
-// threads' best are grouped (8 lanes a group, 4 for more than 32 hypotheses) and the keys from
-// that bound on are listed and ranked against one another. Where they are more than the list
-// holds (most of a row alike), the bound is the K-th of the threads' own best, from which on there
-// are at most K times a thread's keys, in `spill`.
-template <typename Push>
-__device__ __forceinline__ void block_topk(u64 mine, const Push &push, int K, SelShared &s, u64 *spill)
+// The K best of the CTA's keys into s.best, sorted. `top` is the best score of the thread's keys
+// (-inf: none), push(least, f) calls f with each of the thread's keys of a score >= least, and
+// best_key() is its best key. Of any disjoint groups of keys, the K-th best of the groups' best
+// scores is no better than the K-th best of all: first the threads' best are grouped (32 groups, 64
+// for more than 32 hypotheses) and the keys from that score on are listed and ranked against one
+// another. Where they are more than the list holds (most of a row alike), the bound is the K-th of
+// the threads' own best keys, from which on there are at most K times a thread's keys, in `spill`.
+template <int NT, typename Push, typename Best>
+__device__ __forceinline__ void block_topk(float top, const Push &push, const Best &best_key, int K, SelShared &s, u64 *spill)
 {
     const int tid = threadIdx.x, lane = tid & 31;
-    const int width = K <= 32 ? 8 : 4, groups = kSelThreads / width;
-    u64 g = mine;
-    for (int o = 1; o < width; o <<= 1) {
-        const u64 w = __shfl_xor_sync(0xffffffffu, g, o);
-        g = w > g ? w : g;
-    }
+    const int width = K <= 32 ? NT / 32 : NT / 64, groups = NT / width;
+    float g = top;
+    for (int o = 1; o < width; o <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, o));
     __syncthreads();
-    if (lane % width == 0) s.top[tid / width] = g;
+    if (lane % width == 0) s.group[tid / width] = g;
     if (tid == 0) {
         s.count = 0;
-        s.kth = 1;  // fewer than K groups with a candidate: every one counts
+        s.least = -INFINITY;  // fewer than K groups with a candidate: every one counts
     }
     if (tid < K) s.best[tid] = 0;
     __syncthreads();
     if (tid < groups) {
-        const u64 k = s.top[tid];
+        const float mine = s.group[tid];
         int above = 0;
 #pragma unroll 8
-        for (int i = 0; i < groups; ++i) above += s.top[i] > k;
-        if (k && above == K - 1) s.kth = k;
+        for (int i = 0; i < groups; ++i) above += s.group[i] > mine || (s.group[i] == mine && i < tid);
+        if (above == K - 1) s.least = mine;
     }
     __syncthreads();
-    const u64 bound = s.kth;
-    if (mine >= bound)
-        push(bound, [&](u64 k) {
+    const float least = s.least;
+    if (top > -INFINITY && top >= least)
+        push(least, [&](u64 k) {
             const int at = atomicAdd(&s.count, 1);  // any order: they are ranked below
             if (at < kList) s.list[at] = k;
         });
@@ -155,6 +154,7 @@ __device__ __forceinline__ void block_topk(u64 mine, const Push &push, int K, Se
     u64 *list = s.list;
     if (n > kList) {
         list = spill;
+        const u64 mine = best_key();
         __syncthreads();
         s.top[tid] = mine;
         if (tid == 0) {
@@ -164,15 +164,18 @@ __device__ __forceinline__ void block_topk(u64 mine, const Push &push, int K, Se
         __syncthreads();
         int above = 0;
         if (mine)
-            for (int i = 0; i < kSelThreads; ++i) above += s.top[i] > mine;
+            for (int i = 0; i < NT; ++i) above += s.top[i] > mine;
         if (mine && above == K - 1) s.kth = mine;
         __syncthreads();
-        const u64 tight = s.kth;
-        if (mine >= tight) push(tight, [&](u64 k) { list[atomicAdd(&s.count, 1)] = k; });
+        const u64 kth = s.kth;
+        if (mine >= kth)
+            push(key_score(kth), [&](u64 k) {
+                if (k >= kth) list[atomicAdd(&s.count, 1)] = k;
+            });
         __syncthreads();
         n = s.count;
     }
-    for (int e = tid; e < n; e += kSelThreads) {
+    for (int e = tid; e < n; e += NT) {
         const u64 k = list[e];
         int above = 0;
         for (int i = 0; i < n; ++i) above += list[i] > k;
@@ -182,24 +185,24 @@ __device__ __forceinline__ void block_topk(u64 mine, const Push &push, int K, Se
 }
 
 // Keys that a thread has at hand.
-template <int PT>
+template <int NT, int PT>
 __device__ __forceinline__ void keys_topk(const u64 (&key)[PT], int K, SelShared &s, u64 *spill)
 {
     u64 mine = 0;
 #pragma unroll
     for (int i = 0; i < PT; ++i) mine = key[i] > mine ? key[i] : mine;
-    block_topk(mine, [&](u64 bound, auto f) {
+    block_topk<NT>(mine ? key_score(mine) : -INFINITY, [&](float least, auto f) {
 #pragma unroll
         for (int i = 0; i < PT; ++i)
-            if (key[i] >= bound) f(key[i]);
-    }, K, s, spill);
+            if (key[i] && key_score(key[i]) >= least) f(key[i]);
+    }, [&] { return mine; }, K, s, spill);
 }
 
-// Sentence blockIdx.y; the candidates of segment blockIdx.x: kSegment of the sentence's K V
-// (ROWS = false), or kSegment of the V of hypothesis blockIdx.x / per_row. The K best of each
+// Sentence blockIdx.y; the candidates of segment blockIdx.x: NT NI of the sentence's K V
+// (ROWS = false), or NT NI of the V of hypothesis blockIdx.x / per_row. The K best of each
 // segment go to `part`, and the sentence's last CTA joins them.
-template <typename T, bool ROWS>
-__global__ void __launch_bounds__(kSelThreads)
+template <typename T, bool ROWS, int NT, int NI>
+__global__ void __launch_bounds__(NT, !ROWS || (NT == 512 && sizeof(T) == 4) ? 1 : 1024 / NT)
 beam_select(int K, int V, int nseg, int per_row, const T *__restrict__ z, const float *__restrict__ lse,
             const float *__restrict__ score, const uint8_t *__restrict__ done, u64 *__restrict__ part,
             int *__restrict__ arrived, float *__restrict__ out_score, int32_t *__restrict__ parent,
@@ -214,76 +217,65 @@ beam_select(int K, int V, int nseg, int per_row, const T *__restrict__ z, const 
         s.done[tid] = done ? done[(size_t)b * K + tid] : 0;
     }
     if constexpr (ROWS) {
-        constexpr int E = RowVec<T>::E, NP = kSelItems / E;
-        const int k = seg / per_row, piece0 = seg % per_row * (kSegment / E) + tid;
+        constexpr int E = RowVec<T>::E, NP = NI / E;
+        const int k = seg / per_row, piece0 = seg % per_row * (NT * NI / E) + tid;
         const RowVec<T> row((size_t)b * K + k, V);
         const int n = row.pieces();
         uint4 q[NP];
 #pragma unroll
         for (int j = 0; j < NP; ++j)
-            if (piece0 + j * kSelThreads < n) q[j] = row.load(z, piece0 + j * kSelThreads);
+            if (piece0 + j * NT < n) q[j] = row.load(z, piece0 + j * NT);
         __syncthreads();
         const float add = s.score[k], sub = s.lse[k];
         const bool is_done = s.done[k];
         const uint32_t place0 = (uint32_t)k * (uint32_t)V;
-        u64 mine = 0;
-        if (is_done) {
-            if (seg % per_row == 0 && tid == 0) mine = make_key(add, place0);
-        } else {
-            float top = -INFINITY;
-            uint32_t at = 0;
+        // (rounded operations keep the order: the best score is that of the largest logit)
+        float zmax = -INFINITY;
 #pragma unroll
-            for (int j = 0; j < NP; ++j)
-                if (piece0 + j * kSelThreads < n) {
-                    float v[E];
-                    unpack<T>(q[j], v);
-#pragma unroll
-                    for (int i = 0; i < E; ++i) {  // places go up: of equal scores the first stays
-                        const float c = __fadd_rn(add, __fsub_rn(v[i], sub));
-                        if (c > top) {
-                            top = c;
-                            at = (uint32_t)(row.column(piece0 + j * kSelThreads) + i);
-                        }
-                    }
-                }
-            if (top > -INFINITY) mine = make_key(top, place0 + at);
-        }
-        block_topk(mine, [&](u64 bound, auto f) {
+        for (int j = 0; j < NP; ++j)
+            if (piece0 + j * NT < n) zmax = fmaxf(zmax, piece_max<T, false>(q[j]));
+        const auto cand = [&](float v) { return __fadd_rn(add, __fsub_rn(v, sub)); };
+        float top = cand(zmax);
+        if (is_done) top = seg % per_row == 0 && tid == 0 ? add : -INFINITY;
+        if (!(top > -INFINITY)) top = -INFINITY;
+        auto push = [&](float least, auto f) {
             if (is_done) {
-                f(mine);
+                f(make_key(add, place0));
                 return;
             }
-            const float least = bound > 1 ? key_score(bound) : -INFINITY;
 #pragma unroll
             for (int j = 0; j < NP; ++j)
-                if (piece0 + j * kSelThreads < n) {
+                if (piece0 + j * NT < n && cand(piece_max<T, false>(q[j])) >= least) {
                     float v[E];
                     unpack<T>(q[j], v);
 #pragma unroll
                     for (int i = 0; i < E; ++i) {
-                        const float c = __fadd_rn(add, __fsub_rn(v[i], sub));
-                        if (c >= least) {
-                            const u64 key = make_key(c, place0 + (uint32_t)(row.column(piece0 + j * kSelThreads) + i));
-                            if (key >= bound) f(key);
-                        }
+                        const float c = cand(v[i]);
+                        if (c >= least && c > -INFINITY) f(make_key(c, place0 + (uint32_t)(row.column(piece0 + j * NT) + i)));
                     }
                 }
-        }, K, s, spill);
+        };
+        auto best_key = [&] {
+            u64 mine = 0;
+            if (top > -INFINITY) push(top, [&](u64 k) { mine = k > mine ? k : mine; });
+            return mine;
+        };
+        block_topk<NT>(top, push, best_key, K, s, spill);
     } else {
         const uint32_t n = (uint32_t)K * (uint32_t)V;
         const T *zb = z + (size_t)b * n;
-        float v[kSelItems];
-        const uint32_t e0 = (uint32_t)seg * kSegment + tid;
+        float v[NI];
+        const uint32_t e0 = (uint32_t)seg * (NT * NI) + tid;
 #pragma unroll
-        for (int i = 0; i < kSelItems; ++i) {
-            const uint32_t e = e0 + i * kSelThreads;
+        for (int i = 0; i < NI; ++i) {
+            const uint32_t e = e0 + i * NT;
             v[i] = e < n ? to_f32(zb[e]) : -INFINITY;
         }
         __syncthreads();
-        u64 key[kSelItems];
+        u64 key[NI];
 #pragma unroll
-        for (int i = 0; i < kSelItems; ++i) {
-            const uint32_t e = e0 + i * kSelThreads;
+        for (int i = 0; i < NI; ++i) {
+            const uint32_t e = e0 + i * NT;
             key[i] = 0;
             if (e < n) {
                 const uint32_t k = e / (uint32_t)V;
@@ -293,7 +285,7 @@ beam_select(int K, int V, int nseg, int per_row, const T *__restrict__ z, const 
                     key[i] = make_key(s.score[k], e);
             }
         }
-        keys_topk<kSelItems>(key, K, s, spill);
+        keys_topk<NT, NI>(key, K, s, spill);
     }
     if (nseg > 1) {  // the sentence's last CTA joins the segments
         if (tid < K) part[((size_t)b * nseg + seg) * K + tid] = s.best[tid];
@@ -305,18 +297,18 @@ beam_select(int K, int V, int nseg, int per_row, const T *__restrict__ z, const 
         __threadfence();
         if (tid == 0) arrived[b] = 0;  // for the next call
         const u64 *mine = part + (size_t)b * nseg * K;
-        const int total = nseg * K, step = kSelThreads * (kMergeItems - 1);
+        const int total = nseg * K, step = NT * (kMergeItems - 1);
         if (tid < K) s.best[tid] = 0;
         __syncthreads();
         for (int at = 0; at < total; at += step) {
             u64 key[kMergeItems];
 #pragma unroll
             for (int i = 0; i < kMergeItems - 1; ++i) {
-                const int e = at + i * kSelThreads + tid;
+                const int e = at + i * NT + tid;
                 key[i] = e < total ? __ldcg(mine + e) : 0;
             }
             key[kMergeItems - 1] = tid < K ? s.best[tid] : 0;  // the best so far
-            keys_topk<kMergeItems>(key, K, s, spill);
+            keys_topk<NT, kMergeItems>(key, K, s, spill);
         }
     }
     if (tid < K) {
@@ -335,20 +327,43 @@ beam_select(int K, int V, int nseg, int per_row, const T *__restrict__ z, const 
 }
 
 // Segments of a sentence: by rows where a row fills most of a CTA's threads, else across the rows
-// (8 x 83 candidates are one CTA's; by rows they would be eight, and their join).
+// (8 x 83 candidates are one CTA's; by rows they would be eight, and their join). Larger CTAs where
+// the small ones would be more than run at once four to an SM: 64 x 8 x 32003 bf16 25 us in 2048
+// CTAs, 15 in 512.
 struct SelPlan {
-    bool rows;
+    bool rows, large;
     int per_row, nseg;
 };
 template <typename T>
-SelPlan select_plan(int K, int V)
+SelPlan select_plan(int B, int K, int V, int sms)
 {
     SelPlan p;
     p.rows = V >= kWideRow;
     constexpr size_t E = RowVec<T>::E;
-    p.per_row = (int)ceil_div(((size_t)V + E - 1) / E + 1, kSegment / E);
-    p.nseg = p.rows ? K * p.per_row : (int)ceil_div((size_t)K * V, kSegment);
+    const size_t pieces = ((size_t)V + E - 1) / E + 1;
+    p.per_row = (int)ceil_div(pieces, 256 * 32 / E);
+    p.large = p.rows && (size_t)B * K * p.per_row > 4 * (size_t)sms && p.per_row > 1;
+    if (p.large) p.per_row = (int)ceil_div(pieces, 512 * 64 / E);
+    p.nseg = p.rows ? K * p.per_row : (int)ceil_div((size_t)K * V, 256 * 32);
     return p;
+}
+template <typename T>
+cudaError_t launch_select(const stacklstm_op *op, const void *z, const float *lse, const float *score, const uint8_t *done,
+                          float *new_score, int32_t *parent, int32_t *token)
+{
+    const int K = op->beams, V = op->V;
+    const SelPlan p = select_plan<T>(op->B, K, V, op->num_sms);
+    auto launch = [&](auto kernel, int nt, int ni) {
+        kernel<<<dim3(p.nseg, op->B), nt, (size_t)K * ni * 8, op->stream>>>(  // (at most 32 KB)
+            K, V, p.nseg, p.per_row, (const T *)z, lse, score, done, (u64 *)op->ws[0], (int *)op->ws[1], new_score, parent, token);
+    };
+    if (p.large)
+        launch(beam_select<T, true, 512, 64>, 512, 64);
+    else if (p.rows)
+        launch(beam_select<T, true, 256, 32>, 256, 32);
+    else
+        launch(beam_select<T, false, 256, 32>, 256, 32);
+    return cudaGetLastError();
 }
 
 // ------------------------------------------------------------------ stacks
@@ -372,12 +387,39 @@ __device__ __forceinline__ int source_row(int n, int K, int S, const int32_t *pa
     return src;
 }
 
-// Row n (blockIdx.x) of the new stacks: the slots 0 .. p of its source row, and its top. PH and
-// PC pieces (types QH, QC) of h and c a slot. A CTA takes kSlots slots, its threads their pieces in
-// order, four copies in flight each (a CTA a slot kept 75 of 256 threads busy at H = 200).
+// `slots` slots from s0 on of row src to row n, `per` pieces each; slot top also to top_out. The
+// CTA's threads take the pieces in order, four copies in flight each.
+template <typename Q>
+__device__ __forceinline__ void copy_slots(const Q *__restrict__ from, Q *__restrict__ to, Q *__restrict__ top_out, int N,
+                                           int src, int n, int s0, int slots, int per, int top)
+{
+    const int total = slots * per;
+    for (int i0 = threadIdx.x; i0 < total; i0 += 4 * blockDim.x) {
+        Q v[4];
+        size_t at[4];
+        bool last[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int i = i0 + u * blockDim.x, slot = i / per, c = i - slot * per;
+            at[u] = ((size_t)(s0 + slot) * N) * per + c;
+            last[u] = s0 + slot == top;
+            if (i < total) v[u] = from[at[u] + (size_t)src * per];
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (i0 + u * (int)blockDim.x < total) {
+                to[at[u] + (size_t)n * per] = v[u];
+                if (last[u] && top_out) top_out[(size_t)n * per + (at[u] % per)] = v[u];
+            }
+    }
+}
+
+// Row n (blockIdx.x) of the new stacks: kSlots of the slots 0 .. p of its source row, and its top.
+// PH and PC pieces (types QH, QC) of h and c a slot. (A CTA a slot kept 75 of 256 threads busy at
+// H = 200.)
 constexpr int kSlots = 16;
 template <typename QH, typename QC>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 4)
 reorder_rows(int N, int K, int S, int PH, int PC, const int32_t *__restrict__ parent, const int32_t *__restrict__ p,
              const QH *__restrict__ h, const QC *__restrict__ c, int32_t *__restrict__ p_out, QH *__restrict__ h_out,
              QC *__restrict__ c_out, QH *__restrict__ top_h, QC *__restrict__ top_c, int32_t *err)
@@ -388,38 +430,8 @@ reorder_rows(int N, int K, int S, int PH, int PC, const int32_t *__restrict__ pa
     if (blockIdx.y == 0 && threadIdx.x == 0) p_out[n] = top;
     const int slots = min(kSlots, top + 1 - s0);
     if (slots <= 0) return;
-    const int per = PH + PC, total = slots * per;
-    for (int i0 = threadIdx.x; i0 < total; i0 += 4 * 256) {
-        QH vh[4];
-        QC vc[4];
-        int slot[4], at[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int i = i0 + u * 256;
-            slot[u] = i / per;
-            at[u] = i - slot[u] * per;
-            if (i < total) {
-                const size_t from = (size_t)(s0 + slot[u]) * N + src;
-                if (at[u] < PH)
-                    vh[u] = h[from * PH + at[u]];
-                else
-                    vc[u] = c[from * PC + (at[u] - PH)];
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            if (i0 + u * 256 >= total) break;
-            const int s = s0 + slot[u];
-            const size_t to = (size_t)s * N + n;
-            if (at[u] < PH) {
-                h_out[to * PH + at[u]] = vh[u];
-                if (s == top && top_h) top_h[(size_t)n * PH + at[u]] = vh[u];
-            } else {
-                c_out[to * PC + (at[u] - PH)] = vc[u];
-                if (s == top && top_c) top_c[(size_t)n * PC + (at[u] - PH)] = vc[u];
-            }
-        }
-    }
+    copy_slots(c, c_out, top_c, N, src, n, s0, slots, PC, top);
+    copy_slots(h, h_out, top_h, N, src, n, s0, slots, PH, top);
 }
 
 // Row n: the new state into slot p + 1 of a push, p moved by the op, the new top out.
@@ -486,7 +498,7 @@ sl_status stacklstm_beam_create(stacklstm_op_t *out, int B, int K, int V, int S,
     if (!op) return st;
     op->R = B * K; op->B = B; op->beams = K; op->V = V; op->S = S; op->H = H;
     OpDevice guard(device);
-    const size_t nseg = dtype == SL_BF16 ? select_plan<__nv_bfloat16>(K, V).nseg : select_plan<float>(K, V).nseg;
+    const size_t nseg = dtype == SL_BF16 ? select_plan<__nv_bfloat16>(B, K, V, op->num_sms).nseg : select_plan<float>(B, K, V, op->num_sms).nseg;
     cudaError_t e = op_workspace(op, 0, (size_t)B * nseg * K * 8);
     if (!e) e = op_workspace(op, 1, (size_t)B * 4);
     if (!e) e = cudaMemset(op->ws[1], 0, (size_t)B * 4);
@@ -518,20 +530,9 @@ sl_status stacklstm_beam_select(stacklstm_op_t op, const void *logits, const flo
         return op_fail(op, SL_ERR_ARG, m);
     if (new_score == score) return op_fail(op, SL_ERR_ARG, "new_score must not be score: it is read by the whole sentence");
     OpDevice guard(op->device);
-    const int K = op->beams, V = op->V;
-    const size_t smem = (size_t)K * kSelItems * 8;  // at most 16 KB
-    auto launch = [&](auto kernel, const SelPlan &p, auto *z) {
-        kernel<<<dim3(p.nseg, op->B), kSelThreads, smem, op->stream>>>(K, V, p.nseg, p.per_row, z, lse, score, done, (u64 *)op->ws[0],
-                                                                       (int *)op->ws[1], new_score, parent, token);
-    };
-    if (op->dt == SL_BF16) {
-        const SelPlan p = select_plan<__nv_bfloat16>(K, V);
-        launch(p.rows ? beam_select<__nv_bfloat16, true> : beam_select<__nv_bfloat16, false>, p, (const __nv_bfloat16 *)logits);
-    } else {
-        const SelPlan p = select_plan<float>(K, V);
-        launch(p.rows ? beam_select<float, true> : beam_select<float, false>, p, (const float *)logits);
-    }
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = op->dt == SL_BF16
+                              ? launch_select<__nv_bfloat16>(op, logits, lse, score, done, new_score, parent, token)
+                              : launch_select<float>(op, logits, lse, score, done, new_score, parent, token);
     return e ? op_cuda(op, e, "stacklstm_beam_select") : SL_OK;
 }
 

@@ -12,6 +12,7 @@
 // CTA order, so the gradients are bitwise reproducible. (Products that a sum follows are rounded
 // by __fmul_rn where a null output would otherwise let the compiler fuse the two, and change bits.)
 #include "rowvec.cuh"
+#include "tc.cuh"
 
 namespace sl {
 namespace {
@@ -21,12 +22,28 @@ namespace {
 // row starts on 16 bytes, else 1.
 constexpr int kWideThreads = 256;
 __host__ __device__ constexpr int norm_threads(int tpr) { return tpr == 32 ? 128 : 256; }
-// CTAs an SM: as many as their registers allow (the next row's pieces, and in the backward the
-// column sums, stay in them), and no more than leave the parts few
-__host__ __device__ constexpr int norm_ctas(int tpr, int elems, bool bwd)
+// CTAs an SM of the forward: as many as their registers allow (the next row's pieces stay in them)
+__host__ __device__ constexpr int norm_ctas(int tpr, int elems)
 {
-    return tpr == 32 ? (elems <= 8 ? 8 : elems <= 16 ? (bwd ? 5 : 8) : bwd ? 3 : 6)
-                     : (elems <= 8 ? 4 : elems <= 16 ? (bwd ? 2 : 4) : bwd ? 1 : 3);
+    return tpr == 32 ? (elems <= 16 ? 8 : 6) : (elems <= 16 ? 4 : 3);
+}
+
+// VEC fp32 values (whole: their address is on 32 bytes).
+template <int VEC>
+__device__ __forceinline__ void load_f32(const float *p, bool whole, float *v)
+{
+    if constexpr (VEC == 8)
+        load8(p, whole, v);
+    else
+        load_vec<float, VEC>(p, v);
+}
+template <int VEC>
+__device__ __forceinline__ void store_f32(float *p, bool whole, const float *v)
+{
+    if constexpr (VEC == 8)
+        store8(p, whole, v);
+    else
+        store_vec<float, VEC>(p, v);
 }
 
 // A piece as it lies in memory.
@@ -58,7 +75,7 @@ struct Piece<T, 1> {
 };
 
 template <typename T, int VEC, int CH, int TPR>
-__global__ void __launch_bounds__(norm_threads(TPR), norm_ctas(TPR, CH * VEC, false))
+__global__ void __launch_bounds__(norm_threads(TPR), norm_ctas(TPR, CH * VEC))
 norm_fwd(int rows, int N, const T *__restrict__ x, const float *__restrict__ gamma, const float *__restrict__ beta,
          float eps, T *__restrict__ y, float *__restrict__ mean, float *__restrict__ rstd)
 {
@@ -66,6 +83,7 @@ norm_fwd(int rows, int N, const T *__restrict__ x, const float *__restrict__ gam
     __shared__ float sm[32];
     const int t = threadIdx.x % TPR, step = gridDim.x * RPB;
     const float inv = 1.0f / (float)N;
+    const bool whole = on_32(gamma) && on_32(beta);
     int r = blockIdx.x * RPB + threadIdx.x / TPR;
     Piece<T, VEC> next[CH];
     auto fetch = [&](int row) {
@@ -109,8 +127,8 @@ norm_fwd(int rows, int N, const T *__restrict__ x, const float *__restrict__ gam
                     g[i] = 1.0f;
                     b[i] = 0.0f;
                 }
-                if (gamma) load_vec<float, VEC>(gamma + c, g);
-                if (beta) load_vec<float, VEC>(beta + c, b);
+                if (gamma) load_f32<VEC>(gamma + c, whole, g);
+                if (beta) load_f32<VEC>(beta + c, whole, b);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) v[j][i] = fmaf(v[j][i] * s, g[i], b[i]);
                 store_vec<T, VEC>(y + at + c, v[j]);
@@ -151,60 +169,87 @@ norm_fwd_wide(int rows, int N, const T *__restrict__ x, const float *__restrict_
     }
 }
 
-// part [gridDim.x][2][N]: this CTA's sums of dy xh and dy over its rows.
+// part [gridDim.x][2][N]: this CTA's sums of dy xh and dy over its rows. The pieces (of VEC > 1) of
+// the next kAhead rows of a row's threads are on their way to shared memory while one is worked
+// on, each copied by the thread that uses it; registers are left to the column sums.
+constexpr int kAhead = 2;
+__host__ __device__ constexpr int norm_bwd_threads(int tpr, int elems) { return tpr == 32 ? (elems <= 16 ? 512 : 384) : 256; }
+template <typename T>
+__host__ __device__ constexpr size_t norm_row_bytes(int tpr, int vec, int ch)
+{
+    return vec > 1 ? (size_t)tpr * ch * vec * (4 + sizeof(T)) : 0;
+}
 template <typename T, int VEC, int CH, int TPR>
-__global__ void __launch_bounds__(norm_threads(TPR), norm_ctas(TPR, CH * VEC, true))
+__global__ void __launch_bounds__(norm_bwd_threads(TPR, CH * VEC), TPR == 32 ? 1 : CH * VEC <= 16 ? 2 : 1)
 norm_bwd(int rows, int N, const float *__restrict__ dy, const T *__restrict__ x, const float *__restrict__ gamma,
          const float *__restrict__ mean, const float *__restrict__ rstd, float *__restrict__ dx,
          float *__restrict__ part)
 {
-    constexpr int RPB = norm_threads(TPR) / TPR;
+    constexpr int NT = norm_bwd_threads(TPR, CH * VEC), RPB = NT / TPR;
+    constexpr size_t kRow = norm_row_bytes<T>(TPR, VEC, CH);
     __shared__ float sm[2 * 32];
-    extern __shared__ float cols[];  // [RPB][N] when RPB > 1: the warps' column sums
+    extern __shared__ __align__(16) uint8_t dyn[];  // the rows ahead; then the column sums [RPB][N]
     const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR, step = gridDim.x * RPB;
     const float inv = 1.0f / (float)N;
+    const bool whole = on_32(gamma) && on_32(dx);
     float dg[CH][VEC], db[CH][VEC];
 #pragma unroll
     for (int j = 0; j < CH; ++j)
 #pragma unroll
         for (int i = 0; i < VEC; ++i) dg[j][i] = db[j][i] = 0.0f;
-    Piece<float, VEC> nd[CH];
-    Piece<T, VEC> nx[CH];
-    float nm = 0.0f, ns = 0.0f;
-    auto fetch = [&](int row) {
-        if (row < rows) {
-            nm = mean[row];
-            ns = rstd[row];
+    // slot s of this thread: dy pieces at d(s) + j TPR VEC, x pieces at e(s) + j TPR VEC
+    auto slot = [&](int s) { return dyn + ((size_t)s * RPB + sub) * kRow; };
+    auto d_of = [&](int s) { return (float *)slot(s) + t * VEC; };
+    auto x_of = [&](int s) { return (T *)(slot(s) + (size_t)TPR * CH * VEC * 4) + t * VEC; };
+    auto fetch = [&](int row, int s) {
+        if constexpr (VEC > 1) {
+            if (row < rows)
 #pragma unroll
-            for (int j = 0; j < CH; ++j) {
-                const size_t o = (size_t)row * N + (j * TPR + t) * VEC;
-                if ((j * TPR + t) * VEC < N) {
-                    nd[j].load(dy + o);
-                    nx[j].load(x + o);
+                for (int j = 0; j < CH; ++j) {
+                    const int c = (j * TPR + t) * VEC;
+                    if (c < N) {
+                        const size_t o = (size_t)row * N + c;
+#pragma unroll
+                        for (int i = 0; i < VEC; i += 4) tc::cp_async16(tc::smem_u32(d_of(s) + j * TPR * VEC + i), dy + o + i, 16);
+                        tc::cp_async16(tc::smem_u32(x_of(s) + j * TPR * VEC), x + o, 16);
+                    }
                 }
-            }
+            tc::cp_async_commit();
         }
     };
     int r = blockIdx.x * RPB + sub;
-    fetch(r);
-    for (; r < rows; r += step) {
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) fetch(r + s * step, s);
+    for (int s = 0; r < rows; r += step, s = s + 1 == kAhead ? 0 : s + 1) {
         const size_t at = (size_t)r * N;
-        const float m = nm, s = ns;
+        const float m = mean[r], rs = rstd[r];
         float a[CH][VEC], xh[CH][VEC];
         float sums[2] = {0.0f, 0.0f};  // of a and of a xh
+        if constexpr (VEC > 1) tc::cp_async_wait<kAhead - 1>();
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            const int c = (j * TPR + t) * VEC;
+            if (c < N) {
+                if constexpr (VEC > 1) {
+                    load_vec<float, VEC>(d_of(s) + j * TPR * VEC, a[j]);
+                    load_vec<T, VEC>(x_of(s) + j * TPR * VEC, xh[j]);
+                } else {
+                    load_vec<float, VEC>(dy + at + c, a[j]);
+                    load_vec<T, VEC>(x + at + c, xh[j]);
+                }
+            }
+        }
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
             const int c = (j * TPR + t) * VEC;
             if (c < N) {
                 float g[VEC];
-                nd[j].get(a[j]);
-                nx[j].get(xh[j]);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) g[i] = 1.0f;
-                if (gamma) load_vec<float, VEC>(gamma + c, g);
+                if (gamma) load_f32<VEC>(gamma + c, whole, g);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
-                    xh[j][i] = __fmul_rn(xh[j][i] - m, s);
+                    xh[j][i] = __fmul_rn(xh[j][i] - m, rs);
                     dg[j][i] = fmaf(a[j][i], xh[j][i], dg[j][i]);
                     db[j][i] += a[j][i];
                     a[j][i] = __fmul_rn(a[j][i], g[i]);
@@ -213,7 +258,7 @@ norm_bwd(int rows, int N, const float *__restrict__ dy, const T *__restrict__ x,
                 }
             }
         }
-        fetch(r + step);  // on its way while this row is worked on
+        fetch(r + kAhead * step, s);  // into the slot just read
         if (dx) {
             row_join<false, TPR>(sums, sm);
             const float ma = __fmul_rn(sums[0], inv), mx = __fmul_rn(sums[1], inv);
@@ -222,14 +267,15 @@ norm_bwd(int rows, int N, const float *__restrict__ dy, const T *__restrict__ x,
                 const int c = (j * TPR + t) * VEC;
                 if (c < N) {
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i) a[j][i] = s * (a[j][i] - ma - xh[j][i] * mx);
-                    store_vec<float, VEC>(dx + at + c, a[j]);
+                    for (int i = 0; i < VEC; ++i) a[j][i] = rs * (a[j][i] - ma - xh[j][i] * mx);
+                    store_f32<VEC>(dx + at + c, whole, a[j]);
                 }
             }
         }
     }
+    if constexpr (VEC > 1) tc::cp_async_wait<0>();
     if (!part) return;
-    float *out = part + (size_t)blockIdx.x * 2 * N;
+    float *out = part + (size_t)blockIdx.x * 2 * N, *cols = (float *)dyn;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
         if constexpr (RPB > 1) __syncthreads();
@@ -243,7 +289,7 @@ norm_bwd(int rows, int N, const float *__restrict__ dy, const T *__restrict__ x,
         }
         if constexpr (RPB > 1) {
             __syncthreads();
-            for (int c = threadIdx.x; c < N; c += norm_threads(TPR)) {
+            for (int c = threadIdx.x; c < N; c += NT) {
                 float acc = 0.0f;
 #pragma unroll
                 for (int w = 0; w < RPB; ++w) acc += cols[(size_t)w * N + c];
@@ -327,8 +373,9 @@ NormPlan norm_plan(const stacklstm_op *op, int rows, bool bwd)
     p.tpr = ceil_div(N, p.vec * 32) <= (unsigned)most ? 32 : 256;
     const int n = (int)ceil_div(N, p.vec * p.tpr);
     p.ch = p.vec == 1 ? (n <= 4 ? 4 : n <= 16 ? 16 : 0) : n <= 1 ? 1 : n <= 2 ? 2 : n <= 4 ? 4 : 0;
-    const int per_sm = p.ch ? std::min(norm_ctas(p.tpr, p.ch * p.vec, bwd), bwd ? 4 : 8) : 4;
-    const int rpb = p.ch ? norm_threads(p.tpr) / p.tpr : 1;
+    // (the backward: a CTA an SM of 12 or 16 rows, so that its column sums are few parts)
+    const int per_sm = !p.ch ? 4 : bwd ? (p.tpr == 32 || p.ch * p.vec > 16 ? 1 : 2) : norm_ctas(p.tpr, p.ch * p.vec);
+    const int rpb = !p.ch ? 1 : (bwd ? norm_bwd_threads(p.tpr, p.ch * p.vec) : norm_threads(p.tpr)) / p.tpr;
     p.grid = (int)std::min<size_t>(ceil_div((size_t)rows, (size_t)rpb), (size_t)op->num_sms * per_sm);
     return p;
 }
@@ -347,16 +394,21 @@ struct NormCall {
 };
 
 template <typename T, int VEC, int CH, int TPR>
-void launch_norm(const NormCall &c, int grid)
+cudaError_t launch_norm(const NormCall &c, int grid)
 {
-    constexpr int NT = norm_threads(TPR), RPB = NT / TPR;
     const int N = c.op->N;
-    if (!c.dy)
-        norm_fwd<T, VEC, CH, TPR><<<grid, NT, 0, c.op->stream>>>(c.rows, N, (const T *)c.x, c.gamma, c.beta, c.eps, (T *)c.y,
-                                                                 c.mean, c.rstd);
-    else  // (RPB > 1: N <= 1024, 16 KB)
-        norm_bwd<T, VEC, CH, TPR><<<grid, NT, RPB > 1 ? (size_t)RPB * N * 4 : 0, c.op->stream>>>(
-            c.rows, N, c.dy, (const T *)c.x, c.gamma, c.mean, c.rstd, c.dx, c.part);
+    if (!c.dy) {
+        norm_fwd<T, VEC, CH, TPR><<<grid, norm_threads(TPR), 0, c.op->stream>>>(c.rows, N, (const T *)c.x, c.gamma, c.beta,
+                                                                               c.eps, (T *)c.y, c.mean, c.rstd);
+    } else {
+        constexpr int NT = norm_bwd_threads(TPR, CH * VEC), RPB = NT / TPR;
+        const size_t smem = std::max(kAhead * RPB * norm_row_bytes<T>(TPR, VEC, CH), RPB > 1 ? (size_t)RPB * N * 4 : 0);
+        if (smem > 40 * 1024)
+            if (cudaError_t e = smem_at_least((const void *)norm_bwd<T, VEC, CH, TPR>, smem)) return e;
+        norm_bwd<T, VEC, CH, TPR><<<grid, NT, smem, c.op->stream>>>(c.rows, N, c.dy, (const T *)c.x, c.gamma, c.mean, c.rstd,
+                                                                    c.dx, c.part);
+    }
+    return cudaGetLastError();
 }
 
 template <typename T>
@@ -364,7 +416,7 @@ cudaError_t run_norm(const NormCall &c, const NormPlan &p)
 {
     constexpr int V = 16 / (int)sizeof(T);
 #define SL_NORM(v, n, t) \
-    if (p.vec == v && p.ch == n && p.tpr == t) launch_norm<T, v, n, t>(c, p.grid);
+    if (p.vec == v && p.ch == n && p.tpr == t) return launch_norm<T, v, n, t>(c, p.grid);
     SL_NORM(V, 1, 32) SL_NORM(V, 2, 32) SL_NORM(V, 4, 32) SL_NORM(V, 1, 256) SL_NORM(V, 2, 256) SL_NORM(V, 4, 256)
     SL_NORM(1, 4, 32) SL_NORM(1, 16, 32) SL_NORM(1, 4, 256) SL_NORM(1, 16, 256)
 #undef SL_NORM

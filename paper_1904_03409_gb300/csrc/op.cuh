@@ -130,6 +130,28 @@ __device__ __forceinline__ void store_vec(T *p, const float *v)
     }
 }
 
+// 8 fp32 values as one 32-byte access where `whole` (the address is on 32 bytes), else as two of 16:
+// neighbouring lanes' 32 bytes in two accesses move every sector twice between L1 and L2.
+__device__ __forceinline__ void load8(const float *p, bool whole, float *v)
+{
+    if (whole)
+        asm volatile("ld.global.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                     : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+                     : "l"(p));
+    else
+        load_vec<float, 8>(p, v);
+}
+__device__ __forceinline__ void store8(float *p, bool whole, const float *v)
+{
+    if (whole)
+        asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]),
+                     "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+                     : "memory");
+    else
+        store_vec<float, 8>(p, v);
+}
+__device__ __forceinline__ bool on_32(const void *p) { return ((uintptr_t)p & 31u) == 0; }
+
 __device__ __forceinline__ float warp_sum(float v)
 {
 #pragma unroll

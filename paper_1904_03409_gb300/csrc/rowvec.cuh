@@ -61,11 +61,15 @@ struct RowVec {
         for (int i = 0; i < E; ++i) u.e[i] = c + i >= 0 && c + i < V ? base[o + i] : from_f32<T>(-INFINITY);
         return u.q;
     }
-    __device__ __forceinline__ void store_f32(float *base, int p, const float (&v)[E]) const
+    // (aligned: base is on 32 bytes, so pieces of eight are)
+    __device__ __forceinline__ void store_f32(float *base, bool aligned, int p, const float (&v)[E]) const
     {
         const size_t o = at + (size_t)p * E;
         if (whole(p)) {
-            store_vec<float, E>(base + o, v);
+            if constexpr (E == 8)
+                store8(base + o, aligned, v);
+            else
+                store_vec<float, E>(base + o, v);
         } else {
             const int c = column(p);
 #pragma unroll
@@ -83,12 +87,30 @@ __device__ __forceinline__ float max_nan(float a, float b)
     return m;
 }
 
-// A warp's sums (maxima) of NV values at once: their shuffles in flight together.
-template <bool MAX, int NV>
-__device__ __forceinline__ void warp_join(float (&v)[NV])
+// The largest element of a piece: NaN if any is (NANS), or of those that are not.
+template <typename T, bool NANS>
+__device__ __forceinline__ float piece_max(const uint4 &q)
+{
+    if constexpr (sizeof(T) == 4) {
+        float v[4];
+        unpack<T>(q, v);
+        return NANS ? max_nan(max_nan(v[0], v[1]), max_nan(v[2], v[3])) : fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
+    } else {  // two at a time
+        const __nv_bfloat162 *h = (const __nv_bfloat162 *)&q;
+        const __nv_bfloat162 m = NANS ? __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]))
+                                      : __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+        const float a = __low2float(m), b = __high2float(m);
+        return NANS ? max_nan(a, b) : fmaxf(a, b);
+    }
+}
+
+// The sums (maxima) of NV values at once over groups of G lanes (of a warp), their shuffles in
+// flight together.
+template <bool MAX, int G, int NV>
+__device__ __forceinline__ void lanes_join(float (&v)[NV])
 {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
+    for (int o = G / 2; o > 0; o >>= 1) {
         float w[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) w[i] = __shfl_xor_sync(0xffffffffu, v[i], o);
@@ -96,12 +118,12 @@ __device__ __forceinline__ void warp_join(float (&v)[NV])
         for (int i = 0; i < NV; ++i) v[i] = MAX ? max_nan(v[i], w[i]) : v[i] + w[i];
     }
 }
-// The same over the TPR threads of a row: a warp, or the whole CTA through `sm` (NV TPR / 32
-// floats, free again after the call).
+// The same over the TPR threads of a row: some lanes of a warp, or the whole CTA through `sm`
+// (NV TPR / 32 floats, free again after the call).
 template <bool MAX, int TPR, int NV>
 __device__ __forceinline__ void row_join(float (&v)[NV], float *sm)
 {
-    warp_join<MAX>(v);
+    lanes_join<MAX, (TPR < 32 ? TPR : 32)>(v);
     if constexpr (TPR > 32) {
         constexpr int W = TPR / 32;
         const int lane = threadIdx.x & 31;
@@ -112,7 +134,7 @@ __device__ __forceinline__ void row_join(float (&v)[NV], float *sm)
         // every warp joins the warps' values, lane by lane and then in a butterfly
 #pragma unroll
         for (int i = 0; i < NV; ++i) v[i] = lane < W ? sm[i * W + lane] : MAX ? -INFINITY : 0.0f;
-        warp_join<MAX>(v);
+        lanes_join<MAX, 32>(v);
         __syncthreads();
     }
 }
@@ -125,27 +147,27 @@ __device__ __forceinline__ float exp2_hw(float x)
 }
 constexpr float kLog2e = 1.4426950408889634f;
 
-// How a row of V elements is spread: over a warp where four pieces a lane hold it, else over the
-// least of 128, 512 and 1024 threads with up to eight pieces in the registers of each; the widest
-// rows are read again in each pass (NP = 0).
+// How a row of V elements is spread: over 8 lanes or a warp where four pieces a lane hold it, else
+// over the least of 128, 512 and 1024 threads with up to eight pieces in the registers of each; the
+// widest rows are read again in each pass (NP = 0). (Eight lanes: four rows share a warp's
+// instructions; 11840 rows of 83 fp32 classes a warp each were bound by them.)
 template <typename T>
 inline void row_plan(int V, int *tpr, int *np)
 {
     const int n = (int)(((size_t)V + RowVec<T>::E - 1) / RowVec<T>::E) + 1;  // most pieces of a row
     auto up = [](unsigned v) { return v <= 1 ? 1 : v <= 2 ? 2 : v <= 4 ? 4 : v <= 8 ? 8 : 0; };
-    *tpr = 32;
-    *np = up(ceil_div(n, 32));
-    if (*np && *np <= 4) return;
-    for (int t : {128, 512, 1024}) {
+    for (int t : {8, 32, 128, 512, 1024}) {
         *tpr = t;
         *np = up(ceil_div(n, t));
-        if (*np) return;
+        if (*np && *np <= (t <= 32 ? 4 : 8)) return;
     }
+    *np = 0;
 }
 // the kernels that row_plan can ask for: X(threads, pieces)
 #define SL_ROW_PLANS(X) \
-    X(32, 1) X(32, 2) X(32, 4) X(128, 2) X(128, 4) X(128, 8) X(512, 4) X(512, 8) X(1024, 8) X(1024, 0)
-__host__ __device__ constexpr int row_cta(int tpr) { return tpr == 32 ? 256 : tpr; }
-__host__ __device__ constexpr int row_ctas_per_sm(int tpr) { return tpr == 32 ? 5 : tpr == 128 ? 8 : tpr == 512 ? 2 : 1; }
+    X(8, 1) X(8, 2) X(8, 4) X(32, 2) X(32, 4) X(128, 2) X(128, 4) X(128, 8) X(512, 4) X(512, 8) X(1024, 8) X(1024, 0)
+__host__ __device__ constexpr int row_cta(int tpr) { return tpr <= 32 ? 256 : tpr; }
+__host__ __device__ constexpr int row_ctas_per_sm(int tpr) { return tpr <= 32 ? 5 : tpr == 128 ? 8 : tpr == 512 ? 2 : 1; }
+__host__ __device__ constexpr int rows_per_cta(int tpr) { return tpr <= 32 ? 256 / tpr : 1; }
 
 }  // namespace sl

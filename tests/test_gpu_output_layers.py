@@ -581,7 +581,42 @@ def test_reorder_offsets_beyond_32_bits():
     assert torch.equal(ho[0], h[0].view(B, K, H).flip(1).reshape(N, H)) and not ho[1:, :-K].any()
 
 
-# ------------------------------------------------------------------ refusals
+# ------------------------------------------------------------------ alignment, refusals
+def shifted(t):
+    """The same values 16 bytes into another allocation: on 16 bytes, not on 32."""
+    n = 16 // t.element_size()
+    flat = torch.empty(t.numel() + n, dtype=t.dtype, device=t.device)
+    flat[n:] = t.reshape(-1)
+    return flat[n:].view(t.shape)
+
+
+@TYPES
+@pytest.mark.parametrize("N", [200, 1024, 83])
+def test_tensors_on_16_bytes_give_the_same_bits(dt, N):
+    rng = np.random.default_rng(N)
+    R, k = 19, 5
+    x, z = rounded(rng, dt, R, N)[1], rounded(rng, dt, R, N)[1]
+    gamma, beta, dy = up(rng.normal(size=N)), up(rng.normal(size=N)), up(rng.normal(size=(R, N)))
+    idx, t, gold = up(rng.integers(0, N, (R, k)), torch.int32), up(rng.normal(size=(R, k))), up(rng.integers(0, N, R), torch.int32)
+    norm, lin, dist = (bd.stacklstm_norm_create(R, N, dt), bd.stacklstm_linear_create(R, N, 48, dt, bd.SL_ACT_SILU),
+                       bd.stacklstm_distill_create(R, N, k, dt))
+    W, dz, pre = rounded(rng, dt, 48, N)[1], up(rng.normal(size=(R, 48))), rounded(rng, dt, R, 48)[1]
+
+    def run(f):
+        o = [f(out(R, N, dtype=tdt(dt))), f(out(R)), f(out(R)), f(out(R, N)), f(out(N)), f(out(N)), f(out(R)), f(out(R, N)),
+             f(out(R, 48, dtype=tdt(dt))), f(out(R, N)), f(out(48, N)), f(out(48))]
+        bd.stacklstm_norm_forward(norm, f(x), f(gamma), f(beta), 1e-5, *o[:3])
+        bd.stacklstm_norm_backward(norm, f(dy), f(x), f(gamma), o[1], o[2], *o[3:6])
+        bd.stacklstm_distill_run(dist, f(z), f(idx), f(t), f(gold), 2.0, 0.5, 1.0, o[6], o[7])
+        bd.stacklstm_linear_forward(lin, f(x), f(W), None, None, o[8])
+        bd.stacklstm_linear_backward(lin, f(dz), f(x), f(W), f(pre), None, *o[9:])
+        torch.cuda.synchronize()
+        return o
+
+    for a, b in zip(run(lambda v: v), run(shifted)):
+        assert torch.equal(a, b)
+
+
 def test_arguments_are_checked():
     norm, lin = bd.stacklstm_norm_create(4, 8, FP), bd.stacklstm_linear_create(4, 8, 8, FP, bd.SL_ACT_RELU)
     x, y = torch.zeros(4, 8, device="cuda"), out(4, 8)
