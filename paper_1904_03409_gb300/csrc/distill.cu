@@ -6,13 +6,12 @@
 //   loss = scale [ alpha tau^2 sum_j q_j (ln q_j - ln p_{i_j}) + (1 - alpha) (-ln P_gold) ]
 //   dz_v = scale [ alpha tau (p_v - sum_{j: i_j = v} q_j) + (1 - alpha) (P_v - [v = gold]) ],
 // each term only where the row has a teacher (a gold class).
-// Bound by HBM: z is read once (into the registers of the row's threads, where the widths allow),
-// dz is written once. Both softmaxes share the maximum of z; the sums are fp32.
+// Bound by HBM: z is read from it once (and again from the caches where a row is wide), dz is
+// written once. Both softmaxes share the maximum of z; the sums are fp32.
 // The few classes of the teacher and the gold class are written once more after the row's dense
 // gradient: the first entry of each class takes the sum of the class's weights in entry order, so
 // that repeated classes need no atomics and the result does not depend on timing.
 #include "rowvec.cuh"
-#include "tc.cuh"
 
 namespace sl {
 namespace {
@@ -30,242 +29,316 @@ struct DistillArgs {
     int32_t *err;
 };
 
-// Threads TPR to a row (8 or 32 lanes: several rows a warp or CTA; else the whole CTA), NP pieces a
-// thread in registers, as they lie in memory (0: read again in each pass). A CTA takes rows
-// gridDim.x rows_per_cta apart; where a row is the CTA's, the pieces and the teacher's entries of
-// its next one are copied to shared memory while one is worked on, each by the thread that uses it
-// (4096 x 32003 bf16: 202 us without).
-// With l_j = (t_j - max t) / tau, w_j = exp(l_j) and x_v = z_v - max z, four sums are joined at
-// once: sum_j w_j, sum_j w_j (l_j - x_{i_j} / tau), sum_v exp(x_v / tau), sum_v exp(x_v).
-template <typename T, int TPR, int NP>
-__global__ void __launch_bounds__(row_cta(TPR), row_ctas_per_sm(TPR))
-distill_rows(const __grid_constant__ DistillArgs a)
+// With l_j = (t_j - max t) / tau, w_j = exp(l_j) and x_v = z_v - max z, a row needs four sums:
+// sum_j w_j, sum_j w_j (l_j - x_{i_j} / tau), sum_v exp(x_v / tau) and sum_v exp(x_v).
+
+// An entry's place in a row: its class (-1: none), teacher's logit (later its weight), its class's z.
+struct Entries {
+    int *c;
+    float *w, *z;
+};
+
+// Entry j of row r, checked.
+template <typename T>
+__device__ __forceinline__ float read_entry(const DistillArgs &a, const Entries &e, size_t r, const T *zr, int j)
 {
-    constexpr int E = RowVec<T>::E, RPC = rows_per_cta(TPR);
-    constexpr bool AHEAD = TPR > 32 && NP > 0;
-    __shared__ float sm[4 * 32];
-    extern __shared__ __align__(16) uint8_t dyn[];
-    const int sub = TPR <= 32 ? threadIdx.x / TPR : 0, t = threadIdx.x % TPR, k1 = a.k + 1;
-    uint4 *ahead = (uint4 *)dyn + threadIdx.x;  // piece j at ahead[j TPR]
-    uint8_t *dyn2 = dyn + (AHEAD ? (size_t)TPR * NP * 16 : 0);
-    int *ci = (int *)dyn2 + (size_t)sub * k1;                          // classes of the entries
-    float *cw = (float *)(dyn2 + (size_t)RPC * k1 * 4) + (size_t)sub * k1;  // their logits, then weights
-    float *cz = (float *)(dyn2 + (size_t)RPC * k1 * 8) + (size_t)sub * k1;  // z - max z of their classes
-    auto sync = [] {
-        if constexpr (TPR <= 32)
-            __syncwarp();
-        else
-            __syncthreads();
-    };
-    const T *z = (const T *)a.z;
-    const int step = gridDim.x * RPC;
-    const bool aligned = on_32(a.dz);
-    // the next row's pieces (whole ones) on their way, and its entry of this thread and gold class
-    int next_c = -1, next_gold = -1;
-    float next_l = 0.0f;
-    auto fetch = [&](int row_i) {
-        if constexpr (AHEAD) {
-            if (row_i < a.rows) {
-                const RowVec<T> row(row_i, a.V);
-                const int n = row.pieces();
+    int c = a.t_idx[r * a.k + j];
+    const float l = a.t_logit[r * a.k + j];
+    if (c < -1 || c >= a.V) {
+        atomicCAS(a.err, 0, (int)SL_ERR_ARG);  // the entry is skipped
+        c = -1;
+    }
+    if (l == -INFINITY) c = -1;
+    e.c[j] = c;
+    e.w[j] = l;
+    if (c < 0) return -INFINITY;
+    e.z[j] = to_f32(zr[c]);
+    return l;
+}
+// The gold class of row r, checked (lead: the thread that reports).
+__device__ __forceinline__ int read_gold(const DistillArgs &a, size_t r, bool lead)
+{
+    int gold = a.gold ? a.gold[r] : -1;
+    if (gold < -1 || gold >= a.V) {
+        if (lead) atomicCAS(a.err, 0, (int)SL_ERR_ARG);
+        gold = -1;
+    }
+    return gold;
+}
+// Entry j's share of the two sums over the entries; its logit becomes its weight before the sum's
+// division.
+__device__ __forceinline__ void add_entry(const Entries &e, int j, float top, float m, float rtau, float &s0, float &s1)
+{
+    if (e.c[j] < 0) return;
+    const float l = (e.w[j] - top) * rtau, w = expf(l);
+    s0 += w;
+    if (w > 0.0f)
+        s1 += w * (l - (e.z[j] - m) * rtau);  // (weight 0 on a class of -inf is 0)
+    else if (isnan(w))
+        s1 = w;
+    e.w[j] = w;
+}
+
+// What a row's outputs are made of.
+struct Row {
+    float m, wt, w1;   // gradient: wt exp((z - m) / tau) + w1 exp(z - m)
+    float ct, c1;      // the weights of the teacher's entries (over their sum) and of the gold class
+    bool soft, hard;
+    float k2;          // log2(e) / tau
+    __device__ __forceinline__ Row(const DistillArgs &a, float m_, float top, int gold) : m(m_), k2(kLog2e / a.tau)
+    {
+        const bool some = m > -INFINITY || isnan(m), taught = top > -INFINITY || isnan(top);
+        soft = some && taught && a.alpha > 0.0f;
+        hard = some && gold >= 0 && a.alpha < 1.0f;
+        ct = soft ? a.scale * a.alpha * a.tau : 0.0f;
+        c1 = hard ? a.scale * (1.0f - a.alpha) : 0.0f;
+    }
+    __device__ __forceinline__ void sums(const float (&s)[4])
+    {
+        wt = soft ? ct / s[2] : 0.0f;
+        w1 = hard ? c1 / s[3] : 0.0f;
+    }
+    __device__ __forceinline__ float grad(float z) const
+    {
+        const float d = z - m;
+        float g = 0.0f;
+        if (soft) g = wt * exp2_hw(d * k2);
+        if (hard) g = fmaf(w1, exp2_hw(d * kLog2e), g);
+        return g;
+    }
+    __device__ __forceinline__ float loss(const DistillArgs &a, const float (&s)[4], float zgold) const
+    {
+        float l = 0.0f;
+        if (soft) l = a.alpha * a.tau * a.tau * (s[1] / s[0] - logf(s[0]) + logf(s[2]));
+        if (hard) l += (1.0f - a.alpha) * (logf(s[3]) - (zgold - m));
+        return a.scale * l;
+    }
+    // the gradient of a piece
+    template <int E>
+    __device__ __forceinline__ void grads(const float (&v)[E], float (&g)[E]) const
+    {
+        if (soft && hard) {
 #pragma unroll
-                for (int j = 0; j < NP; ++j) {
-                    const int p = j * TPR + t;
-                    if (p < n && row.whole(p))
-                        tc::cp_async16(tc::smem_u32(ahead + j * TPR), z + row.at + (size_t)p * E, 16);
-                }
-                if (t < a.k) {
-                    next_c = a.t_idx[(size_t)row_i * a.k + t];
-                    next_l = a.t_logit[(size_t)row_i * a.k + t];
-                }
-                next_gold = a.gold ? a.gold[row_i] : -1;
+            for (int i = 0; i < E; ++i) {
+                const float d = v[i] - m;
+                g[i] = fmaf(w1, exp2_hw(d * kLog2e), wt * exp2_hw(d * k2));
             }
-            tc::cp_async_commit();
-        }
-    };
-    int r0 = blockIdx.x * RPC;
-    fetch(r0);
-    for (; r0 < a.rows; r0 += step) {
-        const int r = r0 + sub;
-        const bool here = r < a.rows;  // (lanes of a row past the end stay for the joins)
-        const RowVec<T> row(r, a.V);
-        const T *zr = z + row.first();
-        const int n = here ? row.pieces() : 0, k = here ? a.k : 0;
-        uint4 q[NP > 0 ? NP : 1];
-        if constexpr (AHEAD) tc::cp_async_wait<0>();
-        if constexpr (NP > 0) {
-#pragma unroll
-            for (int j = 0; j < NP; ++j) {
-                const int p = j * TPR + t;
-                if (p < n) q[j] = AHEAD && row.whole(p) ? ahead[j * TPR] : row.load(z, p);
-            }
-        }
-        // f(piece, its elements) over this thread's pieces
-        auto each = [&](auto f) {
-            if constexpr (NP > 0) {
-#pragma unroll
-                for (int j = 0; j < NP; ++j)
-                    if (j * TPR + t < n) {
-                        float v[E];
-                        unpack<T>(q[j], v);
-                        f(j * TPR + t, v);
-                    }
-            } else {
-                for (int p = t; p < n; p += TPR) {
-                    float v[E];
-                    unpack<T>(row.load(z, p), v);
-                    f(p, v);
-                }
-            }
-        };
-        float top[2] = {-INFINITY, -INFINITY};  // of z, of the teacher's logits
-        int gold = AHEAD ? next_gold : here && a.gold ? a.gold[r] : -1;
-        for (int j = t; j < k; j += TPR) {
-            int c = AHEAD && j == t ? next_c : a.t_idx[(size_t)r * a.k + j];
-            const float l = AHEAD && j == t ? next_l : a.t_logit[(size_t)r * a.k + j];
-            if (c < -1 || c >= a.V) {
-                atomicCAS(a.err, 0, (int)SL_ERR_ARG);  // the entry is skipped
-                c = -1;
-            }
-            if (l == -INFINITY) c = -1;
-            ci[j] = c;
-            cw[j] = l;
-            if (c >= 0) {
-                cz[j] = to_f32(zr[c]);
-                top[1] = max_nan(top[1], l);
-            }
-        }
-        if (gold < -1 || gold >= a.V) {
-            if (t == 0) atomicCAS(a.err, 0, (int)SL_ERR_ARG);
-            gold = -1;
-        }
-        const float zgold = t == 0 && gold >= 0 ? to_f32(zr[gold]) : 0.0f;  // (thread 0 uses it)
-        if constexpr (NP > 0) {
-#pragma unroll
-            for (int j = 0; j < NP; ++j)
-                if (j * TPR + t < n) top[0] = max_nan(top[0], piece_max<T, true>(q[j]));
         } else {
-            for (int p = t; p < n; p += TPR) top[0] = max_nan(top[0], piece_max<T, true>(row.load(z, p)));
-        }
-        row_join<true, TPR>(top, sm);
-        fetch(r0 + step);  // (after the join: every thread has its pieces and entry)
-        const float m = top[0], rtau = 1.0f / a.tau;
-        const bool some = m > -INFINITY || isnan(m);
-        const bool taught = top[1] > -INFINITY || isnan(top[1]);
-        const bool soft = some && taught && a.alpha > 0.0f, hard = some && a.alpha < 1.0f && gold >= 0;
-        const float k2 = kLog2e / a.tau;
-        float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (soft)
-            for (int j = t; j < k; j += TPR)
-                if (ci[j] >= 0) {
-                    const float l = (cw[j] - top[1]) * rtau, w = expf(l);
-                    s[0] += w;
-                    if (w > 0.0f)
-                        s[1] += w * (l - (cz[j] - m) * rtau);  // (weight 0 on a class of -inf is 0)
-                    else if (isnan(w))
-                        s[1] = w;
-                    cw[j] = w;
-                }
-        if (soft && hard)
-            each([&](int, const float (&v)[E]) {
-#pragma unroll
-                for (int i = 0; i < E; ++i) {
-                    const float d = v[i] - m;
-                    s[2] += exp2_hw(d * k2);
-                    s[3] += exp2_hw(d * kLog2e);
-                }
-            });
-        else if (soft || hard) {
-            const float kk = soft ? k2 : kLog2e;
-            float one = 0.0f;
-            each([&](int, const float (&v)[E]) {
-#pragma unroll
-                for (int i = 0; i < E; ++i) one += exp2_hw((v[i] - m) * kk);
-            });
-            s[2] = soft ? one : 0.0f;
-            s[3] = soft ? 0.0f : one;
-        }
-        row_join<false, TPR>(s, sm);
-        const float ct = soft ? a.scale * a.alpha * a.tau : 0.0f, c1 = hard ? a.scale * (1.0f - a.alpha) : 0.0f;
-        const float wt = soft ? ct / s[2] : 0.0f, w1 = hard ? c1 / s[3] : 0.0f;
-        if (t == 0 && here && a.loss) {
-            float loss = 0.0f;
-            if (soft) loss = a.alpha * a.tau * a.tau * (s[1] / s[0] - logf(s[0]) + logf(s[2]));
-            if (hard) loss += (1.0f - a.alpha) * (logf(s[3]) - (zgold - m));
-            a.loss[r] = a.scale * loss;
-        }
-        if (!a.dz) {
-            sync();  // the entries' arrays are the next row's
-            continue;
-        }
-        // the entries' weights in the gradient; entry k is the gold class (read by all after the sync)
-        for (int j = t; j < k; j += TPR)
-            if (ci[j] >= 0) {
-                if (soft)
-                    cw[j] = ct * (cw[j] / s[0]);
-                else
-                    ci[j] = -1;
-            }
-        if (t == 0) {
-            ci[a.k] = hard ? gold : -1;
-            cw[a.k] = c1;
-            cz[a.k] = zgold;
-        }
-        if (soft && hard)
-            each([&](int p, const float (&v)[E]) {
-                float g[E];
-#pragma unroll
-                for (int i = 0; i < E; ++i) {
-                    const float d = v[i] - m;
-                    g[i] = fmaf(w1, exp2_hw(d * kLog2e), wt * exp2_hw(d * k2));
-                }
-                row.store_f32(a.dz, aligned, p, g);
-            });
-        else {
             const float kk = soft ? k2 : kLog2e, w = soft ? wt : w1;
-            const bool any = soft || hard;
-            each([&](int p, const float (&v)[E]) {
-                float g[E];
 #pragma unroll
-                for (int i = 0; i < E; ++i) g[i] = any ? w * exp2_hw((v[i] - m) * kk) : 0.0f;
-                row.store_f32(a.dz, aligned, p, g);
-            });
+            for (int i = 0; i < E; ++i) g[i] = soft || hard ? w * exp2_hw((v[i] - m) * kk) : 0.0f;
         }
-        sync();
-        if (here)
-            for (int j = t; j <= a.k; j += TPR) {
-                const int c = ci[j];
-                if (c < 0) continue;
-                bool first = true;
-                float w = cw[j];
-                for (int i = 0; i <= a.k; ++i)
-                    if (ci[i] == c) {
-                        if (i < j) first = false;
-                        if (i > j) w += cw[i];
-                    }
-                if (!first) continue;
-                const float d = cz[j] - m;
-                float g = 0.0f;
-                if (soft) g = wt * exp2_hw(d * k2);
-                if (hard) g = fmaf(w1, exp2_hw(d * kLog2e), g);
-                a.dz[row.first() + c] = g - w;
+    }
+    // entry j's weight in the gradient, or that it has none
+    __device__ __forceinline__ void weigh(const Entries &e, int j, float s0) const
+    {
+        if (e.c[j] < 0) return;
+        if (soft)
+            e.w[j] = ct * (e.w[j] / s0);
+        else
+            e.c[j] = -1;
+    }
+    // entry k: the gold class
+    __device__ __forceinline__ void gold_entry(const Entries &e, int k, int gold, float zgold) const
+    {
+        e.c[k] = hard ? gold : -1;
+        e.w[k] = c1;
+        e.z[k] = zgold;
+    }
+};
+
+// Rows of up to 4 pieces a lane: TPR lanes (8 or 32) to a row, NP pieces a lane in registers, as
+// they lie in memory.
+template <typename T, int TPR, int NP>
+__global__ void __launch_bounds__(256, 5)
+distill_narrow(const __grid_constant__ DistillArgs a)
+{
+    constexpr int E = RowVec<T>::E, RPC = 256 / TPR;
+    extern __shared__ __align__(16) uint8_t dyn[];
+    const int sub = threadIdx.x / TPR, t = threadIdx.x % TPR, k1 = a.k + 1;
+    const Entries e = {(int *)dyn + (size_t)sub * k1, (float *)(dyn + (size_t)RPC * k1 * 4) + (size_t)sub * k1,
+                       (float *)(dyn + (size_t)RPC * k1 * 8) + (size_t)sub * k1};
+    const size_t r = (size_t)blockIdx.x * RPC + sub;
+    const bool here = r < (size_t)a.rows;  // (lanes of a row past the end stay for the joins)
+    const T *z = (const T *)a.z;
+    const RowVec<T> row(r, a.V);
+    const T *zr = z + row.first();
+    const int n = here ? row.pieces() : 0, k = here ? a.k : 0;
+    uint4 q[NP];
+#pragma unroll
+    for (int j = 0; j < NP; ++j)
+        if (j * TPR + t < n) q[j] = row.load(z, j * TPR + t);
+    auto each = [&](auto f) {  // f(piece, its elements) over this lane's pieces
+#pragma unroll
+        for (int j = 0; j < NP; ++j)
+            if (j * TPR + t < n) {
+                float v[E];
+                unpack<T>(q[j], v);
+                f(j * TPR + t, v);
             }
-        sync();  // the entries' arrays are the next row's
+    };
+    float top[2] = {-INFINITY, -INFINITY};  // of z, of the teacher's logits
+    for (int j = t; j < k; j += TPR) top[1] = max_nan(top[1], read_entry(a, e, r, zr, j));
+    const int gold = here ? read_gold(a, r, t == 0) : -1;
+    const float zgold = t == 0 && gold >= 0 ? to_f32(zr[gold]) : 0.0f;  // (lane 0 uses it)
+#pragma unroll
+    for (int j = 0; j < NP; ++j)
+        if (j * TPR + t < n) top[0] = max_nan(top[0], piece_max<T, true>(q[j]));
+    lanes_join<true, TPR>(top);
+    Row w(a, top[0], top[1], gold);
+    const float rtau = 1.0f / a.tau;
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (w.soft)
+        for (int j = t; j < k; j += TPR) add_entry(e, j, top[1], w.m, rtau, s[0], s[1]);
+    if (w.soft || w.hard)
+        each([&](int, const float (&v)[E]) {
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const float d = v[i] - w.m;
+                if (w.soft) s[2] += exp2_hw(d * w.k2);
+                if (w.hard) s[3] += exp2_hw(d * kLog2e);
+            }
+        });
+    lanes_join<false, TPR>(s);
+    w.sums(s);
+    if (t == 0 && here && a.loss) a.loss[r] = w.loss(a, s, zgold);
+    if (!a.dz) return;
+    const bool aligned = on_32(a.dz);
+    for (int j = t; j < k; j += TPR) w.weigh(e, j, s[0]);
+    if (t == 0) w.gold_entry(e, a.k, gold, zgold);
+    each([&](int p, const float (&v)[E]) {
+        float g[E];
+        w.grads(v, g);
+        row.store_f32(a.dz, aligned, p, g);
+    });
+    __syncwarp();  // the row's gradient, and its entries
+    if (!here) return;
+    for (int j = t; j <= a.k; j += TPR) {
+        const int c = e.c[j];
+        if (c < 0) continue;
+        bool first = true;
+        float wj = e.w[j];
+        for (int i = 0; i <= a.k; ++i)
+            if (e.c[i] == c) {
+                if (i < j) first = false;
+                if (i > j) wj += e.w[i];
+            }
+        if (first) a.dz[row.first() + c] = w.grad(e.z[j]) - wj;
     }
 }
 
-template <typename T, int TPR, int NP>
-cudaError_t launch_rows(const stacklstm_op *op, const DistillArgs &a)
+// Wider rows: a CTA of TPR threads a row, the row read twice, the second time from the caches. A
+// thread keeps its own maximum and the sums against it, so that the first reading is one pass; 1536
+// threads an SM hide one another's latencies. At 4096 x 32003 bf16: 159 us with 512 threads a row
+// (5.0 TB/s), 164 with 256, 186 with 128; 182 with the row held in the registers of 512 threads, two
+// CTAs an SM, and no less with the next row on its way to shared memory: the barriers and the
+// entries' part of each row were not hidden.
+template <typename T, int TPR>
+__global__ void __launch_bounds__(TPR, 1536 / TPR)
+distill_wide(const __grid_constant__ DistillArgs a)
 {
-    constexpr int RPC = rows_per_cta(TPR);
-    const size_t smem = (TPR > 32 ? (size_t)TPR * NP * 16 : 0) + (size_t)RPC * (a.k + 1) * 12;
-    if (smem > 48 * 1024)
-        if (cudaError_t e = smem_at_least((const void *)distill_rows<T, TPR, NP>, smem)) return e;
-    // a CTA a row group, or as many CTAs as run at once where they read ahead
-    const size_t groups = ceil_div(a.rows, RPC);
-    const unsigned grid = (unsigned)(TPR > 32 && NP > 0 ? std::min(groups, (size_t)op->num_sms * row_ctas_per_sm(TPR)) : groups);
-    distill_rows<T, TPR, NP><<<grid, row_cta(TPR), smem, op->stream>>>(a);
-    return cudaGetLastError();
+    constexpr int E = RowVec<T>::E, NW = TPR / 32;
+    __shared__ float sm_max[2 * 32], sm_sum[4 * 32];
+    __shared__ int ec[kMaxTeacher + 1];
+    __shared__ float ew[kMaxTeacher + 1], ez[kMaxTeacher + 1];
+    const Entries e = {ec, ew, ez};
+    const int t = threadIdx.x, lane = t & 31;
+    const size_t r = blockIdx.x;
+    const T *z = (const T *)a.z;
+    const RowVec<T> row(r, a.V);
+    const T *zr = z + row.first();
+    const int n = row.pieces();
+    const float k2 = kLog2e / a.tau;
+    const bool want2 = a.alpha > 0.0f, want1 = a.alpha < 1.0f;
+    float top[2] = {-INFINITY, -INFINITY};
+    for (int j = t; j < a.k; j += TPR) top[1] = max_nan(top[1], read_entry(a, e, r, zr, j));
+    const int gold = read_gold(a, r, t == 0);
+    const float zgold = t == 0 && gold >= 0 ? to_f32(zr[gold]) : 0.0f;
+    // the first pass, four pieces in flight; m: this thread's maximum, s2 and s1 against it
+    float m = -INFINITY, s2 = 0.0f, s1 = 0.0f;
+    auto add = [&](const uint4 &q) {
+        const float pm = piece_max<T, true>(q);
+        if (!(pm <= m)) {  // a new maximum (or NaN)
+            const float d = m - pm;  // (-inf at first: the sums are 0)
+            s2 *= exp2_hw(d * k2);
+            s1 *= exp2_hw(d * kLog2e);
+            m = pm;
+        }
+        if (m == -INFINITY) return;  // nothing yet
+        float v[E];
+        unpack<T>(q, v);
+        if (want2 && want1) {
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const float d = v[i] - m;
+                s2 += exp2_hw(d * k2);
+                s1 += exp2_hw(d * kLog2e);
+            }
+        } else {
+            const float kk = want2 ? k2 : kLog2e;
+            float s = 0.0f;
+#pragma unroll
+            for (int i = 0; i < E; ++i) s += exp2_hw((v[i] - m) * kk);
+            if (want2) s2 += s;
+            else s1 += s;
+        }
+    };
+    for (int p = t; p < n; p += 4 * TPR) {
+        uint4 q[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (p + u * TPR < n) q[u] = row.load(z, p + u * TPR);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (p + u * TPR < n) add(q[u]);
+    }
+    top[0] = m;
+    row_join<true, TPR, true>(top, sm_max);
+    Row w(a, top[0], top[1], gold);
+    const float rtau = 1.0f / a.tau;
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (m > -INFINITY || isnan(m)) {  // this thread's sums against the row's maximum
+        s[2] = s2 * exp2_hw((m - w.m) * k2);
+        s[3] = s1 * exp2_hw((m - w.m) * kLog2e);
+    }
+    if (w.soft)
+        for (int j = t; j < a.k; j += TPR) add_entry(e, j, top[1], w.m, rtau, s[0], s[1]);
+    row_join<false, TPR, true>(s, sm_sum);
+    w.sums(s);
+    if (t == 0 && a.loss) a.loss[r] = w.loss(a, s, zgold);
+    if (!a.dz) return;
+    const bool aligned = on_32(a.dz);
+    for (int j = t; j < a.k; j += TPR) w.weigh(e, j, s[0]);
+    if (t == 0) w.gold_entry(e, a.k, gold, zgold);
+    for (int p = t; p < n; p += 2 * TPR) {
+        uint4 q[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+            if (p + u * TPR < n) q[u] = row.load(z, p + u * TPR);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+            if (p + u * TPR < n) {
+                float v[E], g[E];
+                unpack<T>(q[u], v);
+                w.grads(v, g);
+                row.store_f32(a.dz, aligned, p + u * TPR, g);
+            }
+    }
+    __syncthreads();  // the row's gradient, and its entries
+    for (int j = t / 32; j <= a.k; j += NW) {  // a warp an entry
+        const int c = e.c[j];
+        if (c < 0) continue;
+        bool earlier = false;
+        float wj = 0.0f;
+        for (int i = lane; i <= a.k; i += 32)
+            if (e.c[i] == c) {
+                earlier = earlier || i < j;
+                wj += e.w[i];
+            }
+        if (__any_sync(0xffffffffu, earlier)) continue;
+        wj = warp_sum(wj);
+        if (lane == 0) a.dz[row.first() + c] = w.grad(e.z[j]) - wj;
+    }
 }
 
 template <typename T>
@@ -273,11 +346,23 @@ cudaError_t launch_distill(const stacklstm_op *op, const DistillArgs &a)
 {
     int tpr, np;
     row_plan<T>(a.V, &tpr, &np);
-#define SL_DIST(t, n) \
-    if (tpr == t && np == n) return launch_rows<T, t, n>(op, a);
-    SL_ROW_PLANS(SL_DIST)
-#undef SL_DIST
-    return cudaErrorInvalidValue;  // not reached
+    if (tpr <= 32) {
+        const unsigned grid = ceil_div(a.rows, 256 / tpr);
+        const size_t smem = (size_t)(256 / tpr) * (a.k + 1) * 12;  // (at most 99 KB)
+        auto launch = [&](auto kernel) {
+            if (smem > 48 * 1024)
+                if (cudaError_t e = smem_at_least((const void *)kernel, smem)) return e;
+            kernel<<<grid, 256, smem, op->stream>>>(a);
+            return cudaGetLastError();
+        };
+        return tpr == 8 ? launch(np == 1 ? distill_narrow<T, 8, 1> : np == 2 ? distill_narrow<T, 8, 2> : distill_narrow<T, 8, 4>)
+                        : launch(np <= 2 ? distill_narrow<T, 32, 2> : distill_narrow<T, 32, 4>);
+    }
+    if (tpr == 128)
+        distill_wide<T, 128><<<a.rows, 128, 0, op->stream>>>(a);
+    else
+        distill_wide<T, 512><<<a.rows, 512, 0, op->stream>>>(a);
+    return cudaGetLastError();
 }
 
 }  // namespace

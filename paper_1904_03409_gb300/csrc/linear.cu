@@ -14,7 +14,8 @@
 //   forward  A = x   [R][K] K-major    B = W  [N][K] K-major     (few rows: A = W, B = x)
 //   dx       A = dz  [R][N] K-major    B = W  [N][K] MN-major
 //   dW       A = dz  [R][N] MN-major   B = x  [R][K] MN-major
-// dz is written once, as three bf16 parts, with the column sums of dbias.
+// dz is written once, as three bf16 parts, with the column sums of dbias, in the launch that also
+// makes the parts of an fp32 x and W.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -73,42 +74,108 @@ __device__ __forceinline__ void split3(float v, __nv_bfloat16 (&p)[3])
     p[2] = finite ? __float2bfloat16(r1 - __bfloat162float(p[1])) : __float2bfloat16(0.0f);
 }
 
-// out [parts][rows][ld] from src [rows][cols]: the parts of fp32 numbers, or (bf16) a copy whose
-// rows start on 16 bytes.
+// What a call makes of its tensors before the contractions, in one launch: x and W as parts (or, bf16
+// whose rows do not start on 16 bytes, as a copy whose rows do), and dz = dy act'(pre) as parts with
+// its column sums. Each is a range of CTAs.
+struct Pack {
+    const void *src;        // [rows][cols], or null
+    __nv_bfloat16 *out;     // [parts][rows][ld]
+    size_t rows;
+    int cols, ld;
+    unsigned ctas;
+};
+struct Dz {
+    const float *dy;
+    const void *pre;
+    __nv_bfloat16 *out;     // [3][rows][ld], or null
+    float *part;            // [row blocks][N] column sums, or null
+    float *dbias;
+    int *arrived;           // [column blocks], 0 between calls
+    int rows, N, ld, act;
+    unsigned row_blocks, ctas;
+};
+struct Prepare {
+    Pack x, w;
+    Dz dz;
+};
+
+constexpr int kPackItems = 4;  // groups of four columns a thread
+constexpr int kDzCols = 128, kDzRows = 64, kDzSub = 8;
+
+// Groups of four columns, 8 bytes a part. (The groups of `out` follow one another whatever the rows'
+// length is; those of src do where its rows are as long.)
 template <typename T>
-__global__ void __launch_bounds__(256)
-pack_parts(size_t rows, int cols, int ld, const T *__restrict__ src, __nv_bfloat16 *__restrict__ out)
+__device__ __forceinline__ void pack_block(const Pack &a, unsigned cta)
 {
-    const size_t n = rows * cols, plane = rows * ld;
-    for (size_t e = blockIdx.x * (size_t)256 + threadIdx.x; e < n; e += (size_t)gridDim.x * 256) {
-        const size_t r = e / cols, c = e - r * cols, o = r * ld + c;
-        if constexpr (sizeof(T) == 4) {
-            __nv_bfloat16 p[3];
-            split3(src[e], p);
+    const size_t per = (size_t)a.ld / 4, groups = a.rows * per, plane = a.rows * a.ld;
+    const bool flat = a.cols == a.ld, quads = a.cols % 4 == 0;
+    const T *src = (const T *)a.src;
+    float v[kPackItems][4];
+    T raw[kPackItems][4];
 #pragma unroll
-            for (int i = 0; i < 3; ++i) out[i * plane + o] = p[i];
+    for (int u = 0; u < kPackItems; ++u) {
+        const size_t g = (size_t)cta * (256 * kPackItems) + u * 256 + threadIdx.x;
+        if (g >= groups) break;
+        const size_t r = flat ? 0 : g / per;
+        const int c = flat ? 0 : (int)(g - r * per) * 4;
+        const T *p = flat ? src + g * 4 : src + r * a.cols + c;
+        const int n = flat ? 4 : a.cols - c;  // columns left (the last groups of a row may be past them)
+        if constexpr (sizeof(T) == 4) {
+            if (quads && n >= 4) {
+                const float4 q = *(const float4 *)p;
+                v[u][0] = q.x; v[u][1] = q.y; v[u][2] = q.z; v[u][3] = q.w;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[u][j] = j < n ? p[j] : 0.0f;
+            }
         } else {
-            out[o] = src[e];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) raw[u][j] = j < n ? p[j] : from_f32<T>(0.0f);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kPackItems; ++u) {
+        const size_t g = (size_t)cta * (256 * kPackItems) + u * 256 + threadIdx.x;
+        if (g >= groups) break;
+        union {
+            __nv_bfloat16 b[4];
+            uint2 q;
+        } o[3];
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                __nv_bfloat16 p[3];
+                split3(v[u][j], p);
+#pragma unroll
+                for (int k = 0; k < 3; ++k) o[k].b[j] = p[k];
+            }
+#pragma unroll
+            for (int k = 0; k < 3; ++k) *(uint2 *)(a.out + k * plane + g * 4) = o[k].q;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[0].b[j] = raw[u][j];
+            *(uint2 *)(a.out + g * 4) = o[0].q;
         }
     }
 }
 
-constexpr int kDzCols = 128, kDzRows = 64, kDzSub = 8;
-
-// dz = dy act'(pre) as three parts [3][rows][ld], and this CTA's column sums of it over its rows,
-// part [row blocks][N]. A lane takes four columns (one 8-byte store a part, from one 16-byte read
-// where the rows of dy start on 16 bytes), warp w the rows w, w + 8, ... of the block, four at a
-// time; the eight warps' sums are added in order. HBM-bound: 4 + 6 bytes an element.
-template <typename T, bool ALIGNED>
-__global__ void __launch_bounds__(32 * kDzSub)
-dz_parts(int rows, int N, int ld, int act, const float *__restrict__ dy, const T *__restrict__ pre,
-         __nv_bfloat16 *__restrict__ out, float *__restrict__ part)
+// dz of kDzRows rows and kDzCols columns, and the column sums of it. A lane takes four columns (one
+// 8-byte store a part, from one 16-byte read where the rows of dy start on 16 bytes), warp w the
+// rows w, w + 8, ... of the block, four at a time; the eight warps' sums are added in order, and the
+// last block of a column block to end adds the blocks' sums: parts w, w + 8, ... by warp w, then the
+// eight in order. HBM-bound: 4 + 6 bytes an element.
+template <typename T>
+__device__ __forceinline__ void dz_block(const Dz &a, unsigned cta)
 {
     __shared__ float4 sm[kDzSub][32];
-    const int lane = threadIdx.x & 31, sub = threadIdx.x >> 5;
-    const int c = blockIdx.y * kDzCols + lane * 4, nc = min(4, N - c);
-    const int r0 = blockIdx.x * kDzRows, r1 = min(rows, r0 + kDzRows);
-    const size_t plane = (size_t)rows * ld;
+    __shared__ int last;
+    const int lane = threadIdx.x & 31, sub = threadIdx.x >> 5, N = a.N;
+    const unsigned rb = cta % a.row_blocks, cb = cta / a.row_blocks;
+    const int c = (int)cb * kDzCols + lane * 4, nc = min(4, N - c);
+    const int r0 = (int)rb * kDzRows, r1 = min(a.rows, r0 + kDzRows);
+    const size_t plane = (size_t)a.rows * a.ld;
+    const bool quads = N % 4 == 0;
+    const T *pre = (const T *)a.pre;
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (nc > 0) {
         for (int r = r0 + sub; r < r1; r += 4 * kDzSub) {
@@ -117,15 +184,15 @@ dz_parts(int rows, int N, int ld, int act, const float *__restrict__ dy, const T
             for (int i = 0; i < 4; ++i) {
                 const int ri = r + i * kDzSub;
                 const size_t at = (size_t)ri * N + c;
-                if constexpr (ALIGNED) {
-                    const float4 q = ri < r1 ? *(const float4 *)(dy + at) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (quads) {
+                    const float4 q = ri < r1 ? *(const float4 *)(a.dy + at) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                     v[i][0] = q.x; v[i][1] = q.y; v[i][2] = q.z; v[i][3] = q.w;
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) v[i][j] = ri < r1 && j < nc ? dy[at + j] : 0.0f;
+                    for (int j = 0; j < 4; ++j) v[i][j] = ri < r1 && j < nc ? a.dy[at + j] : 0.0f;
                 }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) z[i][j] = act != kActNone && ri < r1 && j < nc ? to_f32(pre[at + j]) : 0.0f;
+                for (int j = 0; j < 4; ++j) z[i][j] = a.act != kActNone && ri < r1 && j < nc ? to_f32(pre[at + j]) : 0.0f;
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -137,56 +204,68 @@ dz_parts(int rows, int N, int ld, int act, const float *__restrict__ dy, const T
                 } o[3];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float w = act != kActNone ? __fmul_rn(v[i][j], act_grad(z[i][j], act)) : v[i][j];  // (not fused with the sum)
+                    const float w = a.act != kActNone ? __fmul_rn(v[i][j], act_grad(z[i][j], a.act)) : v[i][j];  // (not fused with the sum)
                     sum[j] += w;
                     __nv_bfloat16 p[3];
                     split3(w, p);
 #pragma unroll
                     for (int k = 0; k < 3; ++k) o[k].b[j] = p[k];
                 }
-                if (out)  // (a row has room for whole groups of eight: what is past N is never read)
+                if (a.out)  // (a row has room for whole groups of eight: what is past N is never read)
 #pragma unroll
-                    for (int k = 0; k < 3; ++k) *(uint2 *)(out + k * plane + (size_t)ri * ld + c) = o[k].q;
+                    for (int k = 0; k < 3; ++k) *(uint2 *)(a.out + k * plane + (size_t)ri * a.ld + c) = o[k].q;
             }
         }
     }
-    if (!part) return;
-    sm[sub][lane] = make_float4(sum[0], sum[1], sum[2], sum[3]);
-    __syncthreads();
-    if (sub == 0 && nc > 0) {
+    if (!a.part) return;
+    auto eight = [&](const float4 &mine) {  // the warps' sums in order, to warp 0
+        sm[sub][lane] = mine;
+        __syncthreads();
         float4 t = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (sub == 0)
 #pragma unroll
-        for (int i = 0; i < kDzSub; ++i) {
-            const float4 q = sm[i][lane];
-            t.x += q.x; t.y += q.y; t.z += q.z; t.w += q.w;
-        }
+            for (int i = 0; i < kDzSub; ++i) {
+                const float4 q = sm[i][lane];
+                t.x += q.x; t.y += q.y; t.z += q.z; t.w += q.w;
+            }
+        return t;
+    };
+    auto put = [&](float *to, const float4 &t) {
         const float w[4] = {t.x, t.y, t.z, t.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            if (j < nc) part[(size_t)blockIdx.x * N + c + j] = w[j];
+            if (j < nc) to[j] = w[j];
+    };
+    float4 t = eight(make_float4(sum[0], sum[1], sum[2], sum[3]));
+    if (sub == 0) {
+        put(a.part + (size_t)rb * N + c, t);
+        __threadfence();
+        __syncwarp();
+        if (lane == 0) last = atomicAdd(&a.arrived[cb], 1) == (int)a.row_blocks - 1;
     }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    if (threadIdx.x == 0) a.arrived[cb] = 0;  // for the next call
+    float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (unsigned s = sub; s < a.row_blocks; s += kDzSub)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < nc) acc[j] += __ldcg(a.part + (size_t)s * N + c + j);
+    t = eight(make_float4(acc[0], acc[1], acc[2], acc[3]));
+    if (sub == 0) put(a.dbias + c, t);
 }
 
-// out[c] = the sum over s of part[s][c]: warp w adds parts w, w + 8, ..., then the eight in order.
+template <typename T>
 __global__ void __launch_bounds__(256)
-sum_parts(const float *__restrict__ part, int n, int N, float *__restrict__ out)
+prepare(const __grid_constant__ Prepare a)
 {
-    __shared__ float sm[8][32];
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    const size_t c = blockIdx.x * (size_t)32 + lane;
-    float acc = 0.0f;
-    if (c < (size_t)N) {
-#pragma unroll 8
-        for (int s = w; s < n; s += 8) acc += part[(size_t)s * N + c];
-    }
-    sm[w][lane] = acc;
-    __syncthreads();
-    if (w == 0 && c < (size_t)N) {
-        float v = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v += sm[i][lane];
-        out[c] = v;
-    }
+    unsigned cta = blockIdx.x;
+    if (cta < a.dz.ctas) return dz_block<T>(a.dz, cta);
+    cta -= a.dz.ctas;
+    if (cta < a.x.ctas) return pack_block<T>(a.x, cta);
+    pack_block<T>(a.w, cta - a.x.ctas);
 }
 
 // ------------------------------------------------------------------ the contraction
@@ -272,8 +351,6 @@ struct Plain {
 };
 
 // Two neighbours in one access.
-__device__ __forceinline__ float2 load2(const float *p) { return *(const float2 *)p; }
-__device__ __forceinline__ float2 load2(const __nv_bfloat16 *p) { return __bfloat1622float2(*(const __nv_bfloat162 *)p); }
 __device__ __forceinline__ void store2(float *p, float x, float y) { *(float2 *)p = make_float2(x, y); }
 __device__ __forceinline__ void store2(__nv_bfloat16 *p, float x, float y) { *(__nv_bfloat162 *)p = __floats2bfloat162_rn(x, y); }
 
@@ -324,10 +401,10 @@ __device__ __forceinline__ void put_cols(const Out &o, const float *stage, int l
 
 // A warp's 32 rows x 32 NSEG columns of an output with an even number of columns: two neighbours a
 // lane, two rows at a time; stage_in(seg) brings 32 columns of sums into `stage`. What is added to
-// a block of 32 columns (residual, add) is read while the block before it is worked on, and rows
-// are finished four at a time (more of them keep more activations in flight than there are
-// registers).
-template <typename T, bool FORWARD, int ACT, int NSEG, typename StageIn>
+// a block of 32 columns (residual, add) is read while the block before it is worked on (AHEAD: where
+// few warps share an SM) or while its sums come in, and rows are finished four at a time (more of
+// them keep more activations in flight than there are registers).
+template <typename T, bool FORWARD, int ACT, int NSEG, bool AHEAD, typename StageIn>
 __device__ __forceinline__ void put_pairs(const StageIn &stage_in, const float *stage, int lane, int r0, int n0, int rows,
                                           int cols, const float *bias_p, const T *extra_p, T *y, T *pre)
 {
@@ -341,12 +418,13 @@ __device__ __forceinline__ void put_pairs(const StageIn &stage_in, const float *
             for (int i = 0; i < 16; ++i)
                 if (half + 2 * i < m) next[i] = *(const Two *)(extra_p + first + seg * 32 + i * step);
     };
-    if (extra_p) fetch(0);
+    if (AHEAD && extra_p) fetch(0);
 #pragma unroll 1
     for (int seg = 0; seg < NSEG; ++seg) {
+        if (!AHEAD && extra_p) fetch(seg);
 #pragma unroll
         for (int i = 0; i < 16; ++i) extra[i] = next[i];
-        if (extra_p && seg + 1 < NSEG) fetch(seg + 1);
+        if (AHEAD && extra_p && seg + 1 < NSEG) fetch(seg + 1);
         const int n = n0 + seg * 32 + j;
         float2 bias = make_float2(0.0f, 0.0f);
         if (FORWARD && bias_p && n < cols) bias = *(const float2 *)(bias_p + n);
@@ -376,22 +454,22 @@ __device__ __forceinline__ void put_pairs(const StageIn &stage_in, const float *
         __syncwarp();
     }
 }
-template <typename T, int NSEG, typename StageIn>
+template <typename T, int NSEG, bool AHEAD, typename StageIn>
 __device__ __forceinline__ void put_pairs_forward(const StageIn &in, const Epilogue &ep, const float *stage, int lane, int r0, int n0)
 {
     const T *res = (const T *)ep.residual;
     T *y = (T *)ep.y, *pre = (T *)ep.pre;
     switch (ep.act) {
-    case kActRelu: put_pairs<T, true, kActRelu, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre); break;
-    case kActTanh: put_pairs<T, true, kActTanh, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre); break;
-    case kActGelu: put_pairs<T, true, kActGelu, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre); break;
-    case kActSilu: put_pairs<T, true, kActSilu, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre); break;
-    default: put_pairs<T, true, kActNone, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
+    case kActRelu: put_pairs<T, true, kActRelu, NSEG, AHEAD>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre); break;
+    case kActTanh: put_pairs<T, true, kActTanh, NSEG, AHEAD>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre); break;
+    case kActGelu: put_pairs<T, true, kActGelu, NSEG, AHEAD>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre); break;
+    case kActSilu: put_pairs<T, true, kActSilu, NSEG, AHEAD>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre); break;
+    default: put_pairs<T, true, kActNone, NSEG, AHEAD>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
     }
 }
 
 // A warp's 32 rows x SEG NSEG columns of sums to the output.
-template <int SEG, int NSEG, bool GRADIENT, typename StageIn>
+template <int SEG, int NSEG, bool GRADIENT, bool AHEAD, typename StageIn>
 __device__ __forceinline__ void put_tile(const StageIn &in, const Epilogue &ep, bool swapped, int sp, const float *stage,
                                          int lane, int m0, int n0)
 {
@@ -399,12 +477,12 @@ __device__ __forceinline__ void put_tile(const StageIn &in, const Epilogue &ep, 
     const Plain p = {ep.part ? nullptr : ep.add, ep.part ? ep.part + (size_t)sp * ep.rows * ep.cols : ep.out};
     if (SEG == 32 && ep.cols % 2 == 0 && (GRADIENT || !swapped)) {
         if (plain)
-            put_pairs<float, false, kActNone, NSEG>(in, stage, lane, m0, n0, ep.rows, ep.cols, nullptr, p.add, p.out, nullptr);
+            put_pairs<float, false, kActNone, NSEG, AHEAD>(in, stage, lane, m0, n0, ep.rows, ep.cols, nullptr, p.add, p.out, nullptr);
         else if constexpr (!GRADIENT) {
             if (ep.bf16_out)
-                put_pairs_forward<__nv_bfloat16, NSEG>(in, ep, stage, lane, m0, n0);
+                put_pairs_forward<__nv_bfloat16, NSEG, AHEAD>(in, ep, stage, lane, m0, n0);
             else
-                put_pairs_forward<float, NSEG>(in, ep, stage, lane, m0, n0);
+                put_pairs_forward<float, NSEG, AHEAD>(in, ep, stage, lane, m0, n0);
         }
         return;
     }
@@ -433,19 +511,20 @@ __device__ __forceinline__ void put_tile(const StageIn &in, const Epilogue &ep, 
     }
 }
 
-// Three warpgroups: warp 0 for TMA, warp 1 for the MMAs (2 and 3 idle), warps 4-11 for the sums and
-// outputs. They are launched with 168 registers a thread (384 x 168 = 64512); the first group
-// keeps 56 of them and the others take 224 (128 x 56 + 256 x 224 = 64512), so that 128 sums and a
-// batch of reads stay in registers.
-constexpr int kEpiWarps = 8;
-constexpr int kGemmThreads = (kEpiWarps + 4) * 32;
-static_assert(128 * 56 + kEpiWarps * 32 * 224 <= kGemmThreads * 168, "registers of a CTA");
+// Warp 0 for TMA, warp 1 for the MMAs (2 and 3 idle), then the warps for the sums and outputs: eight
+// where they add accumulators up (launched with 168 registers a thread, 384 x 168 = 64512, of which
+// the first group keeps 56 and the others take 224, 128 x 56 + 256 x 224 = 64512, so that 128 sums
+// and a batch of reads stay in registers), else sixteen, whose activations hide one another's
+// latencies (96 registers a thread, 640 x 96 = 61440, split as 128 x 32 + 512 x 112 = 61440).
+constexpr int gemm_epi_warps(int bn, bool sums) { return !sums && bn >= 128 ? 16 : 8; }
+constexpr int gemm_threads(int epi) { return (epi + 4) * 32; }
+static_assert(128 * 56 + 8 * 32 * 224 <= gemm_threads(8) * 168 && 128 * 32 + 16 * 32 * 112 <= gemm_threads(16) * 96,
+              "registers of a CTA");
 constexpr int kMaxRing = 16;
 constexpr uint32_t kTileA = 128 * 128;  // 128 rows (or 2 x 64 columns) x 64 of the contraction
-constexpr uint32_t kStageBytes = kEpiWarps * 32 * 32 * 4;
-constexpr uint32_t kRingBytes = 192 * 1024;
+constexpr uint32_t gemm_ring(int epi) { return 224 * 1024 - epi * 4096; }  // bytes: 4 KB a warp to stage outputs
 constexpr uint32_t kGemmBars = (4 * kMaxRing + 5) * 8 + 16;
-constexpr uint32_t kGemmSmem = 1024 + kRingBytes + kStageBytes + kGemmBars;
+constexpr uint32_t kGemmSmem = 1024 + 224 * 1024 + kGemmBars;
 static_assert(kGemmSmem <= 227 * 1024, "shared memory of a CTA");
 constexpr int kGroupM = 16;             // m tiles that share their B tiles in L2
 constexpr long long kDrain = 4000000000LL;  // clock cycles: waits for a CTA's own copies and MMAs before it ends
@@ -470,14 +549,15 @@ __device__ __forceinline__ void prefetch_map(const void *tmap)
 // that fp32 results come from takes few of them (1.7e-8 of the result each: 1e-4 after 6012).
 // A part is loaded once a chunk, whatever number of products it is in, small products first.
 // MN-major operands: blocks of 64 columns, each 64 rows of 128 bytes.
-template <int BN, bool A_MN, bool B_MN, int PA, int PB>
-__global__ void __launch_bounds__(kGemmThreads, 1)
+template <int BN, bool A_MN, bool B_MN, int PA, int PB, int EPI>
+__global__ void __launch_bounds__(gemm_threads(EPI), 1)
 gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
            const __grid_constant__ GemmArgs g)
 {
     constexpr Pairs<PA, PB> P;
     constexpr uint32_t kTileB = (uint32_t)BN * 128u;
-    constexpr int HALF = BN / 2, SEG = HALF < 32 ? HALF : 32;
+    constexpr int COLS = BN / (EPI / 4), SEG = COLS < 32 ? COLS : 32;  // an output warp's columns
+    constexpr uint32_t kRing = 224 * 1024 - EPI * 4096;
     constexpr bool JOINT = PA == 1 && PB == 1;      // A's and B's slots go together: one barrier for both
     constexpr bool SUMS = A_MN || B_MN || PB == 3;  // fp32 results: several accumulators to a tile
     constexpr uint32_t kCols = 2 * BN < 32 ? 32 : 2 * BN;
@@ -485,7 +565,7 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
     uint8_t *base = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const int SA = g.SA, SB = g.SB;
     const uint32_t ring_a = smem_u32(base), ring_b = ring_a + (uint32_t)SA * kTileA;
-    uint64_t *full_a = (uint64_t *)(base + kRingBytes + kStageBytes);
+    uint64_t *full_a = (uint64_t *)(base + 224 * 1024);
     uint64_t *empty_a = full_a + kMaxRing, *full_b = empty_a + kMaxRing, *empty_b = full_b + kMaxRing;
     uint64_t *acc_full = empty_b + kMaxRing, *acc_empty = acc_full + 2, *done = acc_empty + 2;
     uint32_t *tmem_slot = (uint32_t *)(done + 1);
@@ -499,7 +579,7 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
         tc::mbar_init(&empty_b[tid], 1);
         if (tid < 2) {
             tc::mbar_init(&acc_full[tid], 1);
-            tc::mbar_init(&acc_empty[tid], kEpiWarps);
+            tc::mbar_init(&acc_empty[tid], EPI);
         }
         if (tid == 0) {
             tc::mbar_init(done, 1);
@@ -554,7 +634,10 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
     Ring ra = {SA}, rb = {SB};
 
     if (warp < 4) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if constexpr (EPI == 8)
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        else
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
         if (warp == 0 && lane == 0) {
             long long na = 0, nb = 0;  // loads
             bool ok = true;
@@ -652,15 +735,18 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
         }
         __syncwarp();
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+        if constexpr (EPI == 8)
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+        else
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
         // ------------------------------------------------------ sums and outputs
-        const int q = warp & 3, half = (warp >> 2) - 1;  // a warp reads its quadrant of the lanes
-        float *stage = (float *)(base + kRingBytes) + (warp - 4) * 1024;
+        const int q = warp & 3, group = (warp >> 2) - 1;  // a warp reads its quadrant of the lanes
+        float *stage = (float *)(base + kRing) + (warp - 4) * 1024;
         uint32_t acc = 0;
         bool ok = true;
         for (long long u = blockIdx.x; ok && u < units; u += gridDim.x) {
             unit(u, m0, n0, sp, c_lo, c_hi);
-            const int mm = m0 + q * 32, nn = n0 + half * HALF;
+            const int mm = m0 + q * 32, nn = n0 + group * COLS;
             float *mine = stage + lane * 32;
             // (the whole warp waits together: its reads of tensor memory are collective)
             auto filled = [&]() {
@@ -675,20 +761,20 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
                 ++acc;
             };
             auto read = [&](int col, uint32_t (&v)[SEG / 16][16]) {  // SEG columns, their reads in flight together
-                const uint32_t at = tmem + ((uint32_t)(q * 32) << 16) + (acc & 1) * BN + half * HALF + col;
+                const uint32_t at = tmem + ((uint32_t)(q * 32) << 16) + (acc & 1) * BN + group * COLS + col;
 #pragma unroll
                 for (int j = 0; j < SEG / 16; ++j) tc::tmem_ld16_async(at + 16 * j, v[j]);
                 tc::tmem_wait_ld();
             };
             if constexpr (SUMS) {
-                float sum[HALF];
+                float sum[COLS];
 #pragma unroll
-                for (int i = 0; i < HALF; ++i) sum[i] = 0.0f;
+                for (int i = 0; i < COLS; ++i) sum[i] = 0.0f;
 #pragma unroll 1
                 for (int c = c_lo; c < c_hi; c += g.per_acc) {
                     if (!(ok = filled())) break;
 #pragma unroll
-                    for (int i = 0; i < HALF; i += SEG) {
+                    for (int i = 0; i < COLS; i += SEG) {
                         uint32_t v[SEG / 16][16];
                         read(i, v);
 #pragma unroll
@@ -699,7 +785,7 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
                 if (!ok) break;
                 auto in = [&](int seg) {
 #pragma unroll
-                    for (int k = 0; k < HALF / SEG; ++k)
+                    for (int k = 0; k < COLS / SEG; ++k)
                         if (seg == k)
 #pragma unroll
                             for (int i = 0; i < SEG / 4; ++i) {
@@ -707,7 +793,7 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
                                 *(float4 *)(mine + ((i ^ (lane & 7)) << 2)) = make_float4(v[0], v[1], v[2], v[3]);
                             }
                 };
-                put_tile<SEG, HALF / SEG, A_MN || B_MN>(in, g.ep, g.swapped, sp, stage, lane, mm, nn);
+                put_tile<SEG, COLS / SEG, A_MN || B_MN, true>(in, g.ep, g.swapped, sp, stage, lane, mm, nn);
             } else {
                 if (!(ok = filled())) break;
                 auto in = [&](int seg) {
@@ -717,9 +803,9 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
                     for (int i = 0; i < SEG / 4; ++i)
                         *(uint4 *)(mine + ((i ^ (lane & 7)) << 2)) =
                             make_uint4(v[i / 4][i % 4 * 4], v[i / 4][i % 4 * 4 + 1], v[i / 4][i % 4 * 4 + 2], v[i / 4][i % 4 * 4 + 3]);
-                    if (seg == HALF / SEG - 1) release();
+                    if (seg == COLS / SEG - 1) release();
                 };
-                put_tile<SEG, HALF / SEG, false>(in, g.ep, g.swapped, sp, stage, lane, mm, nn);
+                put_tile<SEG, COLS / SEG, false, EPI == 8>(in, g.ep, g.swapped, sp, stage, lane, mm, nn);
             }
         }
         if (!ok && lane == 0) fail();
@@ -795,14 +881,16 @@ cudaError_t launch_gemm(const stacklstm_op *op, const Operand &a, const Operand 
     CUtensorMap ta, tb;
     cudaError_t e = operand_map(&ta, a, A_MN ? 64 : 128);
     if (!e) e = operand_map(&tb, b, B_MN ? 64 : BN);
-    if (!e) e = smem_at_least((const void *)gemm_parts<BN, A_MN, B_MN, PA, PB>, kGemmSmem);
+    constexpr int EPI = gemm_epi_warps(BN, A_MN || B_MN || PB == 3);
+    constexpr auto kernel = gemm_parts<BN, A_MN, B_MN, PA, PB, EPI>;
+    if (!e) e = smem_at_least((const void *)kernel, kGemmSmem);
     if (e) return e;
     const unsigned grid = (unsigned)std::min<long long>((long long)g.mt * g.nt * g.split, op->num_sms);
-    gemm_parts<BN, A_MN, B_MN, PA, PB><<<grid, kGemmThreads, kGemmSmem, op->stream>>>(ta, tb, g);
+    kernel<<<grid, gemm_threads(EPI), kGemmSmem, op->stream>>>(ta, tb, g);
     return cudaGetLastError();
 }
 
-enum { kWsX = 0, kWsW, kWsDz, kWsSum, kWsPart };  // workspace buffers
+enum { kWsX = 0, kWsW, kWsDz, kWsSum, kWsPart, kWsCount };  // workspace buffers
 
 constexpr size_t kMostPartBytes = (size_t)1 << 30;  // of the splits' sums
 
@@ -851,11 +939,12 @@ cudaError_t contract_parts(stacklstm_op *op, const Operand &a, const Operand &b,
     plan_gemm(g, PA, PB, P.n, M, N, lo, hi, (size_t)ep.rows * ep.cols, op->num_sms, &bn);
     // rings: as many whole chunks as fit, what is left to the single part of B, then to A
     const uint32_t tb = (uint32_t)bn * 128;
-    const int depth = (int)(kRingBytes / (PA * kTileA + PB * tb));
+    const uint32_t ring = gemm_ring(gemm_epi_warps(bn, A_MN || B_MN || PB == 3));
+    const int depth = (int)(ring / (PA * kTileA + PB * tb));
     g.SA = std::min(kMaxRing / PA, depth) * PA;
     g.SB = std::min(kMaxRing / PB, depth) * PB;
-    while (g.SB < kMaxRing && g.SA * kTileA + (g.SB + 1) * tb <= kRingBytes && PB < PA) ++g.SB;
-    while (PA > 1 && g.SA < kMaxRing && (g.SA + 1) * kTileA + g.SB * tb <= kRingBytes) ++g.SA;
+    while (g.SB < kMaxRing && g.SA * kTileA + (g.SB + 1) * tb <= ring && PB < PA) ++g.SB;
+    while (PA > 1 && g.SA < kMaxRing && (g.SA + 1) * kTileA + g.SB * tb <= ring) ++g.SA;
     if (g.split > 1) {
         cudaError_t e = op_workspace(op, kWsPart, (size_t)g.split * ep.rows * ep.cols * 4);
         if (e) return e;
@@ -890,9 +979,9 @@ cudaError_t contract(stacklstm_op *op, const Operand &a, const Operand &b, int k
 
 int row_ld(int cols) { return (cols + 7) / 8 * 8; }
 
-// An activation or weight tensor as an operand: itself where its rows start on 16 bytes, else a
-// copy in the workspace; the three parts of an fp32 one.
-cudaError_t as_operand(stacklstm_op *op, const void *src, size_t rows, int cols, int ws, Operand *o)
+// An activation or weight tensor as an operand: itself where its rows start on 16 bytes, else what
+// `pack` makes of it in the workspace (a copy, or the three parts of an fp32 one).
+cudaError_t as_operand(stacklstm_op *op, const void *src, size_t rows, int cols, int ws, Pack *pack, Operand *o)
 {
     const int ld = row_ld(cols);
     if (op->dt == SL_BF16 && ld == cols) {
@@ -900,14 +989,20 @@ cudaError_t as_operand(stacklstm_op *op, const void *src, size_t rows, int cols,
         return cudaSuccess;
     }
     const int parts = op->dt == SL_BF16 ? 1 : 3;
-    cudaError_t e = op_workspace(op, ws, (size_t)parts * rows * ld * 2);
-    if (e) return e;
-    const unsigned grid = (unsigned)std::min<size_t>(ceil_div(rows * cols, 256), (size_t)op->num_sms * 16);
-    if (op->dt == SL_BF16)
-        pack_parts<<<grid, 256, 0, op->stream>>>(rows, cols, ld, (const __nv_bfloat16 *)src, (__nv_bfloat16 *)op->ws[ws]);
-    else
-        pack_parts<<<grid, 256, 0, op->stream>>>(rows, cols, ld, (const float *)src, (__nv_bfloat16 *)op->ws[ws]);
+    if (cudaError_t e = op_workspace(op, ws, (size_t)parts * rows * ld * 2)) return e;
+    *pack = {src, (__nv_bfloat16 *)op->ws[ws], rows, cols, ld, ceil_div(rows * ld / 4, 256 * kPackItems)};
     *o = {op->ws[ws], rows, cols, ld, parts};
+    return cudaSuccess;
+}
+
+cudaError_t launch_prepare(const stacklstm_op *op, const Prepare &p)
+{
+    const unsigned ctas = p.dz.ctas + p.x.ctas + p.w.ctas;
+    if (!ctas) return cudaSuccess;
+    if (op->dt == SL_BF16)
+        prepare<__nv_bfloat16><<<ctas, 256, 0, op->stream>>>(p);
+    else
+        prepare<float><<<ctas, 256, 0, op->stream>>>(p);
     return cudaGetLastError();
 }
 
@@ -930,6 +1025,13 @@ sl_status stacklstm_linear_create(stacklstm_op_t *out, int R, int K, int N, sl_d
     stacklstm_op *op = op_new(SL_OP_LINEAR, dtype, device, stream, &st);
     if (!op) return st;
     op->R = R; op->K = K; op->N = N; op->act = act;
+    OpDevice guard(device);
+    const size_t counts = ceil_div(N, kDzCols) * 4;
+    if (op_workspace(op, kWsCount, counts) || cudaMemset(op->ws[kWsCount], 0, counts)) {
+        cudaGetLastError();
+        stacklstm_op_destroy(op);
+        return SL_ERR_OOM;
+    }
     *out = op;
     return SL_OK;
 }
@@ -944,8 +1046,10 @@ sl_status stacklstm_linear_forward(stacklstm_op_t op, int rows, const void *x, c
     if (const char *m = check_pointers({x, W, y}, {bias, residual, pre})) return op_fail(op, SL_ERR_ARG, m);
     OpDevice guard(op->device);
     Operand xo, wo;
-    cudaError_t e = as_operand(op, x, rows, op->K, kWsX, &xo);
-    if (!e) e = as_operand(op, W, op->N, op->K, kWsW, &wo);
+    Prepare p = {};
+    cudaError_t e = as_operand(op, x, rows, op->K, kWsX, &p.x, &xo);
+    if (!e) e = as_operand(op, W, op->N, op->K, kWsW, &p.w, &wo);
+    if (!e) e = launch_prepare(op, p);
     if (!e) {
         Epilogue ep = {};
         ep.rows = rows; ep.cols = op->N; ep.act = op->act; ep.bf16_out = op->dt == SL_BF16;
@@ -974,43 +1078,30 @@ sl_status stacklstm_linear_backward(stacklstm_op_t op, int rows, const float *dy
     if (const char *m = check_pointers({dy}, {pre, add, x, W})) return op_fail(op, SL_ERR_ARG, m);
     if (op->act != kActNone && !pre) return op_fail(op, SL_ERR_ARG, "an activation's backward needs pre");
     if ((dx && !W) || (dW && !x)) return op_fail(op, SL_ERR_ARG, "null pointer");
-    // dz in parts, its column sums
-    const int ld = row_ld(N);
-    const unsigned blocks = ceil_div(rows, kDzRows);
-    Operand dz = {nullptr, (size_t)rows, N, ld, 3};
-    if (dx || dW) {
-        if ((e = op_workspace(op, kWsDz, 3 * (size_t)rows * ld * 2))) return op_cuda(op, e, "stacklstm_linear_backward");
-        dz.p = op->ws[kWsDz];
-    }
-    if (dbias && (e = op_workspace(op, kWsSum, (size_t)blocks * N * 4))) return op_cuda(op, e, "stacklstm_linear_backward");
-    const dim3 grid(blocks, ceil_div(N, kDzCols));
-    float *sums = dbias ? (float *)op->ws[kWsSum] : nullptr;
-    auto launch = [&](auto kernel, auto *p) {
-        kernel<<<grid, 32 * kDzSub, 0, op->stream>>>(rows, N, ld, op->act, dy, p, (__nv_bfloat16 *)dz.p, sums);
-    };
-    const bool aligned = N % 4 == 0;
-    if (op->dt == SL_BF16)
-        launch(aligned ? dz_parts<__nv_bfloat16, true> : dz_parts<__nv_bfloat16, false>, (const __nv_bfloat16 *)pre);
-    else
-        launch(aligned ? dz_parts<float, true> : dz_parts<float, false>, (const float *)pre);
-    e = cudaGetLastError();
-    if (!e && dbias) {
-        sum_parts<<<ceil_div(N, 32), 256, 0, op->stream>>>(sums, (int)blocks, N, dbias);
-        e = cudaGetLastError();
+    // dz in parts, its column sums; the operands
+    Prepare p = {};
+    Operand dz = {nullptr, (size_t)rows, N, row_ld(N), 3}, wo, xo;
+    if (dx || dW) e = op_workspace(op, kWsDz, 3 * (size_t)rows * dz.ld * 2);
+    p.dz.row_blocks = ceil_div(rows, kDzRows);
+    if (!e && dbias) e = op_workspace(op, kWsSum, (size_t)p.dz.row_blocks * N * 4);
+    if (!e && dx) e = as_operand(op, W, N, K, kWsW, &p.w, &wo);
+    if (!e && dW) e = as_operand(op, x, rows, K, kWsX, &p.x, &xo);
+    if (!e && (dx || dW || dbias)) {
+        if (dx || dW) dz.p = op->ws[kWsDz];
+        p.dz.dy = dy; p.dz.pre = pre; p.dz.out = (__nv_bfloat16 *)dz.p; p.dz.part = dbias ? (float *)op->ws[kWsSum] : nullptr;
+        p.dz.dbias = dbias; p.dz.arrived = (int *)op->ws[kWsCount]; p.dz.rows = rows; p.dz.N = N; p.dz.ld = dz.ld; p.dz.act = op->act;
+        p.dz.ctas = p.dz.row_blocks * ceil_div(N, kDzCols);
+        e = launch_prepare(op, p);
     }
     if (!e && dx) {
-        Operand wo;
-        e = as_operand(op, W, N, K, kWsW, &wo);
         Epilogue ep = {};
         ep.rows = rows; ep.cols = K; ep.out = dx; ep.add = add;
-        if (!e) e = contract<false, true>(op, dz, wo, N, false, ep);
+        e = contract<false, true>(op, dz, wo, N, false, ep);
     }
     if (!e && dW) {
-        Operand xo;
-        e = as_operand(op, x, rows, K, kWsX, &xo);
         Epilogue ep = {};
         ep.rows = N; ep.cols = K; ep.out = dW;
-        if (!e) e = contract<true, true>(op, dz, xo, rows, false, ep);
+        e = contract<true, true>(op, dz, xo, rows, false, ep);
     }
     return e ? op_cuda(op, e, "stacklstm_linear_backward") : SL_OK;
 }

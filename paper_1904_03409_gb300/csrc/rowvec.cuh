@@ -119,8 +119,8 @@ __device__ __forceinline__ void lanes_join(float (&v)[NV])
     }
 }
 // The same over the TPR threads of a row: some lanes of a warp, or the whole CTA through `sm`
-// (NV TPR / 32 floats, free again after the call).
-template <bool MAX, int TPR, int NV>
+// (NV TPR / 32 floats; free again after the call, or with KEEP after the CTA's next barrier).
+template <bool MAX, int TPR, bool KEEP = false, int NV>
 __device__ __forceinline__ void row_join(float (&v)[NV], float *sm)
 {
     lanes_join<MAX, (TPR < 32 ? TPR : 32)>(v);
@@ -135,7 +135,7 @@ __device__ __forceinline__ void row_join(float (&v)[NV], float *sm)
 #pragma unroll
         for (int i = 0; i < NV; ++i) v[i] = lane < W ? sm[i * W + lane] : MAX ? -INFINITY : 0.0f;
         lanes_join<MAX, 32>(v);
-        __syncthreads();
+        if constexpr (!KEEP) __syncthreads();
     }
 }
 
