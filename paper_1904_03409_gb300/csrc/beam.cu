@@ -28,6 +28,7 @@ lse_rows(int rows, int V, const T *__restrict__ z, float *__restrict__ lse)
 {
     constexpr int E = RowVec<T>::E;
     __shared__ float sm[32];
+    after_previous();
     const int r = blockIdx.x * rows_per_cta(TPR) + (TPR <= 32 ? threadIdx.x / TPR : 0), t = threadIdx.x % TPR;
     const RowVec<T> row(r, V);
     const int n = r < rows ? row.pieces() : 0;  // (a row past the end has no pieces: its lanes stay for the joins)
@@ -79,10 +80,10 @@ cudaError_t launch_lse(int rows, int V, const void *z, float *lse, cudaStream_t 
     row_plan<T>(V, &tpr, &np);
     const unsigned grid = ceil_div(rows, rows_per_cta(tpr));
 #define SL_LSE(t, n) \
-    if (tpr == t && np == n) lse_rows<T, t, n><<<grid, row_cta(t), 0, st>>>(rows, V, (const T *)z, lse);
+    if (tpr == t && np == n) return launch_after(lse_rows<T, t, n>, grid, row_cta(t), 0, st, rows, V, (const T *)z, lse);
     SL_ROW_PLANS(SL_LSE)
 #undef SL_LSE
-    return cudaGetLastError();
+    return cudaErrorInvalidValue;  // not reached
 }
 
 // ------------------------------------------------------------------ selection
@@ -107,7 +108,6 @@ struct SelShared {
     u64 best[kMaxBeams];   // the K best, sorted
     u64 list[kList];
     u64 kth;
-    float least;
     int count, last;
     float score[kMaxBeams], lse[kMaxBeams];
     uint8_t done[kMaxBeams];
@@ -127,23 +127,22 @@ __device__ __forceinline__ void block_topk(float top, const Push &push, const Be
     const int width = K <= 32 ? NT / 32 : NT / 64, groups = NT / width;
     float g = top;
     for (int o = 1; o < width; o <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, o));
-    __syncthreads();
+    __syncthreads();  // (what an earlier call left in s is read)
     if (lane % width == 0) s.group[tid / width] = g;
-    if (tid == 0) {
-        s.count = 0;
-        s.least = -INFINITY;  // fewer than K groups with a candidate: every one counts
-    }
+    if (tid == 0) s.count = 0;
     if (tid < K) s.best[tid] = 0;
     __syncthreads();
-    if (tid < groups) {
-        const float mine = s.group[tid];
+    // every warp finds the K-th best group for itself: lane i ranks groups i and i + 32
+    float least = -INFINITY;  // fewer than K groups: every candidate counts
+    for (int half = 0; half < groups; half += 32) {
+        const int me = half + lane;
+        const float mine = s.group[me];
         int above = 0;
 #pragma unroll 8
-        for (int i = 0; i < groups; ++i) above += s.group[i] > mine || (s.group[i] == mine && i < tid);
-        if (above == K - 1) s.least = mine;
+        for (int i = 0; i < groups; ++i) above += s.group[i] > mine || (s.group[i] == mine && i < me);
+        const unsigned hit = __ballot_sync(0xffffffffu, above == K - 1);
+        if (hit) least = __shfl_sync(0xffffffffu, mine, __ffs(hit) - 1);
     }
-    __syncthreads();
-    const float least = s.least;
     if (top > -INFINITY && top >= least)
         push(least, [&](u64 k) {
             const int at = atomicAdd(&s.count, 1);  // any order: they are ranked below
@@ -210,6 +209,7 @@ beam_select(int K, int V, int nseg, int per_row, const T *__restrict__ z, const 
 {
     __shared__ SelShared s;
     extern __shared__ u64 spill[];
+    after_previous();
     const int tid = threadIdx.x, b = blockIdx.y, seg = blockIdx.x;
     if (tid < K) {
         s.score[tid] = score[(size_t)b * K + tid];
@@ -265,7 +265,7 @@ beam_select(int K, int V, int nseg, int per_row, const T *__restrict__ z, const 
         const uint32_t n = (uint32_t)K * (uint32_t)V;
         const T *zb = z + (size_t)b * n;
         float v[NI];
-        const uint32_t e0 = (uint32_t)seg * (NT * NI) + tid;
+        const uint32_t first = (uint32_t)seg * (NT * NI), e0 = first + tid;
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
             const uint32_t e = e0 + i * NT;
@@ -277,7 +277,7 @@ beam_select(int K, int V, int nseg, int per_row, const T *__restrict__ z, const 
         for (int i = 0; i < NI; ++i) {
             const uint32_t e = e0 + i * NT;
             key[i] = 0;
-            if (e < n) {
+            if (first + i * NT < n && e < n) {  // (the first for the whole CTA: a short segment ends early)
                 const uint32_t k = e / (uint32_t)V;
                 if (!s.done[k])
                     key[i] = make_key(__fadd_rn(s.score[k], __fsub_rn(v[i], s.lse[k])), e);
@@ -354,16 +354,13 @@ cudaError_t launch_select(const stacklstm_op *op, const void *z, const float *ls
     const int K = op->beams, V = op->V;
     const SelPlan p = select_plan<T>(op->B, K, V, op->num_sms);
     auto launch = [&](auto kernel, int nt, int ni) {
-        kernel<<<dim3(p.nseg, op->B), nt, (size_t)K * ni * 8, op->stream>>>(  // (at most 32 KB)
-            K, V, p.nseg, p.per_row, (const T *)z, lse, score, done, (u64 *)op->ws[0], (int *)op->ws[1], new_score, parent, token);
+        return launch_after(kernel, dim3(p.nseg, op->B), nt, (size_t)K * ni * 8, op->stream,  // (at most 32 KB)
+                            K, V, p.nseg, p.per_row, (const T *)z, lse, score, done, (u64 *)op->ws[0], (int *)op->ws[1], new_score,
+                            parent, token);
     };
-    if (p.large)
-        launch(beam_select<T, true, 512, 64>, 512, 64);
-    else if (p.rows)
-        launch(beam_select<T, true, 256, 32>, 256, 32);
-    else
-        launch(beam_select<T, false, 256, 32>, 256, 32);
-    return cudaGetLastError();
+    if (p.large) return launch(beam_select<T, true, 512, 64>, 512, 64);
+    if (p.rows) return launch(beam_select<T, true, 256, 32>, 256, 32);
+    return launch(beam_select<T, false, 256, 32>, 256, 32);
 }
 
 // ------------------------------------------------------------------ stacks
@@ -424,6 +421,7 @@ reorder_rows(int N, int K, int S, int PH, int PC, const int32_t *__restrict__ pa
              const QH *__restrict__ h, const QC *__restrict__ c, int32_t *__restrict__ p_out, QH *__restrict__ h_out,
              QC *__restrict__ c_out, QH *__restrict__ top_h, QC *__restrict__ top_c, int32_t *err)
 {
+    after_previous();
     const int n = blockIdx.x, s0 = blockIdx.y * kSlots;
     int top;
     const int src = source_row(n, K, S, parent, p, &top, err);
@@ -441,6 +439,7 @@ push_rows(int N, int S, int PH, int PC, const int8_t *__restrict__ ops, const QH
           const QC *__restrict__ c_new, int32_t *__restrict__ p, QH *__restrict__ h, QC *__restrict__ c,
           QH *__restrict__ top_h, QC *__restrict__ top_c, int32_t *err)
 {
+    after_previous();
     const int n = blockIdx.x;
     int at = p[n], op = ops[n];
     if (threadIdx.x == 0) {
@@ -549,19 +548,15 @@ sl_status stacklstm_beam_reorder(stacklstm_op_t op, const int32_t *parent, const
     const int N = op->R, K = op->beams, S = op->S, H = op->H;
     const bool bf = op->dt == SL_BF16;
     const dim3 grid(N, ceil_div(S, kSlots));
-    if (H % 8 == 0)
-        reorder_rows<<<grid, 256, 0, op->stream>>>(N, K, S, H / (bf ? 8 : 4), H / 4, parent, p, (const uint4 *)h_stack,
-                                                   (const uint4 *)c_stack, p_out, (uint4 *)h_out, (uint4 *)c_out,
-                                                   (uint4 *)top_h, (uint4 *)top_c, op->err);
-    else if (bf)
-        reorder_rows<<<grid, 256, 0, op->stream>>>(N, K, S, H, H, parent, p, (const uint16_t *)h_stack,
-                                                   (const uint32_t *)c_stack, p_out, (uint16_t *)h_out, (uint32_t *)c_out,
-                                                   (uint16_t *)top_h, (uint32_t *)top_c, op->err);
-    else
-        reorder_rows<<<grid, 256, 0, op->stream>>>(N, K, S, H, H, parent, p, (const uint32_t *)h_stack,
-                                                   (const uint32_t *)c_stack, p_out, (uint32_t *)h_out, (uint32_t *)c_out,
-                                                   (uint32_t *)top_h, (uint32_t *)top_c, op->err);
-    const cudaError_t e = cudaGetLastError();
+    auto copy = [&](auto qh, auto qc, int ph, int pc) {  // in pieces of these types
+        using QH = decltype(qh);
+        using QC = decltype(qc);
+        return launch_after(reorder_rows<QH, QC>, grid, 256, 0, op->stream, N, K, S, ph, pc, parent, p, (const QH *)h_stack,
+                            (const QC *)c_stack, p_out, (QH *)h_out, (QC *)c_out, (QH *)top_h, (QC *)top_c, op->err);
+    };
+    const cudaError_t e = H % 8 == 0 ? copy(uint4(), uint4(), H / (bf ? 8 : 4), H / 4)
+                          : bf       ? copy(uint16_t(), uint32_t(), H, H)
+                                     : copy(uint32_t(), uint32_t(), H, H);
     return e ? op_cuda(op, e, "stacklstm_beam_reorder") : SL_OK;
 }
 
@@ -575,18 +570,15 @@ sl_status stacklstm_beam_push(stacklstm_op_t op, const int8_t *ops, const void *
     OpDevice guard(op->device);
     const int N = op->R, S = op->S, H = op->H;
     const bool bf = op->dt == SL_BF16;
-    if (H % 8 == 0)
-        push_rows<<<N, 128, 0, op->stream>>>(N, S, H / (bf ? 8 : 4), H / 4, ops, (const uint4 *)h_new, (const uint4 *)c_new,
-                                             p, (uint4 *)h_stack, (uint4 *)c_stack, (uint4 *)top_h, (uint4 *)top_c, op->err);
-    else if (bf)
-        push_rows<<<N, 128, 0, op->stream>>>(N, S, H, H, ops, (const uint16_t *)h_new, (const uint32_t *)c_new, p,
-                                             (uint16_t *)h_stack, (uint32_t *)c_stack, (uint16_t *)top_h,
-                                             (uint32_t *)top_c, op->err);
-    else
-        push_rows<<<N, 128, 0, op->stream>>>(N, S, H, H, ops, (const uint32_t *)h_new, (const uint32_t *)c_new, p,
-                                             (uint32_t *)h_stack, (uint32_t *)c_stack, (uint32_t *)top_h,
-                                             (uint32_t *)top_c, op->err);
-    const cudaError_t e = cudaGetLastError();
+    auto step = [&](auto qh, auto qc, int ph, int pc) {
+        using QH = decltype(qh);
+        using QC = decltype(qc);
+        return launch_after(push_rows<QH, QC>, N, 128, 0, op->stream, N, S, ph, pc, ops, (const QH *)h_new, (const QC *)c_new, p,
+                            (QH *)h_stack, (QC *)c_stack, (QH *)top_h, (QC *)top_c, op->err);
+    };
+    const cudaError_t e = H % 8 == 0 ? step(uint4(), uint4(), H / (bf ? 8 : 4), H / 4)
+                          : bf       ? step(uint16_t(), uint32_t(), H, H)
+                                     : step(uint32_t(), uint32_t(), H, H);
     return e ? op_cuda(op, e, "stacklstm_beam_push") : SL_OK;
 }
 

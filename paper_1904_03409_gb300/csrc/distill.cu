@@ -155,6 +155,7 @@ distill_narrow(const __grid_constant__ DistillArgs a)
 {
     constexpr int E = RowVec<T>::E, RPC = 256 / TPR;
     extern __shared__ __align__(16) uint8_t dyn[];
+    after_previous();
     const int sub = threadIdx.x / TPR, t = threadIdx.x % TPR, k1 = a.k + 1;
     const Entries e = {(int *)dyn + (size_t)sub * k1, (float *)(dyn + (size_t)RPC * k1 * 4) + (size_t)sub * k1,
                        (float *)(dyn + (size_t)RPC * k1 * 8) + (size_t)sub * k1};
@@ -241,6 +242,7 @@ distill_wide(const __grid_constant__ DistillArgs a)
     __shared__ float sm_max[2 * 32], sm_sum[4 * 32];
     __shared__ int ec[kMaxTeacher + 1];
     __shared__ float ew[kMaxTeacher + 1], ez[kMaxTeacher + 1];
+    after_previous();
     const Entries e = {ec, ew, ez};
     const int t = threadIdx.x, lane = t & 31;
     const size_t r = blockIdx.x;
@@ -352,17 +354,13 @@ cudaError_t launch_distill(const stacklstm_op *op, const DistillArgs &a)
         auto launch = [&](auto kernel) {
             if (smem > 48 * 1024)
                 if (cudaError_t e = smem_at_least((const void *)kernel, smem)) return e;
-            kernel<<<grid, 256, smem, op->stream>>>(a);
-            return cudaGetLastError();
+            return launch_after(kernel, grid, 256, smem, op->stream, a);
         };
         return tpr == 8 ? launch(np == 1 ? distill_narrow<T, 8, 1> : np == 2 ? distill_narrow<T, 8, 2> : distill_narrow<T, 8, 4>)
                         : launch(np <= 2 ? distill_narrow<T, 32, 2> : distill_narrow<T, 32, 4>);
     }
-    if (tpr == 128)
-        distill_wide<T, 128><<<a.rows, 128, 0, op->stream>>>(a);
-    else
-        distill_wide<T, 512><<<a.rows, 512, 0, op->stream>>>(a);
-    return cudaGetLastError();
+    return tpr == 128 ? launch_after(distill_wide<T, 128>, a.rows, 128, 0, op->stream, a)
+                      : launch_after(distill_wide<T, 512>, a.rows, 512, 0, op->stream, a);
 }
 
 }  // namespace

@@ -261,6 +261,7 @@ template <typename T>
 __global__ void __launch_bounds__(256)
 prepare(const __grid_constant__ Prepare a)
 {
+    after_previous();
     unsigned cta = blockIdx.x;
     if (cta < a.dz.ctas) return dz_block<T>(a.dz, cta);
     cta -= a.dz.ctas;
@@ -596,6 +597,7 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
     __syncthreads();
     tc::tc_fence_after();
     const uint32_t tmem = *tmem_slot;
+    after_previous();
     auto fail = [&]() {
         *abort = 1;
         atomicCAS(g.err, 0, (int)SL_ERR_TIMEOUT);
@@ -830,6 +832,7 @@ __device__ __forceinline__ void join(const Epilogue &ep, int split, const Out &o
 __global__ void __launch_bounds__(256)
 join_splits(const __grid_constant__ Epilogue ep, int split)
 {
+    after_previous();
     if (ep.out)
         join(ep, split, Plain{ep.add, ep.out});
     else if (ep.bf16_out)
@@ -886,8 +889,7 @@ cudaError_t launch_gemm(const stacklstm_op *op, const Operand &a, const Operand 
     if (!e) e = smem_at_least((const void *)kernel, kGemmSmem);
     if (e) return e;
     const unsigned grid = (unsigned)std::min<long long>((long long)g.mt * g.nt * g.split, op->num_sms);
-    kernel<<<grid, gemm_threads(EPI), kGemmSmem, op->stream>>>(ta, tb, g);
-    return cudaGetLastError();
+    return launch_after(kernel, grid, gemm_threads(EPI), kGemmSmem, op->stream, ta, tb, g);
 }
 
 enum { kWsX = 0, kWsW, kWsDz, kWsSum, kWsPart, kWsCount };  // workspace buffers
@@ -959,9 +961,8 @@ cudaError_t contract_parts(stacklstm_op *op, const Operand &a, const Operand &b,
     if constexpr (PB == 1)
         if (bn == 256) e = launch_gemm<256, A_MN, B_MN, PA, PB>(op, a, b, g);
     if (!e && g.split > 1) {
-        join_splits<<<(unsigned)std::min<size_t>(ceil_div((size_t)ep.rows * ep.cols, 256), (size_t)op->num_sms * 8), 256, 0,
-                      op->stream>>>(ep, g.split);
-        e = cudaGetLastError();
+        const unsigned ctas = (unsigned)std::min<size_t>(ceil_div((size_t)ep.rows * ep.cols, 256), (size_t)op->num_sms * 8);
+        e = launch_after(join_splits, ctas, 256, 0, op->stream, ep, g.split);
     }
     return e;
 }
@@ -999,11 +1000,8 @@ cudaError_t launch_prepare(const stacklstm_op *op, const Prepare &p)
 {
     const unsigned ctas = p.dz.ctas + p.x.ctas + p.w.ctas;
     if (!ctas) return cudaSuccess;
-    if (op->dt == SL_BF16)
-        prepare<__nv_bfloat16><<<ctas, 256, 0, op->stream>>>(p);
-    else
-        prepare<float><<<ctas, 256, 0, op->stream>>>(p);
-    return cudaGetLastError();
+    return op->dt == SL_BF16 ? launch_after(prepare<__nv_bfloat16>, ctas, 256, 0, op->stream, p)
+                             : launch_after(prepare<float>, ctas, 256, 0, op->stream, p);
 }
 
 }  // namespace

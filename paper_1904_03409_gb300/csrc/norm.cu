@@ -81,6 +81,7 @@ norm_fwd(int rows, int N, const T *__restrict__ x, const float *__restrict__ gam
 {
     constexpr int RPB = norm_threads(TPR) / TPR;
     __shared__ float sm[32];
+    after_previous();
     const int t = threadIdx.x % TPR, step = gridDim.x * RPB;
     const float inv = 1.0f / (float)N;
     const bool whole = on_32(gamma) && on_32(beta);
@@ -149,6 +150,7 @@ norm_fwd_wide(int rows, int N, const T *__restrict__ x, const float *__restrict_
               float *__restrict__ rstd)
 {
     __shared__ float sm[kWideThreads / 32];
+    after_previous();
     const float inv = 1.0f / (float)N;
     for (int r = blockIdx.x; r < rows; r += gridDim.x) {
         const T *xr = x + (size_t)r * N;
@@ -189,6 +191,7 @@ norm_bwd(int rows, int N, const float *__restrict__ dy, const T *__restrict__ x,
     constexpr size_t kRow = norm_row_bytes<T>(TPR, VEC, CH);
     __shared__ float sm[2 * 32];
     extern __shared__ __align__(16) uint8_t dyn[];  // the rows ahead; then the column sums [RPB][N]
+    after_previous();
     const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR, step = gridDim.x * RPB;
     const float inv = 1.0f / (float)N;
     const bool whole = on_32(gamma) && on_32(dx);
@@ -220,9 +223,14 @@ norm_bwd(int rows, int N, const float *__restrict__ dy, const T *__restrict__ x,
     int r = blockIdx.x * RPB + sub;
 #pragma unroll
     for (int s = 0; s < kAhead; ++s) fetch(r + s * step, s);
+    float next_m = r < rows ? mean[r] : 0.0f, next_rs = r < rows ? rstd[r] : 0.0f;
     for (int s = 0; r < rows; r += step, s = s + 1 == kAhead ? 0 : s + 1) {
         const size_t at = (size_t)r * N;
-        const float m = mean[r], rs = rstd[r];
+        const float m = next_m, rs = next_rs;
+        if (r + step < rows) {
+            next_m = mean[r + step];
+            next_rs = rstd[r + step];
+        }
         float a[CH][VEC], xh[CH][VEC];
         float sums[2] = {0.0f, 0.0f};  // of a and of a xh
         if constexpr (VEC > 1) tc::cp_async_wait<kAhead - 1>();
@@ -306,6 +314,7 @@ norm_bwd_wide(int rows, int N, const float *__restrict__ dy, const T *__restrict
               float *__restrict__ part)
 {
     __shared__ float sm[kWideThreads / 32];
+    after_previous();
     const float inv = 1.0f / (float)N;
     float *out = part ? part + (size_t)blockIdx.x * 2 * N : nullptr;
     if (out)
@@ -340,6 +349,7 @@ __global__ void __launch_bounds__(1024)
 norm_reduce(const float *__restrict__ part, int n, int N, float *__restrict__ dgamma, float *__restrict__ dbeta)
 {
     __shared__ float sm[32][33];
+    after_previous();
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     const size_t c = blockIdx.x * (size_t)32 + lane, W = 2 * (size_t)N;
     float acc = 0.0f;
@@ -398,17 +408,16 @@ cudaError_t launch_norm(const NormCall &c, int grid)
 {
     const int N = c.op->N;
     if (!c.dy) {
-        norm_fwd<T, VEC, CH, TPR><<<grid, norm_threads(TPR), 0, c.op->stream>>>(c.rows, N, (const T *)c.x, c.gamma, c.beta,
-                                                                               c.eps, (T *)c.y, c.mean, c.rstd);
+        return launch_after(norm_fwd<T, VEC, CH, TPR>, grid, norm_threads(TPR), 0, c.op->stream, c.rows, N, (const T *)c.x, c.gamma,
+                            c.beta, c.eps, (T *)c.y, c.mean, c.rstd);
     } else {
         constexpr int NT = norm_bwd_threads(TPR, CH * VEC), RPB = NT / TPR;
         const size_t smem = std::max(kAhead * RPB * norm_row_bytes<T>(TPR, VEC, CH), RPB > 1 ? (size_t)RPB * N * 4 : 0);
         if (smem > 40 * 1024)
             if (cudaError_t e = smem_at_least((const void *)norm_bwd<T, VEC, CH, TPR>, smem)) return e;
-        norm_bwd<T, VEC, CH, TPR><<<grid, NT, smem, c.op->stream>>>(c.rows, N, c.dy, (const T *)c.x, c.gamma, c.mean, c.rstd,
-                                                                    c.dx, c.part);
+        return launch_after(norm_bwd<T, VEC, CH, TPR>, grid, NT, smem, c.op->stream, c.rows, N, c.dy, (const T *)c.x, c.gamma,
+                            (const float *)c.mean, (const float *)c.rstd, c.dx, c.part);
     }
-    return cudaGetLastError();
 }
 
 template <typename T>
@@ -420,13 +429,11 @@ cudaError_t run_norm(const NormCall &c, const NormPlan &p)
     SL_NORM(V, 1, 32) SL_NORM(V, 2, 32) SL_NORM(V, 4, 32) SL_NORM(V, 1, 256) SL_NORM(V, 2, 256) SL_NORM(V, 4, 256)
     SL_NORM(1, 4, 32) SL_NORM(1, 16, 32) SL_NORM(1, 4, 256) SL_NORM(1, 16, 256)
 #undef SL_NORM
-    if (!p.ch && !c.dy)
-        norm_fwd_wide<T><<<p.grid, kWideThreads, 0, c.op->stream>>>(c.rows, c.op->N, (const T *)c.x, c.gamma, c.beta, c.eps,
-                                                                    (T *)c.y, c.mean, c.rstd);
-    if (!p.ch && c.dy)
-        norm_bwd_wide<T><<<p.grid, kWideThreads, 0, c.op->stream>>>(c.rows, c.op->N, c.dy, (const T *)c.x, c.gamma,
-                                                                    c.mean, c.rstd, c.dx, c.part);
-    return cudaGetLastError();
+    if (!c.dy)
+        return launch_after(norm_fwd_wide<T>, p.grid, kWideThreads, 0, c.op->stream, c.rows, c.op->N, (const T *)c.x, c.gamma, c.beta,
+                            c.eps, (T *)c.y, c.mean, c.rstd);
+    return launch_after(norm_bwd_wide<T>, p.grid, kWideThreads, 0, c.op->stream, c.rows, c.op->N, c.dy, (const T *)c.x, c.gamma,
+                        (const float *)c.mean, (const float *)c.rstd, c.dx, c.part);
 }
 
 }  // namespace
@@ -497,10 +504,9 @@ sl_status stacklstm_norm_backward(stacklstm_op_t op, int rows, const float *dy, 
     c.part = sums ? (float *)op->ws[0] : nullptr;
     const NormPlan p = norm_plan(op, rows, true);
     e = op->dt == SL_BF16 ? run_norm<__nv_bfloat16>(c, p) : run_norm<float>(c, p);
-    if (!e && sums) {
-        norm_reduce<<<ceil_div(2 * (size_t)op->N, 32), 1024, 0, op->stream>>>((const float *)op->ws[0], p.grid, op->N, dgamma, dbeta);
-        e = cudaGetLastError();
-    }
+    if (!e && sums)
+        e = launch_after(norm_reduce, ceil_div(2 * (size_t)op->N, 32), 1024, 0, op->stream, (const float *)op->ws[0], p.grid, op->N,
+                         dgamma, dbeta);
     return e ? op_cuda(op, e, "stacklstm_norm_backward") : SL_OK;
 }
 
