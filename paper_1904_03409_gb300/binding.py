@@ -412,7 +412,7 @@ def _arg(t, device, dtype, shape, name):
     if t is None:
         return None
     try:
-        if t.get_device() == device and t.dtype == dtype and t.shape == shape and t.is_contiguous():
+        if t.get_device() == device and t.dtype is dtype and t.shape == shape and t.is_contiguous():
             return t.data_ptr()
     except AttributeError:
         pass

@@ -32,6 +32,18 @@ using tc::smem_u32;
 
 enum { kActNone = 0, kActRelu, kActTanh, kActGelu, kActSilu, kActs };
 
+__device__ __forceinline__ float rcp_hw(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float exp2_hw(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 __device__ __forceinline__ float act_f(float z, int act)
 {
     switch (act) {
@@ -41,6 +53,26 @@ __device__ __forceinline__ float act_f(float z, int act)
     case kActSilu: return z / (1.0f + expf(-z));
     default: return z;
     }
+}
+// The same for a result that is rounded to bf16. Phi(z) = 1 - h / 2 (z >= 0), h / 2 (z < 0) with
+// h = erfc(|z| / sqrt 2) = t (a1 + t (a2 + ...)) exp(-z^2 / 2), t = 1 / (1 + p |z| / sqrt 2), by formula
+// 7.1.26 of Abramowitz and Stegun's Handbook of Mathematical Functions (error 1.5e-7), a third of
+// erff's instructions, which bounded the layer; the sigmoid by the hardware's exponential and
+// quotient (2^-21).
+__device__ __forceinline__ float act_f_bf16(float z, int act)
+{
+    if (act == kActGelu) {
+        const float x = fabsf(z) * 0.70710678f;
+        const float t = rcp_hw(fmaf(0.3275911f, x, 1.0f));
+        float h = fmaf(t, 1.061405429f, -1.453152027f);
+        h = fmaf(t, h, 1.421413741f);
+        h = fmaf(t, h, -0.284496736f);
+        h = fmaf(t, h, 0.254829592f);
+        h *= t * exp2_hw(x * x * -1.44269504f);
+        return fmaf(-0.5f * fminf(fabsf(z), 64.0f), h, fmaxf(z, 0.0f));  // (z - z h / 2, -|z| h / 2; no inf x 0)
+    }
+    if (act == kActSilu) return __fdividef(z, 1.0f + __expf(-z));
+    return act_f(z, act);
 }
 __device__ __forceinline__ float act_grad(float z, int act)
 {
@@ -341,7 +373,7 @@ struct Forward {
     {
         v += bias;
         if (pre) pre[at] = from_f32<T>(v);
-        y[at] = from_f32<T>(act_f(v, act) + extra);
+        y[at] = from_f32<T>((sizeof(T) == 2 ? act_f_bf16(v, act) : act_f(v, act)) + extra);
     }
 };
 struct Plain {
@@ -351,9 +383,34 @@ struct Plain {
     __device__ __forceinline__ void put(size_t at, float v, float, float extra) const { out[at] = v + extra; }
 };
 
-// Two neighbours in one access.
-__device__ __forceinline__ void store2(float *p, float x, float y) { *(float2 *)p = make_float2(x, y); }
-__device__ __forceinline__ void store2(__nv_bfloat16 *p, float x, float y) { *(__nv_bfloat162 *)p = __floats2bfloat162_rn(x, y); }
+// W (2 or 4) neighbours in one access.
+template <int W>
+__device__ __forceinline__ void store_w(float *p, const float (&v)[W])
+{
+    if constexpr (W == 4)
+        *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]);
+    else
+        *(float2 *)p = make_float2(v[0], v[1]);
+}
+template <int W>
+__device__ __forceinline__ void store_w(__nv_bfloat16 *p, const float (&v)[W])
+{
+    union {
+        __nv_bfloat162 b[W / 2];
+        typename std::conditional<W == 4, uint2, uint32_t>::type q;
+    } o;
+#pragma unroll
+    for (int i = 0; i < W / 2; ++i) o.b[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+    *(decltype(o.q) *)p = o.q;
+}
+// The same as it lies in memory, and its values.
+template <typename T, int W>
+struct Few {
+    using Q = typename std::conditional<sizeof(T) * W == 16, float4, typename std::conditional<sizeof(T) * W == 8, float2, float>::type>::type;
+    Q q;
+    __device__ __forceinline__ void load(const T *p) { q = *(const Q *)p; }
+    __device__ __forceinline__ float get(int i) const { return to_f32(((const T *)&q)[i]); }
+};
 
 // A warp's 32 rows x SEG columns of sums in shared memory: row r's 16-byte pieces at piece ^ (r mod 8).
 __device__ __forceinline__ const float *staged(const float *stage, int r, int c)
@@ -400,72 +457,74 @@ __device__ __forceinline__ void put_cols(const Out &o, const float *stage, int l
     }
 }
 
-// A warp's 32 rows x 32 NSEG columns of an output with an even number of columns: two neighbours a
-// lane, two rows at a time; stage_in(seg) brings 32 columns of sums into `stage`. What is added to
-// a block of 32 columns (residual, add) is read while the block before it is worked on (AHEAD: where
-// few warps share an SM) or while its sums come in, and rows are finished four at a time (more of
-// them keep more activations in flight than there are registers).
-template <typename T, bool FORWARD, int ACT, int NSEG, bool AHEAD, typename StageIn>
-__device__ __forceinline__ void put_pairs(const StageIn &stage_in, const float *stage, int lane, int r0, int n0, int rows,
-                                          int cols, const float *bias_p, const T *extra_p, T *y, T *pre)
+// A warp's 32 rows x 32 NSEG columns of an output whose number of columns W (2 or 4) divides: W
+// neighbours a lane, W rows at a time; stage_in(seg) brings 32 columns of sums into `stage`. What is
+// added to a block of 32 columns (residual, add) is read while the block before it is worked on
+// (AHEAD: where few warps share an SM) or while its sums come in, and rows are finished a few at a
+// time (more of them keep more activations in flight than there are registers).
+template <typename T, int W, bool FORWARD, int ACT, int NSEG, bool AHEAD, typename StageIn>
+__device__ __forceinline__ void put_w(const StageIn &stage_in, const float *stage, int lane, int r0, int n0, int rows, int cols,
+                                      const float *bias_p, const T *extra_p, T *y, T *pre)
 {
-    const int j = (lane & 15) * 2, half = lane >> 4, m = min(32, rows - r0);
-    const size_t step = 2 * (size_t)cols, first = (size_t)(r0 + half) * cols + n0 + j;
-    using Two = typename std::conditional<sizeof(T) == 2, uint32_t, float2>::type;
-    Two next[16] = {}, extra[16];
+    constexpr int L = 32 / W, NI = 32 / W;  // lanes a row; steps of W rows
+    const int j = lane % L * W, sub = lane / L, m = min(32, rows - r0);
+    const size_t step = W * (size_t)cols, first = (size_t)(r0 + sub) * cols + n0 + j;
+    Few<T, W> next[NI] = {}, extra[NI];
     auto fetch = [&](int seg) {
         if (n0 + seg * 32 + j < cols)
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (half + 2 * i < m) next[i] = *(const Two *)(extra_p + first + seg * 32 + i * step);
+            for (int i = 0; i < NI; ++i)
+                if (sub + W * i < m) next[i].load(extra_p + first + seg * 32 + i * step);
     };
     if (AHEAD && extra_p) fetch(0);
 #pragma unroll 1
     for (int seg = 0; seg < NSEG; ++seg) {
         if (!AHEAD && extra_p) fetch(seg);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) extra[i] = next[i];
+        for (int i = 0; i < NI; ++i) extra[i] = next[i];
         if (AHEAD && extra_p && seg + 1 < NSEG) fetch(seg + 1);
         const int n = n0 + seg * 32 + j;
-        float2 bias = make_float2(0.0f, 0.0f);
-        if (FORWARD && bias_p && n < cols) bias = *(const float2 *)(bias_p + n);
+        float bias[W] = {};
+        if (FORWARD && bias_p && n < cols)
+#pragma unroll
+            for (int k = 0; k < W; ++k) bias[k] = bias_p[n + k];
         stage_in(seg);
         __syncwarp();
         if (n < cols) {
             const size_t at = first + seg * 32;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                if (half + 2 * i < m) {
-                    float2 v = *(const float2 *)staged(stage, half + 2 * i, j), e;
-                    if constexpr (sizeof(T) == 2)
-                        e = __bfloat1622float2(*(const __nv_bfloat162 *)&extra[i]);
-                    else
-                        e = extra[i];
-                    if (FORWARD) {
-                        v.x += bias.x;
-                        v.y += bias.y;
-                        if (pre) store2(pre + at + i * step, v.x, v.y);
-                        v = make_float2(act_f(v.x, ACT), act_f(v.y, ACT));
+            for (int i = 0; i < NI; ++i) {
+                if (sub + W * i < m) {
+                    Few<float, W> s;
+                    s.load(staged(stage, sub + W * i, j));
+                    float v[W];
+#pragma unroll
+                    for (int k = 0; k < W; ++k) v[k] = s.get(k) + (FORWARD ? bias[k] : 0.0f);
+                    if (FORWARD && pre) store_w<W>(pre + at + i * step, v);
+#pragma unroll
+                    for (int k = 0; k < W; ++k) {
+                        if (FORWARD) v[k] = sizeof(T) == 2 ? act_f_bf16(v[k], ACT) : act_f(v[k], ACT);
+                        v[k] += extra[i].get(k);
                     }
-                    store2(y + at + i * step, v.x + e.x, v.y + e.y);
+                    store_w<W>(y + at + i * step, v);
                 }
-                if (i % 4 == 3) asm volatile("" ::: "memory");
+                if (i % (8 / W) == 8 / W - 1) asm volatile("" ::: "memory");
             }
         }
         __syncwarp();
     }
 }
-template <typename T, int NSEG, bool AHEAD, typename StageIn>
-__device__ __forceinline__ void put_pairs_forward(const StageIn &in, const Epilogue &ep, const float *stage, int lane, int r0, int n0)
+template <typename T, int W, int NSEG, bool AHEAD, typename StageIn>
+__device__ __forceinline__ void put_forward(const StageIn &in, const Epilogue &ep, const float *stage, int lane, int r0, int n0)
 {
     const T *res = (const T *)ep.residual;
     T *y = (T *)ep.y, *pre = (T *)ep.pre;
     switch (ep.act) {
-    case kActRelu: put_pairs<T, true, kActRelu, NSEG, AHEAD>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre); break;
-    case kActTanh: put_pairs<T, true, kActTanh, NSEG, AHEAD>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre); break;
-    case kActGelu: put_pairs<T, true, kActGelu, NSEG, AHEAD>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre); break;
-    case kActSilu: put_pairs<T, true, kActSilu, NSEG, AHEAD>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre); break;
-    default: put_pairs<T, true, kActNone, NSEG, AHEAD>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
+    case kActRelu: put_w<T, W, true, kActRelu, NSEG, AHEAD>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre); break;
+    case kActTanh: put_w<T, W, true, kActTanh, NSEG, AHEAD>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre); break;
+    case kActGelu: put_w<T, W, true, kActGelu, NSEG, AHEAD>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre); break;
+    case kActSilu: put_w<T, W, true, kActSilu, NSEG, AHEAD>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre); break;
+    default: put_w<T, W, true, kActNone, NSEG, AHEAD>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
     }
 }
 
@@ -476,14 +535,14 @@ __device__ __forceinline__ void put_tile(const StageIn &in, const Epilogue &ep, 
 {
     const bool plain = GRADIENT || ep.part;
     const Plain p = {ep.part ? nullptr : ep.add, ep.part ? ep.part + (size_t)sp * ep.rows * ep.cols : ep.out};
-    if (SEG == 32 && ep.cols % 2 == 0 && (GRADIENT || !swapped)) {
+    if (SEG == 32 && ep.cols % 4 == 0 && (GRADIENT || !swapped)) {
         if (plain)
-            put_pairs<float, false, kActNone, NSEG, AHEAD>(in, stage, lane, m0, n0, ep.rows, ep.cols, nullptr, p.add, p.out, nullptr);
+            put_w<float, 4, false, kActNone, NSEG, AHEAD>(in, stage, lane, m0, n0, ep.rows, ep.cols, nullptr, p.add, p.out, nullptr);
         else if constexpr (!GRADIENT) {
             if (ep.bf16_out)
-                put_pairs_forward<__nv_bfloat16, NSEG, AHEAD>(in, ep, stage, lane, m0, n0);
+                put_forward<__nv_bfloat16, 4, NSEG, AHEAD>(in, ep, stage, lane, m0, n0);
             else
-                put_pairs_forward<float, NSEG, AHEAD>(in, ep, stage, lane, m0, n0);
+                put_forward<float, 4, NSEG, AHEAD>(in, ep, stage, lane, m0, n0);
         }
         return;
     }
