@@ -597,6 +597,24 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void *tmap, int 
         : "memory");
 }
 
+// The same lane of a whole warp every time.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
+// mbar_wait by a whole warp, one answer for all of it.
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, long long limit, volatile int *abort)
+{
+    if (__all_sync(0xffffffffu, tc::mbar_test_wait(bar, parity))) return true;
+    const long long t0 = clock64();
+    while (true) {
+        if (__any_sync(0xffffffffu, clock64() - t0 >= limit || *abort)) return false;
+        if (__all_sync(0xffffffffu, tc::mbar_try_wait(bar, parity))) return true;
+    }
+}
+
 __device__ __forceinline__ void prefetch_map(const void *tmap)
 {
     asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)tmap) : "memory");
@@ -699,7 +717,11 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
             asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         else
             asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
-        if (warp == 0 && lane == 0) {
+        // Both loops are run by whole warps, one lane of which issues: descriptors and coordinates
+        // are then the same for a warp and stay in its uniform registers (by one thread in a branch
+        // of its own an MMA took 125 cycles to issue, whatever its size).
+        const bool issues = elect_one();
+        if (warp == 0) {
             long long na = 0, nb = 0;  // loads
             bool ok = true;
             for (long long u = blockIdx.x; ok && u < units; u += gridDim.x) {
@@ -710,35 +732,37 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
                     for (int p = 0; p < P.n; ++p) {
                         if (P.load_b[p] && ok) {
                             const int at = P.at_b[P.b[p]], s = rb.slot(at);
-                            ok = tc::mbar_wait(&empty_b[s], rb.phase(at) ^ 1, limit, abort);
+                            ok = warp_wait(&empty_b[s], rb.phase(at) ^ 1, limit, abort);
                             if (ok) {
-                                tc::mbar_arrive_expect_tx(&full_b[s], JOINT ? kTileA + kTileB : kTileB);
                                 ++nb;
                                 const uint32_t dst = ring_b + s * kTileB;
-                                if constexpr (B_MN) {
+                                if (issues) {
+                                    tc::mbar_arrive_expect_tx(&full_b[s], JOINT ? kTileA + kTileB : kTileB);
+                                    if constexpr (B_MN) {
 #pragma unroll
-                                    for (int j = 0; j < BN / 64; ++j)
-                                        tma_load_3d(dst + j * 8192, &tm_b, n0 + j * 64, k0, P.b[p], &full_b[s]);
-                                } else {
-                                    tma_load_3d(dst, &tm_b, k0, n0, P.b[p], &full_b[s]);
+                                        for (int j = 0; j < BN / 64; ++j)
+                                            tma_load_3d(dst + j * 8192, &tm_b, n0 + j * 64, k0, P.b[p], &full_b[s]);
+                                    } else {
+                                        tma_load_3d(dst, &tm_b, k0, n0, P.b[p], &full_b[s]);
+                                    }
                                 }
                             }
                         }
                         if (P.load_a[p] && ok) {
                             const int at = P.at_a[P.a[p]], s = ra.slot(at);
                             uint64_t *full = JOINT ? &full_b[s] : &full_a[s];
-                            if (!JOINT) ok = tc::mbar_wait(&empty_a[s], ra.phase(at) ^ 1, limit, abort);
+                            if (!JOINT) ok = warp_wait(&empty_a[s], ra.phase(at) ^ 1, limit, abort);
                             if (ok) {
-                                if (!JOINT) {
-                                    tc::mbar_arrive_expect_tx(full, kTileA);
-                                    ++na;
-                                }
+                                if (!JOINT) ++na;
                                 const uint32_t dst = ring_a + s * kTileA;
-                                if constexpr (A_MN) {
-                                    tma_load_3d(dst, &tm_a, m0, k0, P.a[p], full);
-                                    tma_load_3d(dst + 8192, &tm_a, m0 + 64, k0, P.a[p], full);
-                                } else {
-                                    tma_load_3d(dst, &tm_a, k0, m0, P.a[p], full);
+                                if (issues) {
+                                    if (!JOINT) tc::mbar_arrive_expect_tx(full, kTileA);
+                                    if constexpr (A_MN) {
+                                        tma_load_3d(dst, &tm_a, m0, k0, P.a[p], full);
+                                        tma_load_3d(dst + 8192, &tm_a, m0 + 64, k0, P.a[p], full);
+                                    } else {
+                                        tma_load_3d(dst, &tm_a, k0, m0, P.a[p], full);
+                                    }
                                 }
                             }
                         }
@@ -747,14 +771,14 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
                     rb.next(PB);
                 }
             }
-            if (!ok) fail();
+            if (!ok && issues) fail();
             // no copy in flight when the CTA ends: the last load of every slot has landed
             for (int s = 0; s < SA; ++s)
                 if (na > s) tc::mbar_wait(&full_a[s], (uint32_t)((na - 1 - s) / SA) & 1, kDrain, nullptr);
             for (int s = 0; s < SB; ++s)
                 if (nb > s) tc::mbar_wait(&full_b[s], (uint32_t)((nb - 1 - s) / SB) & 1, kDrain, nullptr);
         }
-        if (warp == 1 && lane == 0) {
+        if (warp == 1) {
             constexpr uint32_t idesc = tc::idesc_bf16(BN, A_MN, B_MN);
             const uint64_t desc_a = tc::smem_desc(ring_a, A_MN ? 8192 : 16, 1024), desc_b = tc::smem_desc(ring_b, B_MN ? 8192 : 16, 1024);
             uint32_t acc = 0;  // accumulators filled so far
@@ -763,7 +787,7 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
                 unit(u, m0, n0, sp, c_lo, c_hi);
                 for (int c = c_lo; ok && c < c_hi; ++acc) {
                     const uint32_t d = tmem + (acc & 1) * BN;
-                    ok = tc::mbar_wait(&acc_empty[acc & 1], ((acc >> 1) & 1) ^ 1, limit, abort);
+                    ok = warp_wait(&acc_empty[acc & 1], ((acc >> 1) & 1) ^ 1, limit, abort);
                     if (!ok) break;
                     tc::tc_fence_after();
                     const int c_end = min(c_hi, c + g.per_acc);
@@ -772,26 +796,31 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
 #pragma unroll
                         for (int p = 0; p < P.n; ++p) {
                             const int ia = P.at_a[P.a[p]], ib = P.at_b[P.b[p]], sa = ra.slot(ia), sb = rb.slot(ib);
-                            if (P.load_b[p] && ok) ok = tc::mbar_wait(&full_b[sb], rb.phase(ib), limit, abort);
-                            if (P.load_a[p] && ok && !JOINT) ok = tc::mbar_wait(&full_a[sa], ra.phase(ia), limit, abort);
+                            if (P.load_b[p] && ok) ok = warp_wait(&full_b[sb], rb.phase(ib), limit, abort);
+                            if (P.load_a[p] && ok && !JOINT) ok = warp_wait(&full_a[sa], ra.phase(ia), limit, abort);
                             if (ok) {
                                 const uint64_t da = desc_a + (uint32_t)sa * (kTileA >> 4), db = desc_b + (uint32_t)sb * (kTileB >> 4);
+                                if (issues) {
 #pragma unroll
-                                for (int k = 0; k < 4; ++k)  // 16 of the contraction: 32 bytes of a row, or 16 rows
-                                    tc::mma_bf16(d, da + k * (A_MN ? 128 : 2), db + k * (B_MN ? 128 : 2), idesc, k || p ? 1 : more);
-                                if (P.free_a[p] && !JOINT) tc::mma_commit(&empty_a[sa]);
-                                if (P.free_b[p]) tc::mma_commit(&empty_b[sb]);
+                                    for (int k = 0; k < 4; ++k)  // 16 of the contraction: 32 bytes of a row, or 16 rows
+                                        tc::mma_bf16(d, da + k * (A_MN ? 128 : 2), db + k * (B_MN ? 128 : 2), idesc, k || p ? 1 : more);
+                                    if (P.free_a[p] && !JOINT) tc::mma_commit(&empty_a[sa]);
+                                    if (P.free_b[p]) tc::mma_commit(&empty_b[sb]);
+                                }
+                                __syncwarp();
                             }
                         }
                         more = 1;
                         ra.next(PA);
                         rb.next(PB);
                     }
-                    if (ok) tc::mma_commit(&acc_full[acc & 1]);
+                    if (ok && issues) tc::mma_commit(&acc_full[acc & 1]);
+                    __syncwarp();
                 }
             }
-            if (!ok) fail();
-            tc::mma_commit(done);
+            if (!ok && issues) fail();
+            if (issues) tc::mma_commit(done);
+            __syncwarp();
             tc::mbar_wait(done, 0, kDrain, nullptr);  // no MMA in flight when tensor memory is freed
         }
         __syncwarp();
@@ -811,7 +840,7 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
             float *mine = stage + lane * 32;
             // (the whole warp waits together: its reads of tensor memory are collective)
             auto filled = [&]() {
-                const bool got = __all_sync(0xffffffffu, tc::mbar_wait(&acc_full[acc & 1], (acc >> 1) & 1, limit, abort));
+                const bool got = warp_wait(&acc_full[acc & 1], (acc >> 1) & 1, limit, abort);
                 tc::tc_fence_after();
                 return got;
             };
