@@ -458,12 +458,12 @@ __device__ __forceinline__ void put_cols(const Out &o, const float *stage, int l
 }
 
 // A warp's 32 rows x 32 NSEG columns of an output whose number of columns W (2 or 4) divides: W
-// neighbours a lane, W rows at a time; stage_in(seg) brings 32 columns of sums into `stage`. What is
-// added to a block of 32 columns (residual, add) is read while the block before it is worked on
-// (AHEAD: where few warps share an SM) or while its sums come in, and rows are finished a few at a
-// time (more of them keep more activations in flight than there are registers).
-template <typename T, int W, bool FORWARD, int ACT, int NSEG, bool AHEAD, typename StageIn>
-__device__ __forceinline__ void put_w(const StageIn &stage_in, const float *stage, int lane, int r0, int n0, int rows, int cols,
+// neighbours a lane, W rows at a time; stage_in(seg) brings 32 columns of sums into `stage` (false: a
+// wait ran out). What is added to a block of 32 columns (residual, add) is read while the block
+// before it is worked on, the first one's while the sums are waited for, and rows are finished a few
+// at a time (more of them keep more activations in flight than there are registers).
+template <typename T, int W, bool FORWARD, int ACT, int NSEG, typename StageIn>
+__device__ __forceinline__ bool put_w(const StageIn &stage_in, const float *stage, int lane, int r0, int n0, int rows, int cols,
                                       const float *bias_p, const T *extra_p, T *y, T *pre)
 {
     constexpr int L = 32 / W, NI = 32 / W;  // lanes a row; steps of W rows
@@ -476,19 +476,18 @@ __device__ __forceinline__ void put_w(const StageIn &stage_in, const float *stag
             for (int i = 0; i < NI; ++i)
                 if (sub + W * i < m) next[i].load(extra_p + first + seg * 32 + i * step);
     };
-    if (AHEAD && extra_p) fetch(0);
+    if (extra_p) fetch(0);
 #pragma unroll 1
     for (int seg = 0; seg < NSEG; ++seg) {
-        if (!AHEAD && extra_p) fetch(seg);
+        if (!stage_in(seg)) return false;
 #pragma unroll
         for (int i = 0; i < NI; ++i) extra[i] = next[i];
-        if (AHEAD && extra_p && seg + 1 < NSEG) fetch(seg + 1);
+        if (extra_p && seg + 1 < NSEG) fetch(seg + 1);
         const int n = n0 + seg * 32 + j;
         float bias[W] = {};
         if (FORWARD && bias_p && n < cols)
 #pragma unroll
             for (int k = 0; k < W; ++k) bias[k] = bias_p[n + k];
-        stage_in(seg);
         __syncwarp();
         if (n < cols) {
             const size_t at = first + seg * 32;
@@ -513,42 +512,39 @@ __device__ __forceinline__ void put_w(const StageIn &stage_in, const float *stag
         }
         __syncwarp();
     }
+    return true;
 }
-template <typename T, int W, int NSEG, bool AHEAD, typename StageIn>
-__device__ __forceinline__ void put_forward(const StageIn &in, const Epilogue &ep, const float *stage, int lane, int r0, int n0)
+template <typename T, int W, int NSEG, typename StageIn>
+__device__ __forceinline__ bool put_forward(const StageIn &in, const Epilogue &ep, const float *stage, int lane, int r0, int n0)
 {
     const T *res = (const T *)ep.residual;
     T *y = (T *)ep.y, *pre = (T *)ep.pre;
     switch (ep.act) {
-    case kActRelu: put_w<T, W, true, kActRelu, NSEG, AHEAD>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre); break;
-    case kActTanh: put_w<T, W, true, kActTanh, NSEG, AHEAD>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre); break;
-    case kActGelu: put_w<T, W, true, kActGelu, NSEG, AHEAD>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre); break;
-    case kActSilu: put_w<T, W, true, kActSilu, NSEG, AHEAD>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre); break;
-    default: put_w<T, W, true, kActNone, NSEG, AHEAD>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
+    case kActRelu: return put_w<T, W, true, kActRelu, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
+    case kActTanh: return put_w<T, W, true, kActTanh, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
+    case kActGelu: return put_w<T, W, true, kActGelu, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
+    case kActSilu: return put_w<T, W, true, kActSilu, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
+    default: return put_w<T, W, true, kActNone, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
     }
 }
 
 // A warp's 32 rows x SEG NSEG columns of sums to the output.
-template <int SEG, int NSEG, bool GRADIENT, bool AHEAD, typename StageIn>
-__device__ __forceinline__ void put_tile(const StageIn &in, const Epilogue &ep, bool swapped, int sp, const float *stage,
+template <int SEG, int NSEG, bool GRADIENT, typename StageIn>
+__device__ __forceinline__ bool put_tile(const StageIn &in, const Epilogue &ep, bool swapped, int sp, const float *stage,
                                          int lane, int m0, int n0)
 {
     const bool plain = GRADIENT || ep.part;
     const Plain p = {ep.part ? nullptr : ep.add, ep.part ? ep.part + (size_t)sp * ep.rows * ep.cols : ep.out};
     if (SEG == 32 && ep.cols % 4 == 0 && (GRADIENT || !swapped)) {
         if (plain)
-            put_w<float, 4, false, kActNone, NSEG, AHEAD>(in, stage, lane, m0, n0, ep.rows, ep.cols, nullptr, p.add, p.out, nullptr);
-        else if constexpr (!GRADIENT) {
-            if (ep.bf16_out)
-                put_forward<__nv_bfloat16, 4, NSEG, AHEAD>(in, ep, stage, lane, m0, n0);
-            else
-                put_forward<float, 4, NSEG, AHEAD>(in, ep, stage, lane, m0, n0);
-        }
-        return;
+            return put_w<float, 4, false, kActNone, NSEG>(in, stage, lane, m0, n0, ep.rows, ep.cols, nullptr, p.add, p.out, nullptr);
+        if constexpr (!GRADIENT)
+            return ep.bf16_out ? put_forward<__nv_bfloat16, 4, NSEG>(in, ep, stage, lane, m0, n0)
+                               : put_forward<float, 4, NSEG>(in, ep, stage, lane, m0, n0);
     }
 #pragma unroll 1
     for (int seg = 0; seg < NSEG; ++seg, n0 += SEG) {
-        in(seg);
+        if (!in(seg)) return false;
         __syncwarp();
         if (!GRADIENT && swapped) {
             if (plain)
@@ -569,6 +565,7 @@ __device__ __forceinline__ void put_tile(const StageIn &in, const Epilogue &ep, 
         }
         __syncwarp();
     }
+    return true;
 }
 
 // Warp 0 for TMA, warp 1 for the MMAs (2 and 3 idle), then the warps for the sums and outputs: eight
@@ -583,7 +580,7 @@ static_assert(128 * 56 + 8 * 32 * 224 <= gemm_threads(8) * 168 && 128 * 32 + 16 
 constexpr int kMaxRing = 16;
 constexpr uint32_t kTileA = 128 * 128;  // 128 rows (or 2 x 64 columns) x 64 of the contraction
 constexpr uint32_t gemm_ring(int epi) { return 224 * 1024 - epi * 4096; }  // bytes: 4 KB a warp to stage outputs
-constexpr uint32_t kGemmBars = (4 * kMaxRing + 5) * 8 + 16;
+constexpr uint32_t kGemmBars = (6 * kMaxRing + 5) * 8 + 16;
 constexpr uint32_t kGemmSmem = 1024 + 224 * 1024 + kGemmBars;
 static_assert(kGemmSmem <= 227 * 1024, "shared memory of a CTA");
 constexpr int kGroupM = 16;             // m tiles that share their B tiles in L2
@@ -615,6 +612,60 @@ __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, long l
     }
 }
 
+// ---- pairs of CTAs (cta_group::2): one MMA of 256 rows over both, issued by the pair's first CTA;
+// each CTA holds its 128 rows of A, half of B's rows and its 128 rows of the accumulator.
+template <int CG>
+__device__ __forceinline__ void tmem_alloc_cg(uint32_t *dst, uint32_t ncols)
+{
+    if constexpr (CG == 1) {
+        tc::tmem_alloc(dst, ncols);
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(dst)), "r"(ncols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+}
+template <int CG>
+__device__ __forceinline__ void tmem_dealloc_cg(uint32_t addr, uint32_t ncols)
+{
+    if constexpr (CG == 1)
+        tc::tmem_dealloc(addr, ncols);
+    else
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(ncols) : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void mma_cg(uint32_t d, uint64_t da, uint64_t db, uint32_t idesc, uint32_t more)
+{
+    if constexpr (CG == 1)
+        tc::mma_bf16(d, da, db, idesc, more);
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+            "l"(da), "l"(db), "r"(idesc), "r"(more)
+            : "memory");
+}
+// Arrive on the barrier (of both CTAs of a pair) when the MMAs so far are done.
+template <int CG>
+__device__ __forceinline__ void commit_cg(uint64_t *bar)
+{
+    if constexpr (CG == 1)
+        tc::mma_commit(bar);
+    else
+        asm volatile(
+            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)),
+            "h"((uint16_t)3)
+            : "memory");
+}
+// Arrive on the pair's first CTA's barrier. (What is handed over are operands and accumulators that
+// only the asynchronous proxies read and write: no thread's reads are ordered after this, and
+// acquire and release at cluster scope, which a wait would pay 700 to 900 cycles for each time,
+// have nothing to order.)
+__device__ __forceinline__ void arrive_first(uint64_t *bar)
+{
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(tc::mapa(smem_u32(bar), 0)) : "memory");
+}
+
 __device__ __forceinline__ void prefetch_map(const void *tmap)
 {
     asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)tmap) : "memory");
@@ -627,13 +678,14 @@ __device__ __forceinline__ void prefetch_map(const void *tmap)
 // that fp32 results come from takes few of them (1.7e-8 of the result each: 1e-4 after 6012).
 // A part is loaded once a chunk, whatever number of products it is in, small products first.
 // MN-major operands: blocks of 64 columns, each 64 rows of 128 bytes.
-template <int BN, bool A_MN, bool B_MN, int PA, int PB, int EPI>
+template <int BN, bool A_MN, bool B_MN, int PA, int PB, int EPI, int CG>
 __global__ void __launch_bounds__(gemm_threads(EPI), 1)
 gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
            const __grid_constant__ GemmArgs g)
 {
     constexpr Pairs<PA, PB> P;
-    constexpr uint32_t kTileB = (uint32_t)BN * 128u;
+    constexpr int BR = BN / CG;  // rows of B that a CTA holds
+    constexpr uint32_t kTileB = (uint32_t)BR * 128u;
     constexpr int COLS = BN / (EPI / 4), SEG = COLS < 32 ? COLS : 32;  // an output warp's columns
     constexpr uint32_t kRing = 224 * 1024 - EPI * 4096;
     constexpr bool JOINT = PA == 1 && PB == 1;      // A's and B's slots go together: one barrier for both
@@ -645,19 +697,23 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
     const uint32_t ring_a = smem_u32(base), ring_b = ring_a + (uint32_t)SA * kTileA;
     uint64_t *full_a = (uint64_t *)(base + 224 * 1024);
     uint64_t *empty_a = full_a + kMaxRing, *full_b = empty_a + kMaxRing, *empty_b = full_b + kMaxRing;
-    uint64_t *acc_full = empty_b + kMaxRing, *acc_empty = acc_full + 2, *done = acc_empty + 2;
+    uint64_t *peer_a = empty_b + kMaxRing, *peer_b = peer_a + kMaxRing;  // the pair's other CTA's operands have landed
+    uint64_t *acc_full = peer_b + kMaxRing, *acc_empty = acc_full + 2, *done = acc_empty + 2;
     uint32_t *tmem_slot = (uint32_t *)(done + 1);
     volatile int *abort = (volatile int *)(tmem_slot + 1);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int rank = CG == 1 ? 0 : (int)tc::cluster_rank();
     if (tid < kMaxRing) {  // (every ring's, used or not)
         tc::mbar_init(&full_a[tid], 1);
         tc::mbar_init(&empty_a[tid], 1);
         tc::mbar_init(&full_b[tid], 1);
         tc::mbar_init(&empty_b[tid], 1);
+        tc::mbar_init(&peer_a[tid], 1);
+        tc::mbar_init(&peer_b[tid], 1);
         if (tid < 2) {
             tc::mbar_init(&acc_full[tid], 1);
-            tc::mbar_init(&acc_empty[tid], EPI);
+            tc::mbar_init(&acc_empty[tid], CG * EPI);
         }
         if (tid == 0) {
             tc::mbar_init(done, 1);
@@ -669,9 +725,10 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
         prefetch_map(&tm_a);
         prefetch_map(&tm_b);
     }
-    if (warp == 0) tc::tmem_alloc(tmem_slot, kCols);
+    if (warp == 0) tmem_alloc_cg<CG>(tmem_slot, kCols);
     tc::tc_fence_before();
     __syncthreads();
+    if constexpr (CG == 2) tc::cluster_sync();  // the other CTA's barriers are there
     tc::tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     after_previous();
@@ -688,7 +745,7 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
         sp = (int)(u / tiles);
         const int t = (int)(u % tiles), group = t / (kGroupM * g.nt), in = t % (kGroupM * g.nt);
         const int first = group * kGroupM, gm = min(kGroupM, g.mt - first);
-        m0 = (first + in % gm) * 128;
+        m0 = (first + in % gm) * 128 * CG + rank * 128;  // (this CTA's rows)
         n0 = in / gm * BN;
         c_lo = (int)((long long)g.chunks * sp / g.split);
         c_hi = (int)((long long)g.chunks * (sp + 1) / g.split);
@@ -724,7 +781,7 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
         if (warp == 0) {
             long long na = 0, nb = 0;  // loads
             bool ok = true;
-            for (long long u = blockIdx.x; ok && u < units; u += gridDim.x) {
+            for (long long u = blockIdx.x / CG; ok && u < units; u += gridDim.x / CG) {
                 unit(u, m0, n0, sp, c_lo, c_hi);
                 for (int c = c_lo; ok && c < c_hi; ++c) {
                     const int k0 = c * 64;
@@ -740,10 +797,10 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
                                     tc::mbar_arrive_expect_tx(&full_b[s], JOINT ? kTileA + kTileB : kTileB);
                                     if constexpr (B_MN) {
 #pragma unroll
-                                        for (int j = 0; j < BN / 64; ++j)
-                                            tma_load_3d(dst + j * 8192, &tm_b, n0 + j * 64, k0, P.b[p], &full_b[s]);
+                                        for (int j = 0; j < BR / 64; ++j)
+                                            tma_load_3d(dst + j * 8192, &tm_b, n0 + rank * BR + j * 64, k0, P.b[p], &full_b[s]);
                                     } else {
-                                        tma_load_3d(dst, &tm_b, k0, n0, P.b[p], &full_b[s]);
+                                        tma_load_3d(dst, &tm_b, k0, n0 + rank * BR, P.b[p], &full_b[s]);
                                     }
                                 }
                             }
@@ -778,12 +835,12 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
             for (int s = 0; s < SB; ++s)
                 if (nb > s) tc::mbar_wait(&full_b[s], (uint32_t)((nb - 1 - s) / SB) & 1, kDrain, nullptr);
         }
-        if (warp == 1) {
-            constexpr uint32_t idesc = tc::idesc_bf16(BN, A_MN, B_MN);
+        if (warp == 1 && rank == 0) {
+            constexpr uint32_t idesc = tc::idesc_bf16(BN, A_MN, B_MN, 128 * CG);
             const uint64_t desc_a = tc::smem_desc(ring_a, A_MN ? 8192 : 16, 1024), desc_b = tc::smem_desc(ring_b, B_MN ? 8192 : 16, 1024);
             uint32_t acc = 0;  // accumulators filled so far
             bool ok = true;
-            for (long long u = blockIdx.x; ok && u < units; u += gridDim.x) {
+            for (long long u = blockIdx.x / CG; ok && u < units; u += gridDim.x / CG) {
                 unit(u, m0, n0, sp, c_lo, c_hi);
                 for (int c = c_lo; ok && c < c_hi; ++acc) {
                     const uint32_t d = tmem + (acc & 1) * BN;
@@ -798,14 +855,16 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
                             const int ia = P.at_a[P.a[p]], ib = P.at_b[P.b[p]], sa = ra.slot(ia), sb = rb.slot(ib);
                             if (P.load_b[p] && ok) ok = warp_wait(&full_b[sb], rb.phase(ib), limit, abort);
                             if (P.load_a[p] && ok && !JOINT) ok = warp_wait(&full_a[sa], ra.phase(ia), limit, abort);
+                            if (CG == 2 && P.load_b[p] && ok) ok = warp_wait(&peer_b[sb], rb.phase(ib), limit, abort);
+                            if (CG == 2 && P.load_a[p] && ok && !JOINT) ok = warp_wait(&peer_a[sa], ra.phase(ia), limit, abort);
                             if (ok) {
                                 const uint64_t da = desc_a + (uint32_t)sa * (kTileA >> 4), db = desc_b + (uint32_t)sb * (kTileB >> 4);
                                 if (issues) {
 #pragma unroll
                                     for (int k = 0; k < 4; ++k)  // 16 of the contraction: 32 bytes of a row, or 16 rows
-                                        tc::mma_bf16(d, da + k * (A_MN ? 128 : 2), db + k * (B_MN ? 128 : 2), idesc, k || p ? 1 : more);
-                                    if (P.free_a[p] && !JOINT) tc::mma_commit(&empty_a[sa]);
-                                    if (P.free_b[p]) tc::mma_commit(&empty_b[sb]);
+                                        mma_cg<CG>(d, da + k * (A_MN ? 128 : 2), db + k * (B_MN ? 128 : 2), idesc, k || p ? 1 : more);
+                                    if (P.free_a[p] && !JOINT) commit_cg<CG>(&empty_a[sa]);
+                                    if (P.free_b[p]) commit_cg<CG>(&empty_b[sb]);
                                 }
                                 __syncwarp();
                             }
@@ -814,14 +873,38 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
                         ra.next(PA);
                         rb.next(PB);
                     }
-                    if (ok && issues) tc::mma_commit(&acc_full[acc & 1]);
+                    if (ok && issues) commit_cg<CG>(&acc_full[acc & 1]);
                     __syncwarp();
                 }
             }
             if (!ok && issues) fail();
-            if (issues) tc::mma_commit(done);
+            if (issues) commit_cg<CG>(done);
             __syncwarp();
             tc::mbar_wait(done, 0, kDrain, nullptr);  // no MMA in flight when tensor memory is freed
+        }
+        if (CG == 2 && warp == 1 && rank == 1) {  // tells the pair's first CTA what has landed here
+            bool ok = true;
+            for (long long u = blockIdx.x / CG; ok && u < units; u += gridDim.x / CG) {
+                unit(u, m0, n0, sp, c_lo, c_hi);
+                for (int c = c_lo; ok && c < c_hi; ++c) {
+#pragma unroll
+                    for (int p = 0; p < P.n; ++p) {
+                        const int ia = P.at_a[P.a[p]], ib = P.at_b[P.b[p]], sa = ra.slot(ia), sb = rb.slot(ib);
+                        if (P.load_b[p] && ok) {
+                            ok = warp_wait(&full_b[sb], rb.phase(ib), limit, abort);
+                            if (ok && issues) arrive_first(&peer_b[sb]);
+                        }
+                        if (P.load_a[p] && ok && !JOINT) {
+                            ok = warp_wait(&full_a[sa], ra.phase(ia), limit, abort);
+                            if (ok && issues) arrive_first(&peer_a[sa]);
+                        }
+                    }
+                    ra.next(PA);
+                    rb.next(PB);
+                }
+            }
+            if (!ok && issues) fail();
+            tc::mbar_wait(done, 0, kDrain, nullptr);  // (the last arrivals here of the other CTA's MMAs)
         }
         __syncwarp();
     } else {
@@ -834,7 +917,7 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
         float *stage = (float *)(base + kRing) + (warp - 4) * 1024;
         uint32_t acc = 0;
         bool ok = true;
-        for (long long u = blockIdx.x; ok && u < units; u += gridDim.x) {
+        for (long long u = blockIdx.x / CG; ok && u < units; u += gridDim.x / CG) {
             unit(u, m0, n0, sp, c_lo, c_hi);
             const int mm = m0 + q * 32, nn = n0 + group * COLS;
             float *mine = stage + lane * 32;
@@ -847,7 +930,12 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
             auto release = [&]() {
                 tc::tc_fence_before();
                 __syncwarp();
-                if (lane == 0) tc::mbar_arrive(&acc_empty[acc & 1]);
+                if (lane == 0) {
+                    if constexpr (CG == 1)
+                        tc::mbar_arrive(&acc_empty[acc & 1]);
+                    else
+                        arrive_first(&acc_empty[acc & 1]);
+                }
                 ++acc;
             };
             auto read = [&](int col, uint32_t (&v)[SEG / 16][16]) {  // SEG columns, their reads in flight together
@@ -882,11 +970,12 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
                                 const float *v = sum + k * SEG + 4 * i;
                                 *(float4 *)(mine + ((i ^ (lane & 7)) << 2)) = make_float4(v[0], v[1], v[2], v[3]);
                             }
+                    return true;
                 };
-                put_tile<SEG, COLS / SEG, A_MN || B_MN, true>(in, g.ep, g.swapped, sp, stage, lane, mm, nn);
+                put_tile<SEG, COLS / SEG, A_MN || B_MN>(in, g.ep, g.swapped, sp, stage, lane, mm, nn);
             } else {
-                if (!(ok = filled())) break;
                 auto in = [&](int seg) {
+                    if (seg == 0 && !filled()) return false;
                     uint32_t v[SEG / 16][16];
                     read(seg * SEG, v);
 #pragma unroll
@@ -894,15 +983,18 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
                         *(uint4 *)(mine + ((i ^ (lane & 7)) << 2)) =
                             make_uint4(v[i / 4][i % 4 * 4], v[i / 4][i % 4 * 4 + 1], v[i / 4][i % 4 * 4 + 2], v[i / 4][i % 4 * 4 + 3]);
                     if (seg == COLS / SEG - 1) release();
+                    return true;
                 };
-                put_tile<SEG, COLS / SEG, false, EPI == 8>(in, g.ep, g.swapped, sp, stage, lane, mm, nn);
+                ok = put_tile<SEG, COLS / SEG, false>(in, g.ep, g.swapped, sp, stage, lane, mm, nn);
             }
         }
         if (!ok && lane == 0) fail();
     }
     tc::tc_fence_before();
     __syncthreads();
-    if (warp == 0) tc::tmem_dealloc(tmem, kCols);
+    // (a pair's CTAs end together: one's MMAs read the other's operands, the other arrives on its barriers)
+    if constexpr (CG == 2) tc::cluster_sync();
+    if (warp == 0) tmem_dealloc_cg<CG>(tmem, kCols);
 }
 
 // The splits' sums of each output added in split order, then its epilogue.
@@ -966,47 +1058,78 @@ cudaError_t operand_map(CUtensorMap *tm, const Operand &o, int box_rows)
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-template <int BN, bool A_MN, bool B_MN, int PA, int PB>
+template <int BN, bool A_MN, bool B_MN, int PA, int PB, int CG>
 cudaError_t launch_gemm(const stacklstm_op *op, const Operand &a, const Operand &b, const GemmArgs &g)
 {
     CUtensorMap ta, tb;
     cudaError_t e = operand_map(&ta, a, A_MN ? 64 : 128);
-    if (!e) e = operand_map(&tb, b, B_MN ? 64 : BN);
+    if (!e) e = operand_map(&tb, b, B_MN ? 64 : BN / CG);
     constexpr int EPI = gemm_epi_warps(BN, A_MN || B_MN || PB == 3);
-    constexpr auto kernel = gemm_parts<BN, A_MN, B_MN, PA, PB, EPI>;
+    constexpr auto kernel = gemm_parts<BN, A_MN, B_MN, PA, PB, EPI, CG>;
     if (!e) e = smem_at_least((const void *)kernel, kGemmSmem);
     if (e) return e;
-    const unsigned grid = (unsigned)std::min<long long>((long long)g.mt * g.nt * g.split, op->num_sms);
-    return launch_after(kernel, grid, gemm_threads(EPI), kGemmSmem, op->stream, ta, tb, g);
+    const unsigned grid = (unsigned)std::min<long long>((long long)g.mt * g.nt * g.split, CG == 2 ? op->pairs : op->num_sms) * CG;
+    return launch_cluster(kernel, CG, grid, gemm_threads(EPI), kGemmSmem, op->stream, ta, tb, g);
+}
+
+// Pairs of CTAs that run at once: fewer than half the SMs where a group of SMs has an odd number of
+// them in use (76 pairs in a grid of which 72 run at once took twice the time).
+int most_pairs()
+{
+    constexpr auto kernel = gemm_parts<256, false, false, 1, 1, gemm_epi_warps(256, false), 2>;
+    if (smem_at_least((const void *)kernel, kGemmSmem)) return 0;
+    cudaLaunchAttribute attr = {};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 2;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2);
+    cfg.blockDim = dim3(gemm_threads(gemm_epi_warps(256, false)));
+    cfg.dynamicSmemBytes = kGemmSmem;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    return cudaOccupancyMaxActiveClusters(&n, (const void *)kernel, &cfg) == cudaSuccess ? n : 0;
 }
 
 enum { kWsX = 0, kWsW, kWsDz, kWsSum, kWsPart, kWsCount };  // workspace buffers
 
 constexpr size_t kMostPartBytes = (size_t)1 << 30;  // of the splits' sums
 
-// Tile width and splits: the least of waves x chunks x cycles a chunk (two cycles a column and
-// product, and no fewer than the operands' bytes take at 64 a cycle), a tile's start and end, and
-// for a split contraction its sums written and read again, and a second launch.
-void plan_gemm(GemmArgs &g, int PA, int PB, int npair, int M, int N, int bn_lo, int bn_hi, size_t out_elems, int sms, int *bn_out)
+// One CTA a tile of 128 rows or a pair a tile of 256, the tile's width, and the splits: the least of
+// waves x chunks x cycles a chunk, a tile's start and end, and for a split contraction its sums
+// written and read again, and a second launch. A chunk takes two cycles a column and product, or
+// what shared memory takes for the operands (128 bytes a cycle: written once a part, read once a
+// product), which is more for one CTA: 16 + 32 KB read a product of 128 x 256, 16 + 16 by each of
+// a pair.
+struct GemmPlan {
+    int cg, bn;
+};
+GemmPlan plan_gemm(GemmArgs &g, int PA, int PB, int npair, int M, int N, int bn_lo, int bn_hi, size_t out_elems, int sms, int pairs)
 {
+    GemmPlan best_plan = {1, 64};
     double best = 1e300;
-    for (int bn = bn_lo; bn <= bn_hi; bn *= 2) {
-        const double mt = ceil_div(M, 128), nt = ceil_div(N, bn);
-        const double cyc = std::max(2.0 * bn * npair, (PA * (double)kTileA + PB * bn * 128.0) / 64.0);
-        for (int split = 1; split <= std::min(g.chunks, 64); ++split) {
-            if (split > 1 && (g.chunks / split < 2 || (double)split * out_elems * 4 > (double)kMostPartBytes)) break;
-            const double waves = std::ceil(mt * nt * split / sms), chunks = std::ceil((double)g.chunks / split);
-            double cost = waves * (chunks * cyc + 400.0) + 16.0 * bn + 2000.0;
-            if (split > 1) cost += 5000.0 + 2.0 * split * out_elems * 4 / 3500.0;
-            if (cost < best) {
-                best = cost;
-                g.mt = (int)mt;
-                g.nt = (int)nt;
-                g.split = split;
-                *bn_out = bn;
+    for (int cg = 1; cg <= (pairs ? 2 : 1); ++cg)
+        for (int bn = bn_lo; bn <= bn_hi; bn *= 2) {
+            if (cg == 2 ? bn != 256 : bn == 256 && PB == 3) continue;  // (no such kernels)
+            const double mt = ceil_div(M, 128 * cg), nt = ceil_div(N, bn), b = bn * 128.0 / cg;
+            const double smem = (npair * (kTileA + b) + PA * (double)kTileA + PB * b) / 128.0;
+            const double cyc = std::max(2.0 * bn * npair, smem);
+            for (int split = 1; split <= std::min(g.chunks, 64); ++split) {
+                if (split > 1 && (g.chunks / split < 2 || (double)split * out_elems * 4 > (double)kMostPartBytes)) break;
+                const double waves = std::ceil(mt * nt * split / (cg == 2 ? pairs : sms)), chunks = std::ceil((double)g.chunks / split);
+                double cost = waves * (chunks * cyc + 400.0) + 16.0 * bn + 2000.0 + 1000.0 * cg;
+                if (split > 1) cost += 5000.0 + 2.0 * split * out_elems * 4 / 3500.0;
+                if (cost < best) {
+                    best = cost;
+                    g.mt = (int)mt;
+                    g.nt = (int)nt;
+                    g.split = split;
+                    best_plan = {cg, bn};
+                }
             }
         }
-    }
+    return best_plan;
 }
 
 // D = sum over the parts' products of A B^T, kcols long, and its epilogue.
@@ -1022,13 +1145,11 @@ cudaError_t contract_parts(stacklstm_op *op, const Operand &a, const Operand &b,
     g.limit = op->wait_limit;
     g.err = op->err;
     const int M = swapped ? ep.cols : ep.rows, N = swapped ? ep.rows : ep.cols;
-    // (three parts of a 256-wide B leave the rings no second chunk)
-    constexpr int most = PB == 3 ? 128 : 256;
-    const int lo = swapped && N <= 32 ? 32 : 64, hi = N <= lo ? lo : N <= 64 ? 64 : N <= 128 ? 128 : most;
-    int bn = 64;
-    plan_gemm(g, PA, PB, P.n, M, N, lo, hi, (size_t)ep.rows * ep.cols, op->num_sms, &bn);
+    const int lo = swapped && N <= 32 ? 32 : 64, hi = N <= lo ? lo : N <= 64 ? 64 : N <= 128 ? 128 : 256;
+    const GemmPlan plan = plan_gemm(g, PA, PB, P.n, M, N, lo, hi, (size_t)ep.rows * ep.cols, op->num_sms, op->pairs);
+    const int bn = plan.bn;
     // rings: as many whole chunks as fit, what is left to the single part of B, then to A
-    const uint32_t tb = (uint32_t)bn * 128;
+    const uint32_t tb = (uint32_t)bn * 128 / plan.cg;
     const uint32_t ring = gemm_ring(gemm_epi_warps(bn, A_MN || B_MN || PB == 3));
     const int depth = (int)(ring / (PA * kTileA + PB * tb));
     g.SA = std::min(kMaxRing / PA, depth) * PA;
@@ -1043,11 +1164,12 @@ cudaError_t contract_parts(stacklstm_op *op, const Operand &a, const Operand &b,
     g.ep = ep;
     cudaError_t e = cudaErrorInvalidValue;
     if constexpr (!A_MN && !B_MN)
-        if (bn == 32) e = launch_gemm<32, A_MN, B_MN, PA, PB>(op, a, b, g);
-    if (bn == 64) e = launch_gemm<64, A_MN, B_MN, PA, PB>(op, a, b, g);
-    if (bn == 128) e = launch_gemm<128, A_MN, B_MN, PA, PB>(op, a, b, g);
-    if constexpr (PB == 1)
-        if (bn == 256) e = launch_gemm<256, A_MN, B_MN, PA, PB>(op, a, b, g);
+        if (bn == 32) e = launch_gemm<32, A_MN, B_MN, PA, PB, 1>(op, a, b, g);
+    if (bn == 64) e = launch_gemm<64, A_MN, B_MN, PA, PB, 1>(op, a, b, g);
+    if (bn == 128) e = launch_gemm<128, A_MN, B_MN, PA, PB, 1>(op, a, b, g);
+    if (bn == 256 && plan.cg == 2) e = launch_gemm<256, A_MN, B_MN, PA, PB, 2>(op, a, b, g);
+    if constexpr (PB == 1)  // (three parts of a 256-wide B leave one CTA's rings no second chunk)
+        if (bn == 256 && plan.cg == 1) e = launch_gemm<256, A_MN, B_MN, PA, PB, 1>(op, a, b, g);
     if (!e && g.split > 1) {
         const unsigned ctas = (unsigned)std::min<size_t>(ceil_div((size_t)ep.rows * ep.cols, 256), (size_t)op->num_sms * 8);
         e = launch_after(join_splits, ctas, 256, 0, op->stream, ep, g.split);
@@ -1113,6 +1235,7 @@ sl_status stacklstm_linear_create(stacklstm_op_t *out, int R, int K, int N, sl_d
     op->R = R; op->K = K; op->N = N; op->act = act;
     OpDevice guard(device);
     const size_t counts = ceil_div(N, kDzCols) * 4;
+    op->pairs = most_pairs();
     if (op_workspace(op, kWsCount, counts) || cudaMemset(op->ws[kWsCount], 0, counts)) {
         cudaGetLastError();
         stacklstm_op_destroy(op);

@@ -23,6 +23,7 @@ struct stacklstm_op {
     sl_dtype dt = SL_FP32;
     int R = 0;                         // most rows of a call (beam: B * K)
     int N = 0, K = 0, act = 0;         // norm: N; linear: x [R][K], W [N][K]
+    int pairs = 0;                     // linear: pairs of CTAs that run at once
     int V = 0, k = 0;                  // distill: classes, teacher entries a row; beam: V
     int B = 0, beams = 0, S = 0, H = 0;  // beam
     int32_t *err = nullptr;            // device-detected status (first error wins)
@@ -79,19 +80,28 @@ inline const char *check_pointers(std::initializer_list<const void *> need, std:
 // memory, so the order on the stream is that of plain launches; what is saved is
 // the start of a kernel, one to two microseconds of the short calls.
 template <typename... P, typename... A>
-inline cudaError_t launch_after(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, A &&...args)
+inline cudaError_t launch_cluster(void (*kernel)(P...), unsigned cluster, dim3 grid, unsigned threads, size_t smem, cudaStream_t st,
+                                  A &&...args)
 {
-    cudaLaunchAttribute attr = {};
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchAttribute attr[2] = {};
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...);
+}
+template <typename... P, typename... A>
+inline cudaError_t launch_after(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, A &&...args)
+{
+    return launch_cluster(kernel, 1, grid, threads, smem, st, std::forward<A>(args)...);
 }
 __device__ __forceinline__ void after_previous()
 {

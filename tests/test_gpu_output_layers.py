@@ -148,6 +148,17 @@ def test_linear_forward_activations(dt, name):
     linear_forward(dt, 70, 40, 90, name)
 
 
+# sizes at which pairs of CTAs share a tile: of the forward, of dx and of dW, whole and ragged
+WIDE = [(20001, 136, 330), (9001, 264, 330), (130, 2050, 5000), (300, 2048, 4000)]
+
+
+@TYPES
+@pytest.mark.parametrize("R,K,N", WIDE)
+def test_linear_wide_tiles(dt, R, K, N):
+    linear_forward(dt, R, K, N, "relu")
+    linear_backward(dt, R, K, N, "none")
+
+
 def linear_forward(dt, R, K, N, name):
     rng = np.random.default_rng(R + 31 * K + 977 * N)
     x, xd = rounded(rng, dt, R, K)
