@@ -124,6 +124,7 @@ struct Dz {
     float *dbias;
     int *arrived;           // [column blocks], 0 between calls
     int rows, N, ld, act;
+    int lanes;              // of a warp to a row: 32, or as few (a power of 2) as four columns each fill
     unsigned row_blocks, ctas;
 };
 struct Prepare {
@@ -132,7 +133,7 @@ struct Prepare {
 };
 
 constexpr int kPackItems = 4;  // groups of four columns a thread
-constexpr int kDzCols = 128, kDzRows = 64, kDzSub = 8;
+constexpr int kDzCols = 128, kDzRows = 64, kDzSub = 8;  // a block's columns at most, its rows, its warps
 
 // Groups of four columns, 8 bytes a part. (The groups of `out` follow one another whatever the rows'
 // length is; those of src do where its rows are as long.)
@@ -191,17 +192,18 @@ __device__ __forceinline__ void pack_block(const Pack &a, unsigned cta)
     }
 }
 
-// dz of kDzRows rows and kDzCols columns, and the column sums of it. A lane takes four columns (one
-// 8-byte store a part, from one 16-byte read where the rows of dy start on 16 bytes), warp w the
-// rows w, w + 8, ... of the block, four at a time; the eight warps' sums are added in order, and the
-// last block of a column block to end adds the blocks' sums: parts w, w + 8, ... by warp w, then the
-// eight in order. HBM-bound: 4 + 6 bytes an element.
-template <typename T>
+// dz of kDzRows rows and up to kDzCols columns, and the column sums of it. A lane takes four columns
+// (one 8-byte store a part, from one 16-byte read where the rows of dy start on 16 bytes), a.lanes of
+// them a row (a warp several rows of a narrow layer), four rows at a time; the threads' sums of a
+// column are added in order, and so are, by the last block of a column block to end, the blocks'.
+// HBM-bound: 4 + 6 bytes an element.
+template <typename T, int LANES>  // (0: a.lanes)
 __device__ __forceinline__ void dz_block(const Dz &a, unsigned cta)
 {
-    __shared__ float4 sm[kDzSub][32];
+    __shared__ float4 sm[32 * kDzSub];
     __shared__ int last;
-    const int lane = threadIdx.x & 31, sub = threadIdx.x >> 5, N = a.N;
+    const int lanes = LANES ? LANES : a.lanes;
+    const int N = a.N, lane = threadIdx.x % lanes, sub = threadIdx.x / lanes, subs = 32 * kDzSub / lanes;
     const unsigned rb = cta % a.row_blocks, cb = cta / a.row_blocks;
     const int c = (int)cb * kDzCols + lane * 4, nc = min(4, N - c);
     const int r0 = (int)rb * kDzRows, r1 = min(a.rows, r0 + kDzRows);
@@ -210,11 +212,11 @@ __device__ __forceinline__ void dz_block(const Dz &a, unsigned cta)
     const T *pre = (const T *)a.pre;
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (nc > 0) {
-        for (int r = r0 + sub; r < r1; r += 4 * kDzSub) {
+        for (int r = r0 + sub; r < r1; r += 4 * subs) {
             float v[4][4], z[4][4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int ri = r + i * kDzSub;
+                const int ri = r + i * subs;
                 const size_t at = (size_t)ri * N + c;
                 if (quads) {
                     const float4 q = ri < r1 ? *(const float4 *)(a.dy + at) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -228,7 +230,7 @@ __device__ __forceinline__ void dz_block(const Dz &a, unsigned cta)
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int ri = r + i * kDzSub;
+                const int ri = r + i * subs;
                 if (ri >= r1) break;
                 union {
                     __nv_bfloat16 b[4];
@@ -250,14 +252,15 @@ __device__ __forceinline__ void dz_block(const Dz &a, unsigned cta)
         }
     }
     if (!a.part) return;
-    auto eight = [&](const float4 &mine) {  // the warps' sums in order, to warp 0
-        sm[sub][lane] = mine;
+    // the threads' sums of each column in order, to the first `lanes` threads
+    auto joined = [&](const float4 &mine) {
+        sm[threadIdx.x] = mine;
         __syncthreads();
         float4 t = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (sub == 0)
-#pragma unroll
-            for (int i = 0; i < kDzSub; ++i) {
-                const float4 q = sm[i][lane];
+#pragma unroll 8
+            for (int i = 0; i < subs; ++i) {
+                const float4 q = sm[i * lanes + lane];
                 t.x += q.x; t.y += q.y; t.z += q.z; t.w += q.w;
             }
         return t;
@@ -268,24 +271,24 @@ __device__ __forceinline__ void dz_block(const Dz &a, unsigned cta)
         for (int j = 0; j < 4; ++j)
             if (j < nc) to[j] = w[j];
     };
-    float4 t = eight(make_float4(sum[0], sum[1], sum[2], sum[3]));
+    float4 t = joined(make_float4(sum[0], sum[1], sum[2], sum[3]));
     if (sub == 0) {
         put(a.part + (size_t)rb * N + c, t);
         __threadfence();
-        __syncwarp();
-        if (lane == 0) last = atomicAdd(&a.arrived[cb], 1) == (int)a.row_blocks - 1;
     }
+    __syncthreads();
+    if (threadIdx.x == 0) last = atomicAdd(&a.arrived[cb], 1) == (int)a.row_blocks - 1;
     __syncthreads();
     if (!last) return;
     __threadfence();
     if (threadIdx.x == 0) a.arrived[cb] = 0;  // for the next call
     float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-    for (unsigned s = sub; s < a.row_blocks; s += kDzSub)
+#pragma unroll 8
+    for (unsigned s = sub; s < a.row_blocks; s += subs)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             if (j < nc) acc[j] += __ldcg(a.part + (size_t)s * N + c + j);
-    t = eight(make_float4(acc[0], acc[1], acc[2], acc[3]));
+    t = joined(make_float4(acc[0], acc[1], acc[2], acc[3]));
     if (sub == 0) put(a.dbias + c, t);
 }
 
@@ -295,7 +298,7 @@ prepare(const __grid_constant__ Prepare a)
 {
     after_previous();
     unsigned cta = blockIdx.x;
-    if (cta < a.dz.ctas) return dz_block<T>(a.dz, cta);
+    if (cta < a.dz.ctas) return a.dz.lanes == 32 ? dz_block<T, 32>(a.dz, cta) : dz_block<T, 0>(a.dz, cta);
     cta -= a.dz.ctas;
     if (cta < a.x.ctas) return pack_block<T>(a.x, cta);
     pack_block<T>(a.w, cta - a.x.ctas);
@@ -418,23 +421,48 @@ __device__ __forceinline__ const float *staged(const float *stage, int r, int c)
     return stage + r * 32 + (((c >> 2) ^ (r & 7)) << 2) + (c & 3);
 }
 
-// Those sums (row 0 = output row r0, column 0 = output column n0) to the output, a row's
-// neighbours by neighbouring lanes; what is added is read four rows ahead of the stores.
-template <int SEG, typename Out>
-__device__ __forceinline__ void put_rows(const Out &o, const float *stage, int lane, int r0, int n0, int rows, int cols,
-                                         const float *bias_p)
+// Those sums (row 0 = output row r0, column 0 = output column n0) to an output of any number of
+// columns, a row's neighbours by neighbouring lanes; what is added is read eight rows ahead of the
+// stores.
+template <int SEG, typename T, bool FORWARD, int ACT>
+__device__ __forceinline__ void put_rows(const float *stage, int lane, int r0, int n0, int rows, int cols, const float *bias_p,
+                                         const T *extra_p, T *y, T *pre)
 {
     const int n = n0 + lane;
     if (lane >= SEG || n >= cols) return;
-    const float bias = bias_p ? bias_p[n] : 0.0f;
+    const float bias = FORWARD && bias_p ? bias_p[n] : 0.0f;
     const int m = min(32, rows - r0);
-    for (int i0 = 0; i0 < m; i0 += 4) {
-        float extra[4];
+    size_t at = (size_t)r0 * cols + n;
+#pragma unroll 1
+    for (int i0 = 0; i0 < m; i0 += 8, at += 8 * (size_t)cols) {
+        float extra[8] = {};
+        if (extra_p)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) extra[i] = i0 + i < m ? o.extra((size_t)(r0 + i0 + i) * cols + n) : 0.0f;
+            for (int i = 0; i < 8; ++i)
+                if (i0 + i < m) extra[i] = to_f32(extra_p[at + i * (size_t)cols]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i0 + i < m) o.put((size_t)(r0 + i0 + i) * cols + n, *staged(stage, i0 + i, lane), bias, extra[i]);
+        for (int i = 0; i < 8; ++i)
+            if (i0 + i < m) {
+                float v = *staged(stage, i0 + i, lane) + bias;
+                if (FORWARD) {
+                    if (pre) pre[at + i * (size_t)cols] = from_f32<T>(v);
+                    v = sizeof(T) == 2 ? act_f_bf16(v, ACT) : act_f(v, ACT);
+                }
+                y[at + i * (size_t)cols] = from_f32<T>(v + extra[i]);
+            }
+    }
+}
+template <int SEG, typename T>
+__device__ __forceinline__ void put_rows_forward(const Epilogue &ep, const float *stage, int lane, int r0, int n0)
+{
+    const T *res = (const T *)ep.residual;
+    T *y = (T *)ep.y, *pre = (T *)ep.pre;
+    switch (ep.act) {
+    case kActRelu: return put_rows<SEG, T, true, kActRelu>(stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
+    case kActTanh: return put_rows<SEG, T, true, kActTanh>(stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
+    case kActGelu: return put_rows<SEG, T, true, kActGelu>(stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
+    case kActSilu: return put_rows<SEG, T, true, kActSilu>(stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
+    default: return put_rows<SEG, T, true, kActNone>(stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
     }
 }
 
@@ -555,12 +583,12 @@ __device__ __forceinline__ bool put_tile(const StageIn &in, const Epilogue &ep, 
                 put_cols<SEG>(Forward<float>(ep), stage, lane, n0, m0, ep.rows, ep.cols, ep.bias);
         } else {
             if (plain)
-                put_rows<SEG>(p, stage, lane, m0, n0, ep.rows, ep.cols, nullptr);
+                put_rows<SEG, float, false, kActNone>(stage, lane, m0, n0, ep.rows, ep.cols, nullptr, p.add, p.out, nullptr);
             else if constexpr (!GRADIENT) {
                 if (ep.bf16_out)
-                    put_rows<SEG>(Forward<__nv_bfloat16>(ep), stage, lane, m0, n0, ep.rows, ep.cols, ep.bias);
+                    put_rows_forward<SEG, __nv_bfloat16>(ep, stage, lane, m0, n0);
                 else
-                    put_rows<SEG>(Forward<float>(ep), stage, lane, m0, n0, ep.rows, ep.cols, ep.bias);
+                    put_rows_forward<SEG, float>(ep, stage, lane, m0, n0);
             }
         }
         __syncwarp();
@@ -1004,8 +1032,18 @@ __device__ __forceinline__ void join(const Epilogue &ep, int split, const Out &o
     const size_t n = (size_t)ep.rows * ep.cols;
     for (size_t e = blockIdx.x * (size_t)256 + threadIdx.x; e < n; e += (size_t)gridDim.x * 256) {
         float v = 0.0f;
+        if (n < (size_t)1 << 15) {  // few threads: the reads of sixteen in flight
+            for (int s0 = 0; s0 < split; s0 += 16) {
+                float w[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) w[i] = s0 + i < split ? ep.part[(size_t)(s0 + i) * n + e] : 0.0f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v += w[i];
+            }
+        } else {
 #pragma unroll 4
-        for (int s = 0; s < split; ++s) v += ep.part[(size_t)s * n + e];
+            for (int s = 0; s < split; ++s) v += ep.part[(size_t)s * n + e];
+        }
         o.put(e, v, ep.bias ? ep.bias[e % ep.cols] : 0.0f, o.extra(e));
     }
 }
@@ -1300,6 +1338,7 @@ sl_status stacklstm_linear_backward(stacklstm_op_t op, int rows, const float *dy
         p.dz.dy = dy; p.dz.pre = pre; p.dz.out = (__nv_bfloat16 *)dz.p; p.dz.part = dbias ? (float *)op->ws[kWsSum] : nullptr;
         p.dz.dbias = dbias; p.dz.arrived = (int *)op->ws[kWsCount]; p.dz.rows = rows; p.dz.N = N; p.dz.ld = dz.ld; p.dz.act = op->act;
         p.dz.ctas = p.dz.row_blocks * ceil_div(N, kDzCols);
+        for (p.dz.lanes = 32; p.dz.lanes > 1 && 2 * N <= 4 * p.dz.lanes; p.dz.lanes /= 2) {}
         e = launch_prepare(op, p);
     }
     if (!e && dx) {
