@@ -464,18 +464,21 @@ def stacklstm_norm_create(R: int, N: int, dtype: int, device: int = 0, stream=No
 def stacklstm_norm_forward(hd, x, gamma, beta, eps, y, mean=None, rstd=None):
     """y = (x - mean) rstd gamma + beta, row by row; see include/stacklstm.h for layouts."""
     r, N, d, dt, f = _rows(hd, x, "x"), hd.N, hd.device, hd.tdtype, _f32
-    args = [_arg(x, d, dt, (r, N), "x"), _arg(gamma, d, f, (N,), "gamma"), _arg(beta, d, f, (N,), "beta"), eps,
-            _arg(y, d, dt, (r, N), "y"), _arg(mean, d, f, (r,), "mean"), _arg(rstd, d, f, (r,), "rstd")]
-    _check_op(hd.h, load().stacklstm_norm_forward(hd.h, r, *args), "stacklstm_norm_forward")
+    st = _lib.stacklstm_norm_forward(hd.h, r, _arg(x, d, dt, (r, N), "x"), _arg(gamma, d, f, (N,), "gamma"),
+        _arg(beta, d, f, (N,), "beta"), eps, _arg(y, d, dt, (r, N), "y"), _arg(mean, d, f, (r,), "mean"),
+        _arg(rstd, d, f, (r,), "rstd"))
+    if st:
+        _check_op(hd.h, st, "stacklstm_norm_forward")
 
 
 def stacklstm_norm_backward(hd, dy, x, gamma, mean, rstd, dx=None, dgamma=None, dbeta=None):
     """Gradients of the layer norm; overwritten."""
     r, N, d, f = _rows(hd, dy, "dy"), hd.N, hd.device, _f32
-    args = [_arg(dy, d, f, (r, N), "dy"), _arg(x, d, hd.tdtype, (r, N), "x"), _arg(gamma, d, f, (N,), "gamma"),
-            _arg(mean, d, f, (r,), "mean"), _arg(rstd, d, f, (r,), "rstd"), _arg(dx, d, f, (r, N), "dx"),
-            _arg(dgamma, d, f, (N,), "dgamma"), _arg(dbeta, d, f, (N,), "dbeta")]
-    _check_op(hd.h, load().stacklstm_norm_backward(hd.h, r, *args), "stacklstm_norm_backward")
+    st = _lib.stacklstm_norm_backward(hd.h, r, _arg(dy, d, f, (r, N), "dy"), _arg(x, d, hd.tdtype, (r, N), "x"),
+        _arg(gamma, d, f, (N,), "gamma"), _arg(mean, d, f, (r,), "mean"), _arg(rstd, d, f, (r,), "rstd"),
+        _arg(dx, d, f, (r, N), "dx"), _arg(dgamma, d, f, (N,), "dgamma"), _arg(dbeta, d, f, (N,), "dbeta"))
+    if st:
+        _check_op(hd.h, st, "stacklstm_norm_backward")
 
 
 def stacklstm_linear_create(R: int, K: int, N: int, dtype: int, act: int = SL_ACT_NONE, device: int = 0, stream=None):
@@ -486,18 +489,21 @@ def stacklstm_linear_create(R: int, K: int, N: int, dtype: int, act: int = SL_AC
 def stacklstm_linear_forward(hd, x, W, bias, residual, y, pre=None):
     """y = act(x W^T + bias) + residual; see include/stacklstm.h for layouts."""
     r, K, N, d, dt = _rows(hd, x, "x"), hd.K, hd.N, hd.device, hd.tdtype
-    args = [_arg(x, d, dt, (r, K), "x"), _arg(W, d, dt, (N, K), "W"), _arg(bias, d, _f32, (N,), "bias"),
-            _arg(residual, d, dt, (r, N), "residual"), _arg(y, d, dt, (r, N), "y"), _arg(pre, d, dt, (r, N), "pre")]
-    _check_op(hd.h, load().stacklstm_linear_forward(hd.h, r, *args), "stacklstm_linear_forward")
+    st = _lib.stacklstm_linear_forward(hd.h, r, _arg(x, d, dt, (r, K), "x"), _arg(W, d, dt, (N, K), "W"),
+        _arg(bias, d, _f32, (N,), "bias"), _arg(residual, d, dt, (r, N), "residual"), _arg(y, d, dt, (r, N), "y"),
+        _arg(pre, d, dt, (r, N), "pre"))
+    if st:
+        _check_op(hd.h, st, "stacklstm_linear_forward")
 
 
 def stacklstm_linear_backward(hd, dy, x, W, pre=None, add=None, dx=None, dW=None, dbias=None):
     """Gradients of the linear layer; overwritten (dx includes ``add``)."""
     r, K, N, d, dt, f = _rows(hd, dy, "dy"), hd.K, hd.N, hd.device, hd.tdtype, _f32
-    args = [_arg(dy, d, f, (r, N), "dy"), _arg(x, d, dt, (r, K), "x"), _arg(W, d, dt, (N, K), "W"),
-            _arg(pre, d, dt, (r, N), "pre"), _arg(add, d, f, (r, K), "add"), _arg(dx, d, f, (r, K), "dx"),
-            _arg(dW, d, f, (N, K), "dW"), _arg(dbias, d, f, (N,), "dbias")]
-    _check_op(hd.h, load().stacklstm_linear_backward(hd.h, r, *args), "stacklstm_linear_backward")
+    st = _lib.stacklstm_linear_backward(hd.h, r, _arg(dy, d, f, (r, N), "dy"), _arg(x, d, dt, (r, K), "x"),
+        _arg(W, d, dt, (N, K), "W"), _arg(pre, d, dt, (r, N), "pre"), _arg(add, d, f, (r, K), "add"),
+        _arg(dx, d, f, (r, K), "dx"), _arg(dW, d, f, (N, K), "dW"), _arg(dbias, d, f, (N,), "dbias"))
+    if st:
+        _check_op(hd.h, st, "stacklstm_linear_backward")
 
 
 def stacklstm_distill_create(R: int, V: int, k: int, dtype: int, device: int = 0, stream=None):
@@ -508,10 +514,12 @@ def stacklstm_distill_create(R: int, V: int, k: int, dtype: int, device: int = 0
 def stacklstm_distill_run(hd, logits, t_idx, t_logit, gold, tau, alpha, scale, loss_rows=None, dlogits=None):
     """Loss rows and the logits' gradient; see include/stacklstm.h for the formulas."""
     r, V, k, d, f = _rows(hd, logits, "logits"), hd.V, hd.k, hd.device, _f32
-    args = [_arg(logits, d, hd.tdtype, (r, V), "logits"), _arg(t_idx, d, _i32, (r, k), "t_idx"),
-            _arg(t_logit, d, f, (r, k), "t_logit"), _arg(gold, d, _i32, (r,), "gold"), tau, alpha, scale,
-            _arg(loss_rows, d, f, (r,), "loss_rows"), _arg(dlogits, d, f, (r, V), "dlogits")]
-    _check_op(hd.h, load().stacklstm_distill_run(hd.h, r, *args), "stacklstm_distill_run")
+    st = _lib.stacklstm_distill_run(hd.h, r, _arg(logits, d, hd.tdtype, (r, V), "logits"),
+        _arg(t_idx, d, _i32, (r, k), "t_idx"), _arg(t_logit, d, f, (r, k), "t_logit"),
+        _arg(gold, d, _i32, (r,), "gold"), tau, alpha, scale, _arg(loss_rows, d, f, (r,), "loss_rows"),
+        _arg(dlogits, d, f, (r, V), "dlogits"))
+    if st:
+        _check_op(hd.h, st, "stacklstm_distill_run")
 
 
 def stacklstm_beam_create(B: int, K: int, V: int, S: int, H: int, dtype: int, device: int = 0, stream=None):
@@ -521,37 +529,43 @@ def stacklstm_beam_create(B: int, K: int, V: int, S: int, H: int, dtype: int, de
 
 def stacklstm_beam_lse(hd, logits, lse):
     B, K, V, d = hd.B, hd.K, hd.V, hd.device
-    _check_op(hd.h, load().stacklstm_beam_lse(hd.h, _arg(logits, d, hd.tdtype, (B, K, V), "logits"),
-                                              _arg(lse, d, _f32, (B, K), "lse")), "stacklstm_beam_lse")
+    st = _lib.stacklstm_beam_lse(hd.h, _arg(logits, d, hd.tdtype, (B, K, V), "logits"),
+        _arg(lse, d, _f32, (B, K), "lse"))
+    if st:
+        _check_op(hd.h, st, "stacklstm_beam_lse")
 
 
 def stacklstm_beam_select(hd, logits, lse, score, done, new_score, parent, token):
     """The K best candidates of each sentence; see include/stacklstm.h."""
     B, K, V, d, f, i = hd.B, hd.K, hd.V, hd.device, _f32, _i32
-    args = [_arg(logits, d, hd.tdtype, (B, K, V), "logits"), _arg(lse, d, f, (B, K), "lse"),
-            _arg(score, d, f, (B, K), "score"), _arg(done, d, _u8, (B, K), "done"),
-            _arg(new_score, d, f, (B, K), "new_score"), _arg(parent, d, i, (B, K), "parent"),
-            _arg(token, d, i, (B, K), "token")]
-    _check_op(hd.h, load().stacklstm_beam_select(hd.h, *args), "stacklstm_beam_select")
+    st = _lib.stacklstm_beam_select(hd.h, _arg(logits, d, hd.tdtype, (B, K, V), "logits"),
+        _arg(lse, d, f, (B, K), "lse"), _arg(score, d, f, (B, K), "score"), _arg(done, d, _u8, (B, K), "done"),
+        _arg(new_score, d, f, (B, K), "new_score"), _arg(parent, d, i, (B, K), "parent"),
+        _arg(token, d, i, (B, K), "token"))
+    if st:
+        _check_op(hd.h, st, "stacklstm_beam_select")
 
 
 def stacklstm_beam_reorder(hd, parent, p, h_stack, c_stack, p_out, h_out, c_out, top_h=None, top_c=None):
     """The stacks of the chosen hypotheses' parents; see include/stacklstm.h."""
     B, K, S, H, d, dt, f, i = hd.B, hd.K, hd.S, hd.H, hd.device, hd.tdtype, _f32, _i32
     N = B * K
-    args = [_arg(parent, d, i, (B, K), "parent"), _arg(p, d, i, (N,), "p"), _arg(h_stack, d, dt, (S, N, H), "h_stack"),
-            _arg(c_stack, d, f, (S, N, H), "c_stack"), _arg(p_out, d, i, (N,), "p_out"),
-            _arg(h_out, d, dt, (S, N, H), "h_out"), _arg(c_out, d, f, (S, N, H), "c_out"),
-            _arg(top_h, d, dt, (N, H), "top_h"), _arg(top_c, d, f, (N, H), "top_c")]
-    _check_op(hd.h, load().stacklstm_beam_reorder(hd.h, *args), "stacklstm_beam_reorder")
+    st = _lib.stacklstm_beam_reorder(hd.h, _arg(parent, d, i, (B, K), "parent"), _arg(p, d, i, (N,), "p"),
+        _arg(h_stack, d, dt, (S, N, H), "h_stack"), _arg(c_stack, d, f, (S, N, H), "c_stack"),
+        _arg(p_out, d, i, (N,), "p_out"), _arg(h_out, d, dt, (S, N, H), "h_out"),
+        _arg(c_out, d, f, (S, N, H), "c_out"), _arg(top_h, d, dt, (N, H), "top_h"),
+        _arg(top_c, d, f, (N, H), "top_c"))
+    if st:
+        _check_op(hd.h, st, "stacklstm_beam_reorder")
 
 
 def stacklstm_beam_push(hd, ops, h_new, c_new, p, h_stack, c_stack, top_h=None, top_c=None):
     """One step of Algorithm 1 on the stacks, in place; see include/stacklstm.h."""
     B, K, S, H, d, dt, f = hd.B, hd.K, hd.S, hd.H, hd.device, hd.tdtype, _f32
     N = B * K
-    args = [_arg(ops, d, _i8, (N,), "ops"), _arg(h_new, d, dt, (N, H), "h_new"), _arg(c_new, d, f, (N, H), "c_new"),
-            _arg(p, d, _i32, (N,), "p"), _arg(h_stack, d, dt, (S, N, H), "h_stack"),
-            _arg(c_stack, d, f, (S, N, H), "c_stack"), _arg(top_h, d, dt, (N, H), "top_h"),
-            _arg(top_c, d, f, (N, H), "top_c")]
-    _check_op(hd.h, load().stacklstm_beam_push(hd.h, *args), "stacklstm_beam_push")
+    st = _lib.stacklstm_beam_push(hd.h, _arg(ops, d, _i8, (N,), "ops"), _arg(h_new, d, dt, (N, H), "h_new"),
+        _arg(c_new, d, f, (N, H), "c_new"), _arg(p, d, _i32, (N,), "p"), _arg(h_stack, d, dt, (S, N, H), "h_stack"),
+        _arg(c_stack, d, f, (S, N, H), "c_stack"), _arg(top_h, d, dt, (N, H), "top_h"),
+        _arg(top_c, d, f, (N, H), "top_c"))
+    if st:
+        _check_op(hd.h, st, "stacklstm_beam_push")

@@ -201,7 +201,7 @@ __device__ __forceinline__ void keys_topk(const u64 (&key)[PT], int K, SelShared
 // (ROWS = false), or NT NI of the V of hypothesis blockIdx.x / per_row. The K best of each
 // segment go to `part`, and the sentence's last CTA joins them.
 template <typename T, bool ROWS, int NT, int NI>
-__global__ void __launch_bounds__(NT, !ROWS || (NT == 512 && sizeof(T) == 4) ? 1 : 1024 / NT)
+__global__ void __launch_bounds__(NT, ROWS ? 2048 / NT : 2)
 beam_select(int K, int V, int nseg, int per_row, const T *__restrict__ z, const float *__restrict__ lse,
             const float *__restrict__ score, const uint8_t *__restrict__ done, u64 *__restrict__ part,
             int *__restrict__ arrived, float *__restrict__ out_score, int32_t *__restrict__ parent,
@@ -217,23 +217,29 @@ beam_select(int K, int V, int nseg, int per_row, const T *__restrict__ z, const 
         s.done[tid] = done ? done[(size_t)b * K + tid] : 0;
     }
     if constexpr (ROWS) {
+        // The segment is read for the threads' largest logits alone; the few threads whose best makes
+        // the bound read their pieces again: at 64 x 8 x 32003 bf16 15.7 us, all CTAs at once (6.5 for
+        // the reading alone); 18 to 20 with the pieces held in registers, two CTAs of 512 an SM.
         constexpr int E = RowVec<T>::E, NP = NI / E;
         const int k = seg / per_row, piece0 = seg % per_row * (NT * NI / E) + tid;
         const RowVec<T> row((size_t)b * K + k, V);
         const int n = row.pieces();
-        uint4 q[NP];
+        float zmax = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < NP; ++j)
-            if (piece0 + j * NT < n) q[j] = row.load(z, piece0 + j * NT);
+        for (int j0 = 0; j0 < NP; j0 += 4) {
+            uint4 q[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (piece0 + (j0 + j) * NT < n) q[j] = row.load(z, piece0 + (j0 + j) * NT);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (piece0 + (j0 + j) * NT < n) zmax = fmaxf(zmax, piece_max<T, false>(q[j]));
+        }
         __syncthreads();
         const float add = s.score[k], sub = s.lse[k];
         const bool is_done = s.done[k];
         const uint32_t place0 = (uint32_t)k * (uint32_t)V;
         // (rounded operations keep the order: the best score is that of the largest logit)
-        float zmax = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < NP; ++j)
-            if (piece0 + j * NT < n) zmax = fmaxf(zmax, piece_max<T, false>(q[j]));
         const auto cand = [&](float v) { return __fadd_rn(add, __fsub_rn(v, sub)); };
         float top = cand(zmax);
         if (is_done) top = seg % per_row == 0 && tid == 0 ? add : -INFINITY;
@@ -243,17 +249,26 @@ beam_select(int K, int V, int nseg, int per_row, const T *__restrict__ z, const 
                 f(make_key(add, place0));
                 return;
             }
+#pragma unroll 1
+            for (int p0 = piece0; p0 < n && p0 < piece0 + NP * NT; p0 += 4 * NT) {
+                uint4 q[4];
+                unsigned hit = 0;  // the pieces with a candidate
 #pragma unroll
-            for (int j = 0; j < NP; ++j)
-                if (piece0 + j * NT < n && cand(piece_max<T, false>(q[j])) >= least) {
-                    float v[E];
-                    unpack<T>(q[j], v);
+                for (int j = 0; j < 4; ++j)
+                    if (p0 + j * NT < n) q[j] = row.load(z, p0 + j * NT);
 #pragma unroll
-                    for (int i = 0; i < E; ++i) {
-                        const float c = cand(v[i]);
-                        if (c >= least && c > -INFINITY) f(make_key(c, place0 + (uint32_t)(row.column(piece0 + j * NT) + i)));
+                for (int j = 0; j < 4; ++j)
+                    if (p0 + j * NT < n && cand(piece_max<T, false>(q[j])) >= least) hit |= 1u << j;
+#pragma unroll 1
+                for (; hit; hit &= hit - 1) {  // (its elements one by one: a copy of the code for each cost more)
+                    const int c0 = row.column(p0 + (__ffs(hit) - 1) * NT);
+#pragma unroll 1
+                    for (int c = max(c0, 0); c < min(c0 + E, V); ++c) {
+                        const float x = cand(to_f32(z[row.first() + c]));
+                        if (x >= least && x > -INFINITY) f(make_key(x, place0 + (uint32_t)c));
                     }
                 }
+            }
         };
         auto best_key = [&] {
             u64 mine = 0;
@@ -298,9 +313,19 @@ beam_select(int K, int V, int nseg, int per_row, const T *__restrict__ z, const 
         if (tid == 0) arrived[b] = 0;  // for the next call
         const u64 *mine = part + (size_t)b * nseg * K;
         const int total = nseg * K, step = NT * (kMergeItems - 1);
+        __syncthreads();  // (every thread has read its best of the segment)
         if (tid < K) s.best[tid] = 0;
-        __syncthreads();
-        for (int at = 0; at < total; at += step) {
+        if (total <= NT) {  // few: all of them against one another
+            const u64 key = tid < total ? __ldcg(mine + tid) : 0;
+            s.top[tid] = key;
+            __syncthreads();
+            int above = 0;
+            if (key)
+                for (int i = 0; i < total; ++i) above += s.top[i] > key;
+            if (key && above < K) s.best[above] = key;
+            __syncthreads();
+        }
+        for (int at = 0; total > NT && at < total; at += step) {
             u64 key[kMergeItems];
 #pragma unroll
             for (int i = 0; i < kMergeItems - 1; ++i) {
@@ -328,8 +353,8 @@ beam_select(int K, int V, int nseg, int per_row, const T *__restrict__ z, const 
 
 // Segments of a sentence: by rows where a row fills most of a CTA's threads, else across the rows
 // (8 x 83 candidates are one CTA's; by rows they would be eight, and their join). Larger CTAs where
-// the small ones would be more than run at once four to an SM: 64 x 8 x 32003 bf16 25 us in 2048
-// CTAs, 15 in 512.
+// the small ones would be more than run at once four to an SM: 64 x 8 x 32003 bf16 23 us in 2048
+// CTAs, 16 in 512.
 struct SelPlan {
     bool rows, large;
     int per_row, nseg;
