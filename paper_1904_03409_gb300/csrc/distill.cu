@@ -79,6 +79,16 @@ __device__ __forceinline__ void add_entry(const Entries &e, int j, float top, fl
     e.w[j] = w;
 }
 
+// Two neighbours at a time, each rounded as one alone: the differences from m, and 2^(d k). (The
+// logits less m times k as one operation, k z - k m, would not hold for masks of the type's lowest
+// value, where k m overflows.)
+__device__ __forceinline__ float2 less2(float a, float b, float m) { return __fadd2_rn(make_float2(a, b), make_float2(-m, -m)); }
+__device__ __forceinline__ float2 exp2_2(float2 d, float k)
+{
+    const float2 x = __fmul2_rn(d, make_float2(k, k));
+    return make_float2(exp2_hw(x.x), exp2_hw(x.y));
+}
+
 // What a row's outputs are made of.
 struct Row {
     float m, wt, w1;   // gradient: wt exp((z - m) / tau) + w1 exp(z - m)
@@ -119,9 +129,12 @@ struct Row {
     {
         if (soft && hard) {
 #pragma unroll
-            for (int i = 0; i < E; ++i) {
-                const float d = v[i] - m;
-                g[i] = fmaf(w1, exp2_hw(d * kLog2e), wt * exp2_hw(d * k2));
+            for (int i = 0; i < E; i += 2) {
+                const float2 d = less2(v[i], v[i + 1], m);
+                const float2 x = __ffma2_rn(make_float2(w1, w1), exp2_2(d, kLog2e),
+                                            __fmul2_rn(make_float2(wt, wt), exp2_2(d, k2)));
+                g[i] = x.x;
+                g[i + 1] = x.y;
             }
         } else {
             const float kk = soft ? k2 : kLog2e, w = soft ? wt : w1;
@@ -230,8 +243,9 @@ distill_narrow(const __grid_constant__ DistillArgs a)
 
 // Wider rows: a CTA of TPR threads a row, the row read twice, the second time from the caches. A
 // thread keeps its own maximum and the sums against it, so that the first reading is one pass; 1536
-// threads an SM hide one another's latencies. At 4096 x 32003 bf16: 159 us with 512 threads a row
-// (5.0 TB/s), 164 with 256, 186 with 128; 182 with the row held in the registers of 512 threads, two
+// threads an SM hide one another's latencies. At 4096 x 32003 bf16: 153 us with 512 threads a row
+// (5.1 TB/s), two elements at a time; one at a time 156 (the warps' issue is what bounds it next to
+// HBM). When all forms took one at a time: 159 with 512 threads a row, 164 with 256, 186 with 128; 182 with the row held in the registers of 512 threads, two
 // CTAs an SM, and no less with the next row on its way to shared memory: the barriers and the
 // entries' part of each row were not hidden.
 template <typename T, int TPR>
@@ -257,13 +271,16 @@ distill_wide(const __grid_constant__ DistillArgs a)
     const int gold = read_gold(a, r, t == 0);
     const float zgold = t == 0 && gold >= 0 ? to_f32(zr[gold]) : 0.0f;
     // the first pass, four pieces in flight; m: this thread's maximum, s2 and s1 against it
-    float m = -INFINITY, s2 = 0.0f, s1 = 0.0f;
+    // for even and odd elements apart
+    float m = -INFINITY;
+    float2 s2 = {0.0f, 0.0f}, s1 = {0.0f, 0.0f};
     auto add = [&](const uint4 &q) {
         const float pm = piece_max<T, true>(q);
         if (!(pm <= m)) {  // a new maximum (or NaN)
             const float d = m - pm;  // (-inf at first: the sums are 0)
-            s2 *= exp2_hw(d * k2);
-            s1 *= exp2_hw(d * kLog2e);
+            const float c2 = exp2_hw(d * k2), c1 = exp2_hw(d * kLog2e);
+            s2 = __fmul2_rn(s2, make_float2(c2, c2));
+            s1 = __fmul2_rn(s1, make_float2(c1, c1));
             m = pm;
         }
         if (m == -INFINITY) return;  // nothing yet
@@ -271,18 +288,18 @@ distill_wide(const __grid_constant__ DistillArgs a)
         unpack<T>(q, v);
         if (want2 && want1) {
 #pragma unroll
-            for (int i = 0; i < E; ++i) {
-                const float d = v[i] - m;
-                s2 += exp2_hw(d * k2);
-                s1 += exp2_hw(d * kLog2e);
+            for (int i = 0; i < E; i += 2) {
+                const float2 d = less2(v[i], v[i + 1], m);
+                s2 = __fadd2_rn(s2, exp2_2(d, k2));
+                s1 = __fadd2_rn(s1, exp2_2(d, kLog2e));
             }
         } else {
             const float kk = want2 ? k2 : kLog2e;
-            float s = 0.0f;
+            float2 s = {0.0f, 0.0f};
 #pragma unroll
-            for (int i = 0; i < E; ++i) s += exp2_hw((v[i] - m) * kk);
-            if (want2) s2 += s;
-            else s1 += s;
+            for (int i = 0; i < E; i += 2) s = __fadd2_rn(s, exp2_2(less2(v[i], v[i + 1], m), kk));
+            if (want2) s2 = __fadd2_rn(s2, s);
+            else s1 = __fadd2_rn(s1, s);
         }
     };
     for (int p = t; p < n; p += 4 * TPR) {
@@ -300,8 +317,8 @@ distill_wide(const __grid_constant__ DistillArgs a)
     const float rtau = 1.0f / a.tau;
     float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (m > -INFINITY || isnan(m)) {  // this thread's sums against the row's maximum
-        s[2] = s2 * exp2_hw((m - w.m) * k2);
-        s[3] = s1 * exp2_hw((m - w.m) * kLog2e);
+        s[2] = (s2.x + s2.y) * exp2_hw((m - w.m) * k2);
+        s[3] = (s1.x + s1.y) * exp2_hw((m - w.m) * kLog2e);
     }
     if (w.soft)
         for (int j = t; j < a.k; j += TPR) add_entry(e, j, top[1], w.m, rtau, s[0], s[1]);
