@@ -435,7 +435,8 @@ typedef enum { SL_ACT_NONE = 0, SL_ACT_RELU = 1, SL_ACT_TANH = 2, SL_ACT_GELU = 
  * 2^-23 of the leading one are left out: results have fp32 accuracy. A value that is not
  * finite makes the outputs it enters not finite (inf may become NaN).
  * The first backward allocates 6 rows N bytes of workspace (and 4 rows N / 64 for dbias);
- * SL_FP32 6 (rows + N) K for the parts.
+ * SL_FP32 6 (rows + N) K for the parts. Where the outputs are few and the contraction long, a
+ * call splits it and allocates the splits' partial sums, 4 bytes an output and split, 1 GiB at most.
  */
 sl_status stacklstm_linear_create(stacklstm_op_t *out, int R, int K, int N, sl_dtype dtype, sl_act act, int device,
                                   void *stream);

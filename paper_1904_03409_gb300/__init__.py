@@ -5,7 +5,8 @@ instance of a minibatch runs the same step whatever its stack op (Algorithm 1), 
 whole batch is one gate contraction per step. The kernels live in ``csrc/`` and are
 reached through the C ABI of ``include/stacklstm.h``; ``binding`` is its thin Python
 binding, ``runner`` moves synthetic workloads to and from the device, ``workloads``
-draws them.
+draws them, ``output_layers`` puts norm, linear layers, distillation and beam search on the
+step outputs.
 """
 from .binding import (SL_BF16, SL_FP32, StackLSTMError, StackLSTMHandle, load, stacklstm_backward,
                       stacklstm_create, stacklstm_destroy, stacklstm_forward, stacklstm_set_async,

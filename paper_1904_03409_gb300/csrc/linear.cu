@@ -292,6 +292,7 @@ __device__ __forceinline__ void dz_block(const Dz &a, unsigned cta)
     if (sub == 0) put(a.dbias + c, t);
 }
 
+// Bound by HBM: dz of 4096 x 32003 is read as 4 bytes and written as 6 in 245 us (5.4 TB/s).
 template <typename T>
 __global__ void __launch_bounds__(256)
 prepare(const __grid_constant__ Prepare a)
@@ -386,30 +387,23 @@ struct Plain {
     __device__ __forceinline__ void put(size_t at, float v, float, float extra) const { out[at] = v + extra; }
 };
 
-// W (2 or 4) neighbours in one access.
-template <int W>
-__device__ __forceinline__ void store_w(float *p, const float (&v)[W])
-{
-    if constexpr (W == 4)
-        *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]);
-    else
-        *(float2 *)p = make_float2(v[0], v[1]);
-}
-template <int W>
-__device__ __forceinline__ void store_w(__nv_bfloat16 *p, const float (&v)[W])
+// Four neighbours in one access.
+constexpr int kFew = 4;
+__device__ __forceinline__ void store_few(float *p, const float (&v)[kFew]) { *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]); }
+__device__ __forceinline__ void store_few(__nv_bfloat16 *p, const float (&v)[kFew])
 {
     union {
-        __nv_bfloat162 b[W / 2];
-        typename std::conditional<W == 4, uint2, uint32_t>::type q;
+        __nv_bfloat162 b[2];
+        uint2 q;
     } o;
-#pragma unroll
-    for (int i = 0; i < W / 2; ++i) o.b[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-    *(decltype(o.q) *)p = o.q;
+    o.b[0] = __floats2bfloat162_rn(v[0], v[1]);
+    o.b[1] = __floats2bfloat162_rn(v[2], v[3]);
+    *(uint2 *)p = o.q;
 }
 // The same as it lies in memory, and its values.
-template <typename T, int W>
+template <typename T>
 struct Few {
-    using Q = typename std::conditional<sizeof(T) * W == 16, float4, typename std::conditional<sizeof(T) * W == 8, float2, float>::type>::type;
+    using Q = typename std::conditional<sizeof(T) == 4, float4, uint2>::type;
     Q q;
     __device__ __forceinline__ void load(const T *p) { q = *(const Q *)p; }
     __device__ __forceinline__ float get(int i) const { return to_f32(((const T *)&q)[i]); }
@@ -485,19 +479,19 @@ __device__ __forceinline__ void put_cols(const Out &o, const float *stage, int l
     }
 }
 
-// A warp's 32 rows x 32 NSEG columns of an output whose number of columns W (2 or 4) divides: W
-// neighbours a lane, W rows at a time; stage_in(seg) brings 32 columns of sums into `stage` (false: a
+// A warp's 32 rows x 32 NSEG columns of an output whose number of columns 4 divides: four
+// neighbours a lane, four rows at a time; stage_in(seg) brings 32 columns of sums into `stage` (false: a
 // wait ran out). What is added to a block of 32 columns (residual, add) is read while the block
 // before it is worked on, the first one's while the sums are waited for, and rows are finished a few
 // at a time (more of them keep more activations in flight than there are registers).
-template <typename T, int W, bool FORWARD, int ACT, int NSEG, typename StageIn>
-__device__ __forceinline__ bool put_w(const StageIn &stage_in, const float *stage, int lane, int r0, int n0, int rows, int cols,
-                                      const float *bias_p, const T *extra_p, T *y, T *pre)
+template <typename T, bool FORWARD, int ACT, int NSEG, typename StageIn>
+__device__ __forceinline__ bool put_few(const StageIn &stage_in, const float *stage, int lane, int r0, int n0, int rows, int cols,
+                                        const float *bias_p, const T *extra_p, T *y, T *pre)
 {
-    constexpr int L = 32 / W, NI = 32 / W;  // lanes a row; steps of W rows
+    constexpr int W = kFew, L = 32 / W, NI = 32 / W;  // lanes a row; steps of W rows
     const int j = lane % L * W, sub = lane / L, m = min(32, rows - r0);
     const size_t step = W * (size_t)cols, first = (size_t)(r0 + sub) * cols + n0 + j;
-    Few<T, W> next[NI] = {}, extra[NI];
+    Few<T> next[NI] = {}, extra[NI];
     auto fetch = [&](int seg) {
         if (n0 + seg * 32 + j < cols)
 #pragma unroll
@@ -522,18 +516,18 @@ __device__ __forceinline__ bool put_w(const StageIn &stage_in, const float *stag
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
                 if (sub + W * i < m) {
-                    Few<float, W> s;
+                    Few<float> s;
                     s.load(staged(stage, sub + W * i, j));
                     float v[W];
 #pragma unroll
                     for (int k = 0; k < W; ++k) v[k] = s.get(k) + (FORWARD ? bias[k] : 0.0f);
-                    if (FORWARD && pre) store_w<W>(pre + at + i * step, v);
+                    if (FORWARD && pre) store_few(pre + at + i * step, v);
 #pragma unroll
                     for (int k = 0; k < W; ++k) {
                         if (FORWARD) v[k] = sizeof(T) == 2 ? act_f_bf16(v[k], ACT) : act_f(v[k], ACT);
                         v[k] += extra[i].get(k);
                     }
-                    store_w<W>(y + at + i * step, v);
+                    store_few(y + at + i * step, v);
                 }
                 if (i % (8 / W) == 8 / W - 1) asm volatile("" ::: "memory");
             }
@@ -542,17 +536,17 @@ __device__ __forceinline__ bool put_w(const StageIn &stage_in, const float *stag
     }
     return true;
 }
-template <typename T, int W, int NSEG, typename StageIn>
+template <typename T, int NSEG, typename StageIn>
 __device__ __forceinline__ bool put_forward(const StageIn &in, const Epilogue &ep, const float *stage, int lane, int r0, int n0)
 {
     const T *res = (const T *)ep.residual;
     T *y = (T *)ep.y, *pre = (T *)ep.pre;
     switch (ep.act) {
-    case kActRelu: return put_w<T, W, true, kActRelu, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
-    case kActTanh: return put_w<T, W, true, kActTanh, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
-    case kActGelu: return put_w<T, W, true, kActGelu, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
-    case kActSilu: return put_w<T, W, true, kActSilu, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
-    default: return put_w<T, W, true, kActNone, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
+    case kActRelu: return put_few<T, true, kActRelu, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
+    case kActTanh: return put_few<T, true, kActTanh, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
+    case kActGelu: return put_few<T, true, kActGelu, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
+    case kActSilu: return put_few<T, true, kActSilu, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
+    default: return put_few<T, true, kActNone, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
     }
 }
 
@@ -565,10 +559,10 @@ __device__ __forceinline__ bool put_tile(const StageIn &in, const Epilogue &ep, 
     const Plain p = {ep.part ? nullptr : ep.add, ep.part ? ep.part + (size_t)sp * ep.rows * ep.cols : ep.out};
     if (SEG == 32 && ep.cols % 4 == 0 && (GRADIENT || !swapped)) {
         if (plain)
-            return put_w<float, 4, false, kActNone, NSEG>(in, stage, lane, m0, n0, ep.rows, ep.cols, nullptr, p.add, p.out, nullptr);
+            return put_few<float, false, kActNone, NSEG>(in, stage, lane, m0, n0, ep.rows, ep.cols, nullptr, p.add, p.out, nullptr);
         if constexpr (!GRADIENT)
-            return ep.bf16_out ? put_forward<__nv_bfloat16, 4, NSEG>(in, ep, stage, lane, m0, n0)
-                               : put_forward<float, 4, NSEG>(in, ep, stage, lane, m0, n0);
+            return ep.bf16_out ? put_forward<__nv_bfloat16, NSEG>(in, ep, stage, lane, m0, n0)
+                               : put_forward<float, NSEG>(in, ep, stage, lane, m0, n0);
     }
 #pragma unroll 1
     for (int seg = 0; seg < NSEG; ++seg, n0 += SEG) {
@@ -706,6 +700,9 @@ __device__ __forceinline__ void prefetch_map(const void *tmap)
 // that fp32 results come from takes few of them (1.7e-8 of the result each: 1e-4 after 6012).
 // A part is loaded once a chunk, whatever number of products it is in, small products first.
 // MN-major operands: blocks of 64 columns, each 64 rows of 128 bytes.
+// Bound by the tensor cores where the contraction is long: both products of the backward at 4096 x
+// 1024 x 32003 bf16, with the 245 us of their parts, 1287 us, as pairs of CTAs on 256 x 256 tiles.
+// Bound by shared memory where it is short: forward 65536 x 1024 x 1024, gelu, residual and pre, 145 us.
 template <int BN, bool A_MN, bool B_MN, int PA, int PB, int EPI, int CG>
 __global__ void __launch_bounds__(gemm_threads(EPI), 1)
 gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
