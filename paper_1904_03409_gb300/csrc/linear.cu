@@ -323,7 +323,8 @@ struct GemmArgs {
     int chunks;             // 64-wide chunks of the contraction
     int per_acc;            // chunks to an accumulator
     int split;              // splits of the chunks
-    int mt, nt;             // tiles
+    int K, N;               // of the contraction, and rows of B
+    int mt, nt, step;       // tiles, and rows of B from one to the next (fp32 results: as few as nt allows)
     int SA, SB;             // ring depths
     int swapped;            // the output's rows are B's rows (few rows: A = W)
     Epilogue ep;
@@ -419,11 +420,11 @@ __device__ __forceinline__ const float *staged(const float *stage, int r, int c)
 // columns, a row's neighbours by neighbouring lanes; what is added is read eight rows ahead of the
 // stores.
 template <int SEG, typename T, bool FORWARD, int ACT>
-__device__ __forceinline__ void put_rows(const float *stage, int lane, int r0, int n0, int rows, int cols, const float *bias_p,
-                                         const T *extra_p, T *y, T *pre)
+__device__ __forceinline__ void put_rows(const float *stage, int lane, int r0, int n0, int n_end, int rows, int cols,
+                                         const float *bias_p, const T *extra_p, T *y, T *pre)
 {
     const int n = n0 + lane;
-    if (lane >= SEG || n >= cols) return;
+    if (lane >= SEG || n >= n_end) return;
     const float bias = FORWARD && bias_p ? bias_p[n] : 0.0f;
     const int m = min(32, rows - r0);
     size_t at = (size_t)r0 * cols + n;
@@ -447,28 +448,28 @@ __device__ __forceinline__ void put_rows(const float *stage, int lane, int r0, i
     }
 }
 template <int SEG, typename T>
-__device__ __forceinline__ void put_rows_forward(const Epilogue &ep, const float *stage, int lane, int r0, int n0)
+__device__ __forceinline__ void put_rows_forward(const Epilogue &ep, const float *stage, int lane, int r0, int n0, int n_end)
 {
     const T *res = (const T *)ep.residual;
     T *y = (T *)ep.y, *pre = (T *)ep.pre;
     switch (ep.act) {
-    case kActRelu: return put_rows<SEG, T, true, kActRelu>(stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
-    case kActTanh: return put_rows<SEG, T, true, kActTanh>(stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
-    case kActGelu: return put_rows<SEG, T, true, kActGelu>(stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
-    case kActSilu: return put_rows<SEG, T, true, kActSilu>(stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
-    default: return put_rows<SEG, T, true, kActNone>(stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
+    case kActRelu: return put_rows<SEG, T, true, kActRelu>(stage, lane, r0, n0, n_end, ep.rows, ep.cols, ep.bias, res, y, pre);
+    case kActTanh: return put_rows<SEG, T, true, kActTanh>(stage, lane, r0, n0, n_end, ep.rows, ep.cols, ep.bias, res, y, pre);
+    case kActGelu: return put_rows<SEG, T, true, kActGelu>(stage, lane, r0, n0, n_end, ep.rows, ep.cols, ep.bias, res, y, pre);
+    case kActSilu: return put_rows<SEG, T, true, kActSilu>(stage, lane, r0, n0, n_end, ep.rows, ep.cols, ep.bias, res, y, pre);
+    default: return put_rows<SEG, T, true, kActNone>(stage, lane, r0, n0, n_end, ep.rows, ep.cols, ep.bias, res, y, pre);
     }
 }
 
 // The same of an output that is D's transpose: stage row i is output column n0 + i.
 template <int SEG, typename Out>
-__device__ __forceinline__ void put_cols(const Out &o, const float *stage, int lane, int r0, int n0, int rows, int cols,
+__device__ __forceinline__ void put_cols(const Out &o, const float *stage, int lane, int r0, int r_end, int n0, int cols,
                                          const float *bias_p)
 {
     const int n = n0 + lane;
     if (n >= cols) return;
     const float bias = bias_p ? bias_p[n] : 0.0f;
-    const int m = min(SEG, rows - r0);
+    const int m = min(SEG, r_end - r0);
     for (int i0 = 0; i0 < m; i0 += 4) {
         float extra[4];
 #pragma unroll
@@ -479,13 +480,13 @@ __device__ __forceinline__ void put_cols(const Out &o, const float *stage, int l
     }
 }
 
-// A warp's 32 rows x 32 NSEG columns of an output whose number of columns 4 divides: four
+// A warp's 32 rows x 32 NSEG columns of an output whose number of columns 4 divides (n_end too): four
 // neighbours a lane, four rows at a time; stage_in(seg) brings 32 columns of sums into `stage` (false: a
 // wait ran out). What is added to a block of 32 columns (residual, add) is read while the block
 // before it is worked on, the first one's while the sums are waited for, and rows are finished a few
 // at a time (more of them keep more activations in flight than there are registers).
 template <typename T, bool FORWARD, int ACT, int NSEG, typename StageIn>
-__device__ __forceinline__ bool put_few(const StageIn &stage_in, const float *stage, int lane, int r0, int n0, int rows, int cols,
+__device__ __forceinline__ bool put_few(const StageIn &stage_in, const float *stage, int lane, int r0, int n0, int n_end, int rows, int cols,
                                         const float *bias_p, const T *extra_p, T *y, T *pre)
 {
     constexpr int W = kFew, L = 32 / W, NI = 32 / W;  // lanes a row; steps of W rows
@@ -493,7 +494,7 @@ __device__ __forceinline__ bool put_few(const StageIn &stage_in, const float *st
     const size_t step = W * (size_t)cols, first = (size_t)(r0 + sub) * cols + n0 + j;
     Few<T> next[NI] = {}, extra[NI];
     auto fetch = [&](int seg) {
-        if (n0 + seg * 32 + j < cols)
+        if (n0 + seg * 32 + j < n_end)
 #pragma unroll
             for (int i = 0; i < NI; ++i)
                 if (sub + W * i < m) next[i].load(extra_p + first + seg * 32 + i * step);
@@ -507,11 +508,11 @@ __device__ __forceinline__ bool put_few(const StageIn &stage_in, const float *st
         if (extra_p && seg + 1 < NSEG) fetch(seg + 1);
         const int n = n0 + seg * 32 + j;
         float bias[W] = {};
-        if (FORWARD && bias_p && n < cols)
+        if (FORWARD && bias_p && n < n_end)
 #pragma unroll
             for (int k = 0; k < W; ++k) bias[k] = bias_p[n + k];
         __syncwarp();
-        if (n < cols) {
+        if (n < n_end) {
             const size_t at = first + seg * 32;
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
@@ -537,32 +538,34 @@ __device__ __forceinline__ bool put_few(const StageIn &stage_in, const float *st
     return true;
 }
 template <typename T, int NSEG, typename StageIn>
-__device__ __forceinline__ bool put_forward(const StageIn &in, const Epilogue &ep, const float *stage, int lane, int r0, int n0)
+__device__ __forceinline__ bool put_forward(const StageIn &in, const Epilogue &ep, const float *stage, int lane, int r0, int n0, int n_end)
 {
     const T *res = (const T *)ep.residual;
     T *y = (T *)ep.y, *pre = (T *)ep.pre;
     switch (ep.act) {
-    case kActRelu: return put_few<T, true, kActRelu, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
-    case kActTanh: return put_few<T, true, kActTanh, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
-    case kActGelu: return put_few<T, true, kActGelu, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
-    case kActSilu: return put_few<T, true, kActSilu, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
-    default: return put_few<T, true, kActNone, NSEG>(in, stage, lane, r0, n0, ep.rows, ep.cols, ep.bias, res, y, pre);
+    case kActRelu: return put_few<T, true, kActRelu, NSEG>(in, stage, lane, r0, n0, n_end, ep.rows, ep.cols, ep.bias, res, y, pre);
+    case kActTanh: return put_few<T, true, kActTanh, NSEG>(in, stage, lane, r0, n0, n_end, ep.rows, ep.cols, ep.bias, res, y, pre);
+    case kActGelu: return put_few<T, true, kActGelu, NSEG>(in, stage, lane, r0, n0, n_end, ep.rows, ep.cols, ep.bias, res, y, pre);
+    case kActSilu: return put_few<T, true, kActSilu, NSEG>(in, stage, lane, r0, n0, n_end, ep.rows, ep.cols, ep.bias, res, y, pre);
+    default: return put_few<T, true, kActNone, NSEG>(in, stage, lane, r0, n0, n_end, ep.rows, ep.cols, ep.bias, res, y, pre);
     }
 }
 
-// A warp's 32 rows x SEG NSEG columns of sums to the output.
-template <int SEG, int NSEG, bool GRADIENT, typename StageIn>
+// A warp's 32 rows x SEG NSEG columns of sums to the output, those of D's columns before n_end
+// (FIT) or all of its columns.
+template <int SEG, int NSEG, bool GRADIENT, bool FIT, typename StageIn>
 __device__ __forceinline__ bool put_tile(const StageIn &in, const Epilogue &ep, bool swapped, int sp, const float *stage,
-                                         int lane, int m0, int n0)
+                                         int lane, int m0, int n0, int n_end)
 {
+    const int c_end = FIT ? n_end : ep.cols, r_end = FIT ? n_end : ep.rows;  // (D's columns are the output's, or, swapped, its rows)
     const bool plain = GRADIENT || ep.part;
     const Plain p = {ep.part ? nullptr : ep.add, ep.part ? ep.part + (size_t)sp * ep.rows * ep.cols : ep.out};
     if (SEG == 32 && ep.cols % 4 == 0 && (GRADIENT || !swapped)) {
         if (plain)
-            return put_few<float, false, kActNone, NSEG>(in, stage, lane, m0, n0, ep.rows, ep.cols, nullptr, p.add, p.out, nullptr);
+            return put_few<float, false, kActNone, NSEG>(in, stage, lane, m0, n0, c_end, ep.rows, ep.cols, nullptr, p.add, p.out, nullptr);
         if constexpr (!GRADIENT)
-            return ep.bf16_out ? put_forward<__nv_bfloat16, NSEG>(in, ep, stage, lane, m0, n0)
-                               : put_forward<float, NSEG>(in, ep, stage, lane, m0, n0);
+            return ep.bf16_out ? put_forward<__nv_bfloat16, NSEG>(in, ep, stage, lane, m0, n0, c_end)
+                               : put_forward<float, NSEG>(in, ep, stage, lane, m0, n0, c_end);
     }
 #pragma unroll 1
     for (int seg = 0; seg < NSEG; ++seg, n0 += SEG) {
@@ -570,19 +573,19 @@ __device__ __forceinline__ bool put_tile(const StageIn &in, const Epilogue &ep, 
         __syncwarp();
         if (!GRADIENT && swapped) {
             if (plain)
-                put_cols<SEG>(p, stage, lane, n0, m0, ep.rows, ep.cols, nullptr);
+                put_cols<SEG>(p, stage, lane, n0, r_end, m0, ep.cols, nullptr);
             else if (ep.bf16_out)
-                put_cols<SEG>(Forward<__nv_bfloat16>(ep), stage, lane, n0, m0, ep.rows, ep.cols, ep.bias);
+                put_cols<SEG>(Forward<__nv_bfloat16>(ep), stage, lane, n0, r_end, m0, ep.cols, ep.bias);
             else
-                put_cols<SEG>(Forward<float>(ep), stage, lane, n0, m0, ep.rows, ep.cols, ep.bias);
+                put_cols<SEG>(Forward<float>(ep), stage, lane, n0, r_end, m0, ep.cols, ep.bias);
         } else {
             if (plain)
-                put_rows<SEG, float, false, kActNone>(stage, lane, m0, n0, ep.rows, ep.cols, nullptr, p.add, p.out, nullptr);
+                put_rows<SEG, float, false, kActNone>(stage, lane, m0, n0, c_end, ep.rows, ep.cols, nullptr, p.add, p.out, nullptr);
             else if constexpr (!GRADIENT) {
                 if (ep.bf16_out)
-                    put_rows_forward<SEG, __nv_bfloat16>(ep, stage, lane, m0, n0);
+                    put_rows_forward<SEG, __nv_bfloat16>(ep, stage, lane, m0, n0, c_end);
                 else
-                    put_rows_forward<SEG, float>(ep, stage, lane, m0, n0);
+                    put_rows_forward<SEG, float>(ep, stage, lane, m0, n0, c_end);
             }
         }
         __syncwarp();
@@ -771,9 +774,17 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
         const int t = (int)(u % tiles), group = t / (kGroupM * g.nt), in = t % (kGroupM * g.nt);
         const int first = group * kGroupM, gm = min(kGroupM, g.mt - first);
         m0 = (first + in % gm) * 128 * CG + rank * 128;  // (this CTA's rows)
-        n0 = in / gm * BN;
+        n0 = in / gm * (SUMS ? g.step : BN);
         c_lo = (int)((long long)g.chunks * sp / g.split);
         c_hi = (int)((long long)g.chunks * (sp + 1) / g.split);
+    };
+    // Columns that a tile's MMAs take. Tiles of fp32 results are as wide as one another, in steps of 16
+    // (a pair of CTAs: 32), and their MMAs stop at the contraction's end: 11840 x 600 x 200 fp32
+    // backward 77.5 us, 83.1 with tiles of 256, 256 and 88 and whole chunks. The rest of an accumulator is
+    // not written, and no output is made of it. (bf16 forward: 65536 x 1024 x 1024 148 us so, 144 with
+    // whole tiles; its MMAs are not what it waits for.)
+    auto width = [&](int n0) {
+        return SUMS ? (uint32_t)min(g.step, (g.N - n0 + 16 * CG - 1) / (16 * CG) * (16 * CG)) : (uint32_t)BN;
     };
     int m0, n0, sp, c_lo, c_hi;
 
@@ -808,6 +819,7 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
             bool ok = true;
             for (long long u = blockIdx.x / CG; ok && u < units; u += gridDim.x / CG) {
                 unit(u, m0, n0, sp, c_lo, c_hi);
+                const int b0 = n0 + (CG == 2 ? rank * (int)width(n0) / 2 : 0);  // (this CTA's rows of B)
                 for (int c = c_lo; ok && c < c_hi; ++c) {
                     const int k0 = c * 64;
 #pragma unroll
@@ -823,9 +835,9 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
                                     if constexpr (B_MN) {
 #pragma unroll
                                         for (int j = 0; j < BR / 64; ++j)
-                                            tma_load_3d(dst + j * 8192, &tm_b, n0 + rank * BR + j * 64, k0, P.b[p], &full_b[s]);
+                                            tma_load_3d(dst + j * 8192, &tm_b, b0 + j * 64, k0, P.b[p], &full_b[s]);
                                     } else {
-                                        tma_load_3d(dst, &tm_b, k0, n0 + rank * BR, P.b[p], &full_b[s]);
+                                        tma_load_3d(dst, &tm_b, k0, b0, P.b[p], &full_b[s]);
                                     }
                                 }
                             }
@@ -861,12 +873,12 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
                 if (nb > s) tc::mbar_wait(&full_b[s], (uint32_t)((nb - 1 - s) / SB) & 1, kDrain, nullptr);
         }
         if (warp == 1 && rank == 0) {
-            constexpr uint32_t idesc = tc::idesc_bf16(BN, A_MN, B_MN, 128 * CG);
             const uint64_t desc_a = tc::smem_desc(ring_a, A_MN ? 8192 : 16, 1024), desc_b = tc::smem_desc(ring_b, B_MN ? 8192 : 16, 1024);
             uint32_t acc = 0;  // accumulators filled so far
             bool ok = true;
             for (long long u = blockIdx.x / CG; ok && u < units; u += gridDim.x / CG) {
                 unit(u, m0, n0, sp, c_lo, c_hi);
+                const uint32_t idesc = tc::idesc_bf16(width(n0), A_MN, B_MN, 128 * CG);
                 for (int c = c_lo; ok && c < c_hi; ++acc) {
                     const uint32_t d = tmem + (acc & 1) * BN;
                     ok = warp_wait(&acc_empty[acc & 1], ((acc >> 1) & 1) ^ 1, limit, abort);
@@ -875,6 +887,7 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
                     const int c_end = min(c_hi, c + g.per_acc);
                     uint32_t more = 0;
                     for (; ok && c < c_end; ++c) {
+                        const int left = g.K - c * 64;  // of the contraction: steps of 16 past its end are left out
 #pragma unroll
                         for (int p = 0; p < P.n; ++p) {
                             const int ia = P.at_a[P.a[p]], ib = P.at_b[P.b[p]], sa = ra.slot(ia), sb = rb.slot(ib);
@@ -887,7 +900,8 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
                                 if (issues) {
 #pragma unroll
                                     for (int k = 0; k < 4; ++k)  // 16 of the contraction: 32 bytes of a row, or 16 rows
-                                        mma_cg<CG>(d, da + k * (A_MN ? 128 : 2), db + k * (B_MN ? 128 : 2), idesc, k || p ? 1 : more);
+                                        if (!SUMS || k == 0 || left > 16 * k)
+                                            mma_cg<CG>(d, da + k * (A_MN ? 128 : 2), db + k * (B_MN ? 128 : 2), idesc, k || p ? 1 : more);
                                     if (P.free_a[p] && !JOINT) commit_cg<CG>(&empty_a[sa]);
                                     if (P.free_b[p]) commit_cg<CG>(&empty_b[sb]);
                                 }
@@ -997,7 +1011,7 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
                             }
                     return true;
                 };
-                put_tile<SEG, COLS / SEG, A_MN || B_MN>(in, g.ep, g.swapped, sp, stage, lane, mm, nn);
+                put_tile<SEG, COLS / SEG, A_MN || B_MN, true>(in, g.ep, g.swapped, sp, stage, lane, mm, nn, min(g.N, n0 + g.step));
             } else {
                 auto in = [&](int seg) {
                     if (seg == 0 && !filled()) return false;
@@ -1010,7 +1024,7 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
                     if (seg == COLS / SEG - 1) release();
                     return true;
                 };
-                ok = put_tile<SEG, COLS / SEG, false>(in, g.ep, g.swapped, sp, stage, lane, mm, nn);
+                ok = put_tile<SEG, COLS / SEG, false, false>(in, g.ep, g.swapped, sp, stage, lane, mm, nn, 0);
             }
         }
         if (!ok && lane == 0) fail();
@@ -1147,18 +1161,20 @@ GemmPlan plan_gemm(GemmArgs &g, int PA, int PB, int npair, int M, int N, int bn_
     for (int cg = 1; cg <= (pairs ? 2 : 1); ++cg)
         for (int bn = bn_lo; bn <= bn_hi; bn *= 2) {
             if (cg == 2 ? bn != 256 : bn == 256 && PB == 3) continue;  // (no such kernels)
-            const double mt = ceil_div(M, 128 * cg), nt = ceil_div(N, bn), b = bn * 128.0 / cg;
-            const double smem = (npair * (kTileA + b) + PA * (double)kTileA + PB * b) / 128.0;
-            const double cyc = std::max(2.0 * bn * npair, smem);
+            const int step = PA > 1 ? 16 * cg * ceil_div(N, (size_t)16 * cg * ceil_div(N, bn)) : bn;
+            const double mt = ceil_div(M, 128 * cg), nt = ceil_div(N, step), b = bn * 128.0 / cg;
+            const double smem = (npair * (kTileA + step * 128.0 / cg) + PA * (double)kTileA + PB * b) / 128.0;
+            const double cyc = std::max(2.0 * step * npair, smem);
             for (int split = 1; split <= std::min(g.chunks, 64); ++split) {
                 if (split > 1 && (g.chunks / split < 2 || (double)split * out_elems * 4 > (double)kMostPartBytes)) break;
                 const double waves = std::ceil(mt * nt * split / (cg == 2 ? pairs : sms)), chunks = std::ceil((double)g.chunks / split);
-                double cost = waves * (chunks * cyc + 400.0) + 16.0 * bn + 2000.0 + 1000.0 * cg;
+                double cost = waves * ((split > 1 || PA == 1 ? chunks : ceil_div(g.K, 16) / 4.0) * cyc + 400.0) + 16.0 * bn + 2000.0 + 1000.0 * cg;
                 if (split > 1) cost += 5000.0 + 2.0 * split * out_elems * 4 / 3500.0;
                 if (cost < best) {
                     best = cost;
                     g.mt = (int)mt;
                     g.nt = (int)nt;
+                    g.step = step;
                     g.split = split;
                     best_plan = {cg, bn};
                 }
@@ -1173,6 +1189,7 @@ cudaError_t contract_parts(stacklstm_op *op, const Operand &a, const Operand &b,
 {
     constexpr Pairs<PA, PB> P;
     GemmArgs g = {};
+    g.K = kcols;
     g.chunks = (int)ceil_div(kcols, 64);
     // fp32 results: 24 or 36 MMAs to an accumulator (24 everywhere: 4096 x 1024 x 32003 backward 1294 us, 1263 so)
     g.per_acc = ep.out || !ep.bf16_out ? std::max(1, 9 / P.n) : g.chunks;
@@ -1181,6 +1198,7 @@ cudaError_t contract_parts(stacklstm_op *op, const Operand &a, const Operand &b,
     g.err = op->err;
     const int M = swapped ? ep.cols : ep.rows, N = swapped ? ep.rows : ep.cols;
     const int lo = swapped && N <= 32 ? 32 : 64, hi = N <= lo ? lo : N <= 64 ? 64 : N <= 128 ? 128 : 256;
+    g.N = N;
     const GemmPlan plan = plan_gemm(g, PA, PB, P.n, M, N, lo, hi, (size_t)ep.rows * ep.cols, op->num_sms, op->pairs);
     const int bn = plan.bn;
     // rings: as many whole chunks as fit, what is left to the single part of B, then to A
