@@ -527,7 +527,7 @@ sl_status stacklstm_beam_create(stacklstm_op_t *out, int B, int K, int V, int S,
     const size_t nseg = dtype == SL_BF16 ? select_plan<__nv_bfloat16>(B, K, V, op->num_sms).nseg : select_plan<float>(B, K, V, op->num_sms).nseg;
     cudaError_t e = op_workspace(op, 0, (size_t)B * nseg * K * 8);
     if (!e) e = op_workspace(op, 1, (size_t)B * 4);
-    if (!e) e = cudaMemset(op->ws[1], 0, (size_t)B * 4);
+    if (!e) e = cudaMemsetAsync(op->ws[1], 0, (size_t)B * 4, op->stream);
     if (e) {
         stacklstm_op_destroy(op);
         return SL_ERR_OOM;

@@ -1289,7 +1289,7 @@ sl_status stacklstm_linear_create(stacklstm_op_t *out, int R, int K, int N, sl_d
     OpDevice guard(device);
     const size_t counts = ceil_div(N, kDzCols) * 4;
     op->pairs = most_pairs();
-    if (op_workspace(op, kWsCount, counts) || cudaMemset(op->ws[kWsCount], 0, counts)) {
+    if (op_workspace(op, kWsCount, counts) || cudaMemsetAsync(op->ws[kWsCount], 0, counts, op->stream)) {
         cudaGetLastError();
         stacklstm_op_destroy(op);
         return SL_ERR_OOM;

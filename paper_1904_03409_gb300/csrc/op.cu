@@ -39,7 +39,9 @@ stacklstm_op *op_new(int kind, sl_dtype dt, int device, void *stream, sl_status 
     OpDevice guard(device);
     bool ok = cudaDeviceGetAttribute(&op->num_sms, cudaDevAttrMultiProcessorCount, device) == cudaSuccess;
     if (ok) ok = cudaMalloc((void **)&op->err, 16) == cudaSuccess;
-    if (ok) ok = cudaMemset(op->err, 0, 16) == cudaSuccess;
+    // (on the handle's stream, as every clearing: cudaMemset is ordered with the default stream's work
+    // alone, and a stream that does not wait for that one could have a call's work before it)
+    if (ok) ok = cudaMemsetAsync(op->err, 0, 16, op->stream) == cudaSuccess;
     if (!ok) {
         cudaGetLastError();
         stacklstm_op_destroy(op);
@@ -92,7 +94,7 @@ sl_status stacklstm_op_status(stacklstm_op_t op)
     int32_t v = 0;
     cudaError_t e = cudaStreamSynchronize(op->stream);
     if (!e) e = cudaMemcpy(&v, op->err, 4, cudaMemcpyDeviceToHost);
-    if (!e && v) e = cudaMemset(op->err, 0, 4);
+    if (!e && v) e = cudaMemsetAsync(op->err, 0, 4, op->stream);
     if (e) return op_cuda(op, e, "stacklstm_op_status");
     if (v == SL_ERR_TIMEOUT) return op_fail(op, SL_ERR_TIMEOUT, "a device-side wait of a contraction ran out");
     if (v == SL_ERR_OP) return op_fail(op, SL_ERR_OP, "an op outside {-1, 0, +1} ran as a hold");

@@ -118,6 +118,15 @@ def test_rows_outside_the_handles(lib, name):
     lib.stacklstm_op_destroy(h)
 
 
+@pytest.mark.parametrize("kind,clears", [("norm", 1), ("linear", 2), ("distill", 1), ("beam", 2)])
+def test_a_new_handle_is_cleared_on_its_stream(lib, kind, clears):
+    """The status word and the arrival counters, before a call on that stream can use them."""
+    lib.fake_reset()
+    h = create(lib, kind)
+    assert lib.fake_calls() >= clears and lib.fake_unjoined(vp(USER)) == 0
+    lib.stacklstm_op_destroy(h)
+
+
 def test_numbers_are_checked(lib):
     h = create(lib, "norm")
     a = calls()["norm_forward"][1]
