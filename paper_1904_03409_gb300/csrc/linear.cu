@@ -598,16 +598,23 @@ __device__ __forceinline__ bool put_tile(const StageIn &in, const Epilogue &ep, 
 // the first group keeps 56 and the others take 224, 128 x 56 + 256 x 224 = 64512, so that 128 sums
 // and a batch of reads stay in registers), else sixteen, whose activations hide one another's
 // latencies (96 registers a thread, 640 x 96 = 61440, split as 128 x 32 + 512 x 112 = 61440).
-constexpr int gemm_epi_warps(int bn, bool sums) { return !sums && bn >= 128 ? 16 : 8; }
+// A bf16 forward of up to 32 rows reads W and does little else: two CTAs an SM with half the shared
+// memory and four output warps each, so that one's start and outputs, and the next launch's start,
+// lie under the other's loads. 8 rows, K = 1024, N = 600: 5.9 us so, 7.3 with one CTA of eight output
+// warps; N = 32003 14.9 and 16.4, of 32 rows 18.1 and 17.5; N = 9728, whose 76 tiles then have half
+// an SM's loads in flight each, 9.7 and 9.1. Up to 64 rows 23.9 and 20.6: one CTA.
+constexpr int gemm_ctas(int bn, bool sums) { return !sums && bn == 32 ? 2 : 1; }
+constexpr int gemm_epi_warps(int bn, bool sums) { return !sums && bn >= 128 ? 16 : gemm_ctas(bn, sums) == 2 ? 4 : 8; }
 constexpr int gemm_threads(int epi) { return (epi + 4) * 32; }
 static_assert(128 * 56 + 8 * 32 * 224 <= gemm_threads(8) * 168 && 128 * 32 + 16 * 32 * 112 <= gemm_threads(16) * 96,
               "registers of a CTA");
 constexpr int kMaxRing = 16;
 constexpr uint32_t kTileA = 128 * 128;  // 128 rows (or 2 x 64 columns) x 64 of the contraction
-constexpr uint32_t gemm_ring(int epi) { return 224 * 1024 - epi * 4096; }  // bytes: 4 KB a warp to stage outputs
+__host__ __device__ constexpr uint32_t gemm_main(int epi) { return (epi == 4 ? 108 : 224) * 1024; }    // bytes: rings and staging
+__host__ __device__ constexpr uint32_t gemm_ring(int epi) { return gemm_main(epi) - epi * 4096; }  // 4 KB a warp to stage outputs
 constexpr uint32_t kGemmBars = (6 * kMaxRing + 5) * 8 + 16;
-constexpr uint32_t kGemmSmem = 1024 + 224 * 1024 + kGemmBars;
-static_assert(kGemmSmem <= 227 * 1024, "shared memory of a CTA");
+constexpr uint32_t gemm_smem(int epi) { return 1024 + gemm_main(epi) + kGemmBars; }
+static_assert(gemm_smem(8) <= 227 * 1024 && 2 * (gemm_smem(4) + 1024) <= 228 * 1024, "shared memory of the CTAs of an SM");
 constexpr int kGroupM = 8;              // m tiles that share their B tiles in L2 (16: 1 % slower at 4096 x 1024 x 32003)
 constexpr long long kDrain = 4000000000LL;  // clock cycles: waits for a CTA's own copies and MMAs before it ends
 
@@ -707,7 +714,7 @@ __device__ __forceinline__ void prefetch_map(const void *tmap)
 // 1024 x 32003 bf16, with the 245 us of their parts, 1287 us, as pairs of CTAs on 256 x 256 tiles.
 // Bound by shared memory where it is short: forward 65536 x 1024 x 1024, gelu, residual and pre, 145 us.
 template <int BN, bool A_MN, bool B_MN, int PA, int PB, int EPI, int CG>
-__global__ void __launch_bounds__(gemm_threads(EPI), 1)
+__global__ void __launch_bounds__(gemm_threads(EPI), EPI == 4 ? 2 : 1)
 gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
            const __grid_constant__ GemmArgs g)
 {
@@ -715,7 +722,7 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
     constexpr int BR = BN / CG;  // rows of B that a CTA holds
     constexpr uint32_t kTileB = (uint32_t)BR * 128u;
     constexpr int COLS = BN / (EPI / 4), SEG = COLS < 32 ? COLS : 32;  // an output warp's columns
-    constexpr uint32_t kRing = 224 * 1024 - EPI * 4096;
+    constexpr uint32_t kRing = gemm_ring(EPI);
     constexpr bool JOINT = PA == 1 && PB == 1;      // A's and B's slots go together: one barrier for both
     constexpr bool SUMS = A_MN || B_MN || PB == 3;  // fp32 results: several accumulators to a tile
     constexpr uint32_t kCols = 2 * BN < 32 ? 32 : 2 * BN;
@@ -723,7 +730,7 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
     uint8_t *base = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const int SA = g.SA, SB = g.SB;
     const uint32_t ring_a = smem_u32(base), ring_b = ring_a + (uint32_t)SA * kTileA;
-    uint64_t *full_a = (uint64_t *)(base + 224 * 1024);
+    uint64_t *full_a = (uint64_t *)(base + gemm_main(EPI));
     uint64_t *empty_a = full_a + kMaxRing, *full_b = empty_a + kMaxRing, *empty_b = full_b + kMaxRing;
     uint64_t *peer_a = empty_b + kMaxRing, *peer_b = peer_a + kMaxRing;  // the pair's other CTA's operands have landed
     uint64_t *acc_full = peer_b + kMaxRing, *acc_empty = acc_full + 2, *done = acc_empty + 2;
@@ -808,7 +815,7 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
     if (warp < 4) {
         if constexpr (EPI == 8)
             asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-        else
+        else if constexpr (EPI == 16)
             asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
         // Both loops are run by whole warps, one lane of which issues: descriptors and coordinates
         // are then the same for a warp and stay in its uniform registers (by one thread in a branch
@@ -949,7 +956,7 @@ gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUt
     } else {
         if constexpr (EPI == 8)
             asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
-        else
+        else if constexpr (EPI == 16)
             asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
         // ------------------------------------------------------ sums and outputs
         const int q = warp & 3, group = (warp >> 2) - 1;  // a warp reads its quadrant of the lanes
@@ -1115,10 +1122,11 @@ cudaError_t launch_gemm(const stacklstm_op *op, const Operand &a, const Operand 
     if (!e) e = operand_map(&tb, b, B_MN ? 64 : BN / CG);
     constexpr int EPI = gemm_epi_warps(BN, A_MN || B_MN || PB == 3);
     constexpr auto kernel = gemm_parts<BN, A_MN, B_MN, PA, PB, EPI, CG>;
-    if (!e) e = smem_at_least((const void *)kernel, kGemmSmem);
+    if (!e) e = smem_at_least((const void *)kernel, gemm_smem(EPI));
     if (e) return e;
-    const unsigned grid = (unsigned)std::min<long long>((long long)g.mt * g.nt * g.split, CG == 2 ? op->pairs : op->num_sms) * CG;
-    return launch_cluster(kernel, CG, grid, gemm_threads(EPI), kGemmSmem, op->stream, ta, tb, g);
+    const int most = CG == 2 ? op->pairs : op->num_sms * gemm_ctas(BN, A_MN || B_MN || PB == 3);
+    const unsigned grid = (unsigned)std::min<long long>((long long)g.mt * g.nt * g.split, most) * CG;
+    return launch_cluster(kernel, CG, grid, gemm_threads(EPI), gemm_smem(EPI), op->stream, ta, tb, g);
 }
 
 // Pairs of CTAs that run at once: fewer than half the SMs where a group of SMs has an odd number of
@@ -1126,7 +1134,7 @@ cudaError_t launch_gemm(const stacklstm_op *op, const Operand &a, const Operand 
 int most_pairs()
 {
     constexpr auto kernel = gemm_parts<256, false, false, 1, 1, gemm_epi_warps(256, false), 2>;
-    if (smem_at_least((const void *)kernel, kGemmSmem)) return 0;
+    if (smem_at_least((const void *)kernel, gemm_smem(16))) return 0;
     cudaLaunchAttribute attr = {};
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = 2;
@@ -1134,7 +1142,7 @@ int most_pairs()
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2);
     cfg.blockDim = dim3(gemm_threads(gemm_epi_warps(256, false)));
-    cfg.dynamicSmemBytes = kGemmSmem;
+    cfg.dynamicSmemBytes = gemm_smem(16);
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     int n = 0;
@@ -1164,10 +1172,11 @@ GemmPlan plan_gemm(GemmArgs &g, int PA, int PB, int npair, int M, int N, int bn_
             const int step = PA > 1 ? 16 * cg * ceil_div(N, (size_t)16 * cg * ceil_div(N, bn)) : bn;
             const double mt = ceil_div(M, 128 * cg), nt = ceil_div(N, step), b = bn * 128.0 / cg;
             const double smem = (npair * (kTileA + step * 128.0 / cg) + PA * (double)kTileA + PB * b) / 128.0;
-            const double cyc = std::max(2.0 * step * npair, smem);
+            const int ctas = cg == 2 ? pairs : sms * gemm_ctas(bn, PA > 1);
+            const double cyc = std::max(2.0 * step * npair, smem) * (cg == 2 ? 1 : ctas / sms);
             for (int split = 1; split <= std::min(g.chunks, 64); ++split) {
                 if (split > 1 && (g.chunks / split < 2 || (double)split * out_elems * 4 > (double)kMostPartBytes)) break;
-                const double waves = std::ceil(mt * nt * split / (cg == 2 ? pairs : sms)), chunks = std::ceil((double)g.chunks / split);
+                const double waves = std::ceil(mt * nt * split / ctas), chunks = std::ceil((double)g.chunks / split);
                 double cost = waves * ((split > 1 || PA == 1 ? chunks : ceil_div(g.K, 16) / 4.0) * cyc + 400.0) + 16.0 * bn + 2000.0 + 1000.0 * cg;
                 if (split > 1) cost += 5000.0 + 2.0 * split * out_elems * 4 / 3500.0;
                 if (cost < best) {
