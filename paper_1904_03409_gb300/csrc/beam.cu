@@ -119,8 +119,9 @@ struct SelShared {
 // best_key() is its best key. Of any disjoint groups of keys, the K-th best of the groups' best
 // scores is no better than the K-th best of all: first the threads' best are grouped (32 groups, 64
 // for more than 32 hypotheses) and the keys from that score on are listed and ranked against one
-// another. Where they are more than the list holds (most of a row alike), the bound is the K-th of
-// the threads' own best keys, from which on there are at most K times a thread's keys, in `spill`.
+// another. Where they are more than the list holds (most of a row alike, or all of it in few threads),
+// the bound is the K-th of the threads' own best keys, from which on there are at most K times a
+// thread's keys, in `spill`.
 template <int NT, typename Push, typename Best>
 __device__ __forceinline__ void block_topk(float top, const Push &push, const Best &best_key, int K, SelShared &s, u64 *spill)
 {
@@ -167,9 +168,9 @@ __device__ __forceinline__ void block_topk(float top, const Push &push, const Be
             for (int i = 0; i < NT; ++i) above += s.top[i] > mine;
         if (mine && above == K - 1) s.kth = mine;
         __syncthreads();
-        const u64 kth = s.kth;
+        const u64 kth = s.kth;  // (1: fewer than K threads have a key, and every key counts)
         if (mine >= kth)
-            push(key_score(kth), [&](u64 k) {
+            push(kth > 1 ? key_score(kth) : -INFINITY, [&](u64 k) {
                 if (k >= kth) list[atomicAdd(&s.count, 1)] = k;
             });
         __syncthreads();

@@ -1,0 +1,60 @@
+"""What the output layers and the search meet at the edges of their ranges, on cuda:0: masks that
+leave few classes. Where a result has to be a given value, equality is asked for."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import output_layers as ol
+from paper_1904_03409_gb300 import binding as bd
+
+pytestmark = pytest.mark.gpu
+BF, FP = bd.SL_BF16, bd.SL_FP32
+TYPES = pytest.mark.parametrize("dt", [FP, BF], ids=["fp32", "bf16"])
+
+
+def tdt(dt):
+    return torch.bfloat16 if dt == BF else torch.float32
+
+
+def up(a, dtype=torch.float32):
+    return None if a is None else torch.from_numpy(np.ascontiguousarray(a)).to("cuda").to(dtype)
+
+
+def out(*s, dtype=torch.float32):
+    t = torch.empty(*s, dtype=dtype, device="cuda")
+    return t.fill_(float("nan")) if t.is_floating_point() else t.fill_(-77)
+
+
+# ------------------------------------------------------------------ selection
+def select_is_exact(dt, z):
+    """The kernel's choice and the oracle's, of values of the type."""
+    B, K, V = z.shape
+    zt = torch.from_numpy(z).to(tdt(dt))
+    score = -np.arange(B * K, dtype=np.float32).reshape(B, K) / 8
+    want = ol.select(zt.float().numpy(), None, score, None)
+    op = bd.stacklstm_beam_create(B, K, V, 2, 8, dt)
+    s, p, t = out(B, K), out(B, K, dtype=torch.int32), out(B, K, dtype=torch.int32)
+    bd.stacklstm_beam_select(op, zt.cuda(), None, up(score), None, s, p, t)
+    for got, w in zip((s, p, t), want):
+        assert np.array_equal(got.cpu().numpy(), w)
+    assert np.isfinite(want[0]).all()  # there are candidates enough
+
+
+@TYPES
+@pytest.mark.parametrize("K,V,allowed", [(64, 256, 40), (64, 128, 20), (40, 256, 36)])
+def test_select_from_the_same_few_classes_of_every_hypothesis(dt, K, V, allowed):
+    """More than 1024 candidates with fewer threads than hypotheses: all of those are ranked."""
+    z = np.random.default_rng(K + V).normal(size=(1, K, V))
+    z[:, :, allowed:] = -np.inf
+    select_is_exact(dt, z)
+
+
+@TYPES
+@pytest.mark.parametrize("B,K,V,threads,allowed", [(1, 40, 8192, 256, 36), (7, 20, 32768, 512, 18)])
+def test_select_from_classes_of_few_threads(dt, B, K, V, threads, allowed):
+    """The same within a row: of the 16-byte pieces that a CTA's threads take in turn, those of a
+    few threads."""
+    E = 8 if dt == BF else 4
+    z = np.random.default_rng(K + V).normal(size=(B, K, V))
+    z[:, :, np.arange(V) // E % threads >= allowed] = -np.inf
+    select_is_exact(dt, z)
