@@ -281,7 +281,7 @@ distill_wide(const __grid_constant__ DistillArgs a)
             const float c2 = exp2_hw(d * k2), c1 = exp2_hw(d * kLog2e);
             s2 = __fmul2_rn(s2, make_float2(c2, c2));
             s1 = __fmul2_rn(s1, make_float2(c1, c1));
-            m = pm;
+            m = max_nan(m, pm);  // (a NaN stays, whatever follows it)
         }
         if (m == -INFINITY) return;  // nothing yet
         float v[E];

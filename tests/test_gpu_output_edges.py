@@ -1,5 +1,8 @@
 """What the output layers and the search meet at the edges of their ranges, on cuda:0: masks that
-leave few classes. Where a result has to be a given value, equality is asked for."""
+leave few classes, NaN before masked places. Where a result has to be a given value, equality is
+asked for."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -58,3 +61,22 @@ def test_select_from_classes_of_few_threads(dt, B, K, V, threads, allowed):
     z = np.random.default_rng(K + V).normal(size=(B, K, V))
     z[:, :, np.arange(V) // E % threads >= allowed] = -np.inf
     select_is_exact(dt, z)
+
+
+# ------------------------------------------------------------------ distillation
+@TYPES
+@pytest.mark.parametrize("V", [40, 3000, 20000])
+def test_distill_nan_before_masked_classes(dt, V):
+    """A NaN stays in its row where every class after it is -inf."""
+    rng = np.random.default_rng(V)
+    R, k = 3, 2
+    z = torch.from_numpy(rng.normal(size=(R, V))).to(tdt(dt))
+    z[:, 16:] = -math.inf
+    z[1, 7] = math.nan
+    idx, gold = np.full((R, k), 3, np.int32), np.full(R, 4, np.int32)
+    op = bd.stacklstm_distill_create(R, V, k, dt)
+    loss, d = out(R), out(R, V)
+    bd.stacklstm_distill_run(op, z.cuda(), up(idx, torch.int32), up(rng.normal(size=(R, k))), up(gold, torch.int32), 1.0, 0.5, 1.0,
+                             loss, d)
+    assert loss.isnan().tolist() == [False, True, False]
+    assert d[1].isnan().all() and d[::2].isfinite().all()
