@@ -385,7 +385,7 @@ _f32 = _i32 = _i8 = _u8 = None  # torch's types, looked up when the first handle
 
 class StackLSTMOpHandle:
     """Owns one operator handle (stacklstm_norm_*, _linear_*, _distill_* or _beam_*); ``destroy``
-    (or garbage collection) frees it."""
+    (or garbage collection) frees it. ``stream`` is the raw stream its calls are ordered on."""
 
     def __init__(self, h, device, dtype, **sizes):
         self.h, self.device, self.dtype = h, device, dtype
@@ -434,7 +434,7 @@ def _op_create(name, device, dtype, stream, args, **sizes):
     raw = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
     h = ctypes.c_void_p()
     _check_op(None, getattr(load(), name)(ctypes.byref(h), *args, device, ctypes.c_void_p(raw)), name)
-    return StackLSTMOpHandle(h, device, dtype, **sizes)
+    return StackLSTMOpHandle(h, device, dtype, stream=raw, **sizes)
 
 
 def _rows(hd, t, name):
@@ -446,6 +446,7 @@ def _rows(hd, t, name):
 def stacklstm_op_set_stream(hd: StackLSTMOpHandle, stream):
     raw = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
     _check_op(hd.h, load().stacklstm_op_set_stream(hd.h, ctypes.c_void_p(raw)), "stacklstm_op_set_stream")
+    hd.stream = raw
 
 
 def stacklstm_op_status(hd: StackLSTMOpHandle):

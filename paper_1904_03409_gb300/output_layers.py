@@ -16,7 +16,9 @@ from . import binding as bd
 
 
 class OutputLayers:
-    """The layers' weights and handles for up to ``rows`` tops of H units and V classes."""
+    """The layers' weights and handles for up to ``rows`` tops of H units and V classes. Calls run on
+    torch's current stream, whichever it is (a call on another one than the last waits, on the
+    host, for what the layers did there)."""
 
     def __init__(self, rows: int, H: int, V: int, k: int, dtype: int = bd.SL_BF16, device: int = 0, seed: int = 0):
         import torch
@@ -38,8 +40,16 @@ class OutputLayers:
         self.mean, self.rstd, self.loss_rows, self.dlogits = f(rows), f(rows), f(rows), f(rows, V)
         self.dh, self.da, self.dy = f(rows, H), f(rows, H), f(rows, H)
 
+    def _on_current_stream(self):
+        import torch
+        stream = torch.cuda.current_stream(self.device).cuda_stream
+        for op in (self.norm, self.hidden, self.scores, self.teacher):
+            if op.stream != stream:
+                bd.stacklstm_op_set_stream(op, stream)
+
     def forward(self, y):
         """Logits of the tops y [r, H] (r up to ``rows``); what the backward needs is kept."""
+        self._on_current_stream()
         r, p = y.shape[0], self.params
         bd.stacklstm_norm_forward(self.norm, y, p["gamma"], p["beta"], 1e-5, self.a[:r], self.mean[:r], self.rstd[:r])
         bd.stacklstm_linear_forward(self.hidden, self.a[:r], p["W1"], p["b1"], self.a[:r], self.h[:r], self.pre[:r])

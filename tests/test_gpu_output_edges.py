@@ -1,6 +1,6 @@
 """What the output layers and the search meet at the edges of their ranges, on cuda:0: masks that
-leave few classes, NaN before masked places. Where a result has to be a given value, equality is
-asked for."""
+leave few classes, NaN before masked places, streams. Where a result has to be a given value or bit
+pattern, equality is asked for."""
 import math
 
 import numpy as np
@@ -9,6 +9,7 @@ import torch
 
 from oracle import output_layers as ol
 from paper_1904_03409_gb300 import binding as bd
+from paper_1904_03409_gb300 import output_layers as om
 
 pytestmark = pytest.mark.gpu
 BF, FP = bd.SL_BF16, bd.SL_FP32
@@ -80,3 +81,28 @@ def test_distill_nan_before_masked_classes(dt, V):
                              loss, d)
     assert loss.isnan().tolist() == [False, True, False]
     assert d[1].isnan().all() and d[::2].isfinite().all()
+
+
+# ------------------------------------------------------------------ the layers on a StackLSTM
+def decoder(B=3, V=9, H=16, I=8, K=4):
+    """Arguments of beam_decode up to the search's sizes."""
+    rng = np.random.default_rng(11)
+    f = lambda *s, sc=1.0: up((sc * rng.normal(size=s)).astype(np.float32))
+    l = om.OutputLayers(B * K, H, V, 1, FP, seed=5)
+    ops = torch.tensor([(1, 1, 1, -1, -1, 0, 0, 1, 0)[v % 9] for v in range(V)], dtype=torch.int8, device="cuda")
+    return l, f(I + H, 4 * H, sc=0.4), f(4 * H, sc=0.2), f(V, I), ops, torch.tanh(f(B, H)), f(B, H)
+
+
+def test_decode_on_another_stream_than_the_layers_were_made_on():
+    """The same bits as on theirs, with that one busy at the call."""
+    args = decoder()
+    want = om.beam_decode(*args, 4, 6, 8)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    torch.cuda._sleep(100_000_000)
+    with torch.cuda.stream(side):
+        got = om.beam_decode(*args, 4, 6, 8)
+    torch.cuda.synchronize()
+    again = om.beam_decode(*args, 4, 6, 8)
+    for w, g, a in zip(want, got, again):
+        assert torch.equal(w, g) and torch.equal(w, a)
