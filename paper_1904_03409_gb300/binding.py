@@ -135,14 +135,16 @@ def stacklstm_create(T: int, B: int, I: int, H: int, dtype: int, device: int = 0
     h = ctypes.c_void_p()
     _check(None, load().stacklstm_create(ctypes.byref(h), T, B, I, H, dtype, device, ctypes.c_void_p(raw)),
            "stacklstm_create")
-    return StackLSTMHandle(h, T, B, I, H, dtype, device)
+    return StackLSTMHandle(h, T, B, I, H, dtype, device, raw)
 
 
 class StackLSTMHandle:
-    """Owns one library handle; ``destroy`` (or garbage collection) frees it."""
+    """Owns one library handle; ``destroy`` (or garbage collection) frees it. ``stream`` is the raw
+    stream its calls are ordered on."""
 
-    def __init__(self, h, T, B, I, H, dtype, device):
+    def __init__(self, h, T, B, I, H, dtype, device, stream=0):
         self.h, self.T, self.B, self.I, self.H, self.dtype, self.device = h, T, B, I, H, dtype, device
+        self.stream = stream
 
     @property
     def tdtype(self):
@@ -164,6 +166,7 @@ class StackLSTMHandle:
 def stacklstm_set_stream(hd: StackLSTMHandle, stream):
     raw = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
     _check(hd.h, load().stacklstm_set_stream(hd.h, ctypes.c_void_p(raw)), "stacklstm_set_stream")
+    hd.stream = raw
 
 
 def stacklstm_set_async(hd: StackLSTMHandle, on: bool):

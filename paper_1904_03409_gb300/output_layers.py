@@ -83,12 +83,27 @@ class OutputLayers:
 def train_step(hd, ins: dict, out: dict, layers: OutputLayers, t_idx, t_logit, gold, tau=2.0, alpha=0.5):
     """One training step of a StackLSTM (handle ``hd``, tensors as in ``runner``) under ``layers``:
     forward, loss against the teacher, backward. t_idx, t_logit [T B, k], gold [T B]; returns the
-    loss rows; the gradients are in ``layers.grads`` and ``out``."""
+    loss rows; the gradients are in ``layers.grads`` and ``out``. ``hd`` may be on a stream of its
+    own: the step comes after the current stream's work and before what follows on it."""
+    import torch
     T, B, H = hd.T, hd.B, hd.H
+    cur = torch.cuda.current_stream(hd.device)
+    own = cur  # the StackLSTM's
+    if hd.stream != cur.cuda_stream:
+        own = torch.cuda.ExternalStream(hd.stream, hd.device) if hd.stream else torch.cuda.default_stream(hd.device)
+
+    def order(first, then):
+        if first is not then:
+            then.wait_stream(first)
+
+    order(cur, own)
     bd.stacklstm_forward(hd, ins["x"], ins["ops"], ins["h0"], ins["c0"], ins["W"], ins["bias"], None, None, out["p_final"], None,
                          None, out["y"])
+    order(own, cur)
     loss, dy = layers.learn(out["y"].view(T * B, H), t_idx, t_logit, gold, tau, alpha)
+    order(cur, own)
     bd.stacklstm_backward(hd, None, dy.view(T, B, H), out["dx"], out["dh0"], out["dc0"], out["dW"], out["dbias"])
+    order(own, cur)
     return loss
 
 

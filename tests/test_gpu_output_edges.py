@@ -10,6 +10,7 @@ import torch
 from oracle import output_layers as ol
 from paper_1904_03409_gb300 import binding as bd
 from paper_1904_03409_gb300 import output_layers as om
+from paper_1904_03409_gb300 import runner, workloads as wl
 
 pytestmark = pytest.mark.gpu
 BF, FP = bd.SL_BF16, bd.SL_FP32
@@ -106,3 +107,44 @@ def test_decode_on_another_stream_than_the_layers_were_made_on():
     again = om.beam_decode(*args, 4, 6, 8)
     for w, g, a in zip(want, got, again):
         assert torch.equal(w, g) and torch.equal(w, a)
+
+
+@pytest.mark.parametrize("own,busy", [("side", "own"), ("side", "current"), ("default", "own")])
+def test_train_step_of_a_stack_on_its_own_stream(own, busy):
+    """The StackLSTM on a side stream, or it on the default one and the step called on a side
+    stream: the same bits as on one, with either stream busy at the call."""
+    T, B, H, V, k = 9, 12, 24, 37, 4
+    w = wl.make_workload("streams", T=T, B=B, I=16, H=H, dtype="fp32", seed=3, ops_kind="random_walk", probs=(0.5, 0.3, 0.2),
+                         bias_scale=0.2, h0_scale=0.5)
+    rng = np.random.default_rng(4)
+    teacher = (up(rng.integers(-1, V, (T * B, k)), torch.int32), up(rng.normal(size=(T * B, k))),
+               up(rng.integers(-1, V, T * B), torch.int32))
+    results = []
+    default, side = torch.cuda.default_stream(), torch.cuda.Stream()
+    for stack, current in ((default, default), (side, default) if own == "side" else (default, side)):
+        hd = bd.stacklstm_create(T, B, 16, H, FP, 0, stack)
+        bd.stacklstm_set_async(hd, True)
+        with torch.cuda.stream(current):
+            layers = om.OutputLayers(T * B, H, V, k, FP, seed=7)
+        torch.cuda.synchronize()
+        ins, o = runner.upload(w), runner.alloc_outputs(w)
+        for t in (*o.values(), *layers.grads.values()):
+            t.fill_(math.nan if t.is_floating_point() else 0)
+        x = ins["x"]
+        ins["x"] = torch.zeros_like(x)
+        torch.cuda.synchronize()
+        if stack is not current:
+            with torch.cuda.stream(stack if busy == "own" else current):
+                torch.cuda._sleep(100_000_000)
+        with torch.cuda.stream(current):
+            ins["x"].copy_(x)  # an input that the current stream's work writes
+            loss = om.train_step(hd, ins, o, layers, *teacher)
+            results.append([loss.clone(), *(layers.grads[n].clone() for n in sorted(layers.grads)),
+                            *(o[n].clone() for n in ("y", "dx", "dh0", "dc0", "dW", "dbias"))])
+        torch.cuda.synchronize()
+        layers.status()
+        bd.stacklstm_status(hd)
+        hd.destroy()
+        layers.destroy()
+    for a, b in zip(*results):
+        assert torch.equal(a, b) and a.isfinite().all()
