@@ -15,6 +15,18 @@ import math
 from . import binding as bd
 
 
+def _raise_first(checks):
+    """Every handle's status read (and so cleared), the first error raised."""
+    errors = []
+    for status, handle in checks:
+        try:
+            status(handle)
+        except bd.StackLSTMError as e:
+            errors.append(e)
+    if errors:
+        raise errors[0]
+
+
 class OutputLayers:
     """The layers' weights and handles for up to ``rows`` tops of H units and V classes. Calls run on
     torch's current stream, whichever it is (a call on another one than the last waits, on the
@@ -72,8 +84,7 @@ class OutputLayers:
         return self.loss_rows[:r], self.dy[:r]
 
     def status(self):
-        for op in (self.norm, self.hidden, self.scores, self.teacher):
-            bd.stacklstm_op_status(op)
+        _raise_first([(bd.stacklstm_op_status, op) for op in (self.norm, self.hidden, self.scores, self.teacher)])
 
     def destroy(self):
         for op in (self.norm, self.hidden, self.scores, self.teacher):
@@ -154,8 +165,8 @@ def beam_decode(layers: OutputLayers, W, bias, emb, ops, h0, c0, K: int, steps: 
             # the cell on the tops of all rows; what it gives is pushed where the class pushes
             bd.stacklstm_forward(cell, emb[cls].view(1, N, I), push, top_h, top_c, W, bias, cell_h, cell_c, p_cell)
             bd.stacklstm_beam_push(search, step_ops, cell_h[1], cell_c[1], p[0], h[0], c[0], top_h, top_c)
-        bd.stacklstm_status(cell)
-        bd.stacklstm_op_status(search)
+        _raise_first([(bd.stacklstm_status, cell)] +
+                     [(bd.stacklstm_op_status, op) for op in (layers.norm, layers.hidden, layers.scores, search)])
         return score[0], history
     finally:
         search.destroy()

@@ -148,3 +148,14 @@ def test_train_step_of_a_stack_on_its_own_stream(own, busy):
         layers.destroy()
     for a, b in zip(*results):
         assert torch.equal(a, b) and a.isfinite().all()
+
+
+def test_decode_reports_what_its_layers_detected(monkeypatch):
+    """A wait of the layers' contractions that runs out (a budget of 0 cycles)."""
+    monkeypatch.setenv("STACKLSTM_WAIT_LIMIT_CYCLES", "0")
+    args = decoder()
+    monkeypatch.delenv("STACKLSTM_WAIT_LIMIT_CYCLES")
+    with pytest.raises(bd.StackLSTMError) as e:
+        om.beam_decode(*args, 4, 2, 8)
+    assert e.value.status == 6
+    args[0].status()  # cleared
