@@ -122,7 +122,8 @@ def beam_decode(layers: OutputLayers, W, bias, emb, ops, h0, c0, K: int, steps: 
     """The K best sequences of up to ``steps`` classes for each of the B sentences whose stacks start
     at h0, c0 [B, H]. Class v pushes, pops or holds (ops [V] int8) with the input emb[v] (emb
     [V, I]); a pop of an empty stack is no candidate; class ``end`` ends a sequence. W, bias: the
-    StackLSTM's. Returns (scores [B, K], classes [B, K, steps], -1 after an end), best first."""
+    StackLSTM's. Returns (scores [B, K], classes [B, K, steps], -1 after an end), best first; where
+    there are fewer than K sequences, -inf and -1."""
     import torch
     B, H = h0.shape
     V, I = emb.shape
@@ -157,6 +158,7 @@ def beam_decode(layers: OutputLayers, W, bias, emb, ops, h0, c0, K: int, steps: 
             # the sequences' own bookkeeping: what each row comes from and whether it has ended
             from_row = parent.clamp_min(0).long()
             history = history.gather(1, from_row[..., None].expand_as(history)).contiguous()
+            history.masked_fill_((parent < 0)[..., None], -1)  # candidates ran out: no sequence
             history[:, :, s] = token.long()
             done = done.gather(1, from_row)
             done |= ((token == end) & (token >= 0)).to(torch.uint8)

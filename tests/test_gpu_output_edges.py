@@ -159,3 +159,12 @@ def test_decode_reports_what_its_layers_detected(monkeypatch):
         om.beam_decode(*args, 4, 2, 8)
     assert e.value.status == 6
     args[0].status()  # cleared
+
+
+def test_decode_hypotheses_that_run_out_have_no_classes():
+    """Two classes, an end and a pop, on empty stacks: one sequence, the end alone."""
+    layers, W, bias, emb, _, h0, c0 = decoder(B=2, V=2, K=4)
+    ops = torch.tensor([0, -1], dtype=torch.int8, device="cuda")
+    score, seqs = om.beam_decode(layers, W, bias, emb, ops, h0, c0, 4, 3, 0)
+    assert score.isfinite().tolist() == [[True, False, False, False]] * 2
+    assert seqs.tolist() == [[[0, -1, -1]] + [[-1, -1, -1]] * 3] * 2
