@@ -73,7 +73,7 @@ class OutputLayers:
         classes), the layers' gradients (``grads``) and the tops' gradient dy [r, H]."""
         r, p, g = y.shape[0], self.params, self.grads
         logits = self.forward(y)
-        bd.stacklstm_distill_run(self.teacher, logits, t_idx, t_logit, gold, tau, alpha, 1.0 / r, self.loss_rows[:r],
+        bd.stacklstm_distill_run(self.teacher, logits, t_idx, t_logit, gold, tau, alpha, 1.0 / max(r, 1), self.loss_rows[:r],
                                  self.dlogits[:r])
         bd.stacklstm_linear_backward(self.scores, self.dlogits[:r], self.h[:r], p["W2"], None, None, self.dh[:r], g["W2"], g["b2"])
         # the residual's gradient is dh itself

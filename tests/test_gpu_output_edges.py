@@ -168,3 +168,15 @@ def test_decode_hypotheses_that_run_out_have_no_classes():
     score, seqs = om.beam_decode(layers, W, bias, emb, ops, h0, c0, 4, 3, 0)
     assert score.isfinite().tolist() == [[True, False, False, False]] * 2
     assert seqs.tolist() == [[[0, -1, -1]] + [[-1, -1, -1]] * 3] * 2
+
+
+def test_learn_of_no_rows():
+    """Zero gradients, not an error."""
+    layers = om.OutputLayers(4, 16, 9, 2, BF)
+    e = lambda *s, dtype=torch.float32: torch.empty(0, *s, dtype=dtype, device="cuda")
+    for g in layers.grads.values():
+        g.fill_(math.nan)
+    loss, dy = layers.learn(e(16, dtype=torch.bfloat16), e(2, dtype=torch.int32), e(2), e(dtype=torch.int32))
+    layers.status()
+    assert loss.shape == (0,) and dy.shape == (0, 16)
+    assert all(not g.any() for g in layers.grads.values())
