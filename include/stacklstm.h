@@ -468,7 +468,7 @@ sl_status stacklstm_distill_run(stacklstm_op_t op, int rows, const void *logits,
  * words), stacks of S slots and H units per row (S = T + 1 slots hold any T transitions).
  * K <= 64, B <= 65535, K V <= 2^30, S <= 1048560.
  * stacklstm_beam_lse: lse [B, K] (float) = ln sum_v exp(logits [B, K, V]) (dtype); -inf for a row
- *   of -inf.
+ *   of -inf, +inf for a row with +inf, NaN for one with NaN.
  * stacklstm_beam_select: candidate (k, v) of sentence b scores
  *   score[b, k] + (logits[b, k, v] - lse[b, k]), each operation rounded to fp32 (lse NULL: 0, the
  *   logits are log-probabilities). A hypothesis with done[b, k] != 0 (done uint8, may be NULL) has

@@ -71,7 +71,7 @@ lse_rows(int rows, int V, const T *__restrict__ z, float *__restrict__ lse)
         for (int i = 0; i < E; ++i) s[0] += exp2_hw((v[i] - base) * kLog2e);
     });
     row_join<false, TPR>(s, sm);
-    if (t == 0 && r < rows) lse[r] = base + logf(s[0]);
+    if (t == 0 && r < rows) lse[r] = base == INFINITY ? base : base + logf(s[0]);  // (+inf: its differences are NaN)
 }
 
 template <typename T>

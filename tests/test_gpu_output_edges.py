@@ -180,3 +180,23 @@ def test_learn_of_no_rows():
     layers.status()
     assert loss.shape == (0,) and dy.shape == (0, 16)
     assert all(not g.any() for g in layers.grads.values())
+
+
+# ------------------------------------------------------------------ normalisers
+@TYPES
+@pytest.mark.parametrize("V", [5, 83, 1500, 9001, 40000, 70001])
+def test_lse_of_infinite_logits(dt, V):
+    """+inf is a row's normaliser, -inf that of a row without classes, NaN stays."""
+    rng = np.random.default_rng(V)
+    z = torch.from_numpy(rng.normal(size=(1, 6, V))).to(tdt(dt)).cuda()
+    z[0, 0, V // 2] = math.inf
+    z[0, 1] = -math.inf
+    z[0, 1, V - 1] = math.inf
+    z[0, 2] = math.inf
+    z[0, 3] = -math.inf
+    z[0, 4, 0], z[0, 4, V - 1] = math.inf, math.nan
+    op = bd.stacklstm_beam_create(1, 6, V, 2, 8, dt)
+    got = out(1, 6)
+    bd.stacklstm_beam_lse(op, z, got)
+    g = got[0].tolist()
+    assert g[:4] == [math.inf, math.inf, math.inf, -math.inf] and math.isnan(g[4]) and math.isfinite(g[5])
