@@ -77,18 +77,19 @@ struct Piece<T, 1> {
 
 template <typename T, int VEC, int CH, int TPR>
 __global__ void __launch_bounds__(norm_threads(TPR), norm_ctas(TPR, CH * VEC))
-norm_fwd(int rows, int N, const T *__restrict__ x, const float *__restrict__ gamma, const float *__restrict__ beta,
+norm_fwd(unsigned rows, int N, const T *__restrict__ x, const float *__restrict__ gamma, const float *__restrict__ beta,
          float eps, T *__restrict__ y, float *__restrict__ mean, float *__restrict__ rstd)
 {
     constexpr int RPB = norm_threads(TPR) / TPR;
     __shared__ float sm[32];
     after_previous();
-    const int t = threadIdx.x % TPR, step = gridDim.x * RPB;
+    const int t = threadIdx.x % TPR;
+    const unsigned step = gridDim.x * RPB;  // (rows are counted without a sign: the last one and a step may pass 2^31)
     const float inv = 1.0f / (float)N;
     const bool whole = on_32(gamma) && on_32(beta);
-    int r = blockIdx.x * RPB + threadIdx.x / TPR;
+    unsigned r = blockIdx.x * RPB + threadIdx.x / TPR;
     Piece<T, VEC> next[CH];
-    auto fetch = [&](int row) {
+    auto fetch = [&](unsigned row) {
         if (row < rows)
 #pragma unroll
             for (int j = 0; j < CH; ++j)
@@ -146,14 +147,14 @@ norm_fwd(int rows, int N, const T *__restrict__ x, const float *__restrict__ gam
 // Rows of any width: a CTA a row, three passes over it (the last two from the caches).
 template <typename T>
 __global__ void __launch_bounds__(kWideThreads)
-norm_fwd_wide(int rows, int N, const T *__restrict__ x, const float *__restrict__ gamma,
+norm_fwd_wide(unsigned rows, int N, const T *__restrict__ x, const float *__restrict__ gamma,
               const float *__restrict__ beta, float eps, T *__restrict__ y, float *__restrict__ mean,
               float *__restrict__ rstd)
 {
     __shared__ float sm[kWideThreads / 32];
     after_previous();
     const float inv = 1.0f / (float)N;
-    for (int r = blockIdx.x; r < rows; r += gridDim.x) {
+    for (unsigned r = blockIdx.x; r < rows; r += gridDim.x) {
         const T *xr = x + (size_t)r * N;
         float sum = 0.0f, sq = 0.0f;
         for (int c = threadIdx.x; c < N; c += kWideThreads) sum += to_f32(xr[c]);
@@ -187,7 +188,7 @@ __host__ __device__ constexpr size_t norm_row_bytes(int tpr, int vec, int ch)
 }
 template <typename T, int VEC, int CH, int TPR>
 __global__ void __launch_bounds__(norm_bwd_threads(TPR, CH * VEC), TPR == 32 ? 1 : CH * VEC <= 16 ? 2 : 1)
-norm_bwd(int rows, int N, const float *__restrict__ dy, const T *__restrict__ x, const float *__restrict__ gamma,
+norm_bwd(unsigned rows, int N, const float *__restrict__ dy, const T *__restrict__ x, const float *__restrict__ gamma,
          const float *__restrict__ mean, const float *__restrict__ rstd, float *__restrict__ dx,
          float *__restrict__ part)
 {
@@ -196,7 +197,8 @@ norm_bwd(int rows, int N, const float *__restrict__ dy, const T *__restrict__ x,
     __shared__ float sm[2 * 32];
     extern __shared__ __align__(16) uint8_t dyn[];  // the rows ahead; then the column sums [RPB][N]
     after_previous();
-    const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR, step = gridDim.x * RPB;
+    const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+    const unsigned step = gridDim.x * RPB;
     const float inv = 1.0f / (float)N;
     const bool whole = on_32(gamma) && on_32(dx);
     float dg[CH][VEC], db[CH][VEC];
@@ -208,7 +210,7 @@ norm_bwd(int rows, int N, const float *__restrict__ dy, const T *__restrict__ x,
     auto slot = [&](int s) { return dyn + ((size_t)s * RPB + sub) * kRow; };
     auto d_of = [&](int s) { return (float *)slot(s) + t * VEC; };
     auto x_of = [&](int s) { return (T *)(slot(s) + (size_t)TPR * CH * VEC * 4) + t * VEC; };
-    auto fetch = [&](int row, int s) {
+    auto fetch = [&](unsigned row, int s) {
         if constexpr (VEC > 1) {
             if (row < rows)
 #pragma unroll
@@ -224,7 +226,7 @@ norm_bwd(int rows, int N, const float *__restrict__ dy, const T *__restrict__ x,
             tc::cp_async_commit();
         }
     };
-    int r = blockIdx.x * RPB + sub;
+    unsigned r = blockIdx.x * RPB + sub;
 #pragma unroll
     for (int s = 0; s < kAhead; ++s) fetch(r + s * step, s);
     float next_m = r < rows ? mean[r] : 0.0f, next_rs = r < rows ? rstd[r] : 0.0f;
@@ -313,7 +315,7 @@ norm_bwd(int rows, int N, const float *__restrict__ dy, const T *__restrict__ x,
 
 template <typename T>
 __global__ void __launch_bounds__(kWideThreads)
-norm_bwd_wide(int rows, int N, const float *__restrict__ dy, const T *__restrict__ x, const float *__restrict__ gamma,
+norm_bwd_wide(unsigned rows, int N, const float *__restrict__ dy, const T *__restrict__ x, const float *__restrict__ gamma,
               const float *__restrict__ mean, const float *__restrict__ rstd, float *__restrict__ dx,
               float *__restrict__ part)
 {
@@ -324,7 +326,7 @@ norm_bwd_wide(int rows, int N, const float *__restrict__ dy, const T *__restrict
     if (out)
         for (int c = threadIdx.x; c < 2 * N; c += kWideThreads) out[c] = 0.0f;
     __syncthreads();
-    for (int r = blockIdx.x; r < rows; r += gridDim.x) {
+    for (unsigned r = blockIdx.x; r < rows; r += gridDim.x) {
         const float *dr = dy + (size_t)r * N;
         const T *xr = x + (size_t)r * N;
         const float m = mean[r], s = rstd[r];

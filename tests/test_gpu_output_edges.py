@@ -200,3 +200,26 @@ def test_lse_of_infinite_logits(dt, V):
     bd.stacklstm_beam_lse(op, z, got)
     g = got[0].tolist()
     assert g[:4] == [math.inf, math.inf, math.inf, -math.inf] and math.isnan(g[4]) and math.isfinite(g[5])
+
+
+# ------------------------------------------------------------------ layer norm
+def test_norm_of_the_most_rows():
+    """2^31 - 1 rows: the last one and a step from it pass 31 bits."""
+    R = 2 ** 31 - 1
+    if torch.cuda.mem_get_info()[0] < 80 << 30:
+        pytest.skip("needs 80 GB")
+    op = bd.stacklstm_norm_create(R, 1, FP)
+    x, beta = torch.ones(R, 1, device="cuda"), torch.full((1,), 3.0, device="cuda")
+    y, mean, rstd = torch.zeros(R, 1, device="cuda"), torch.zeros(R, device="cuda"), torch.zeros(R, device="cuda")
+    bd.stacklstm_norm_forward(op, x, None, beta, 1.0, y, mean, rstd)
+    bd.stacklstm_op_status(op)
+    for t, want in ((y, 3.0), (mean, 1.0), (rstd, 1.0)):  # a row of one is its mean
+        lo, hi = torch.aminmax(t)
+        assert lo == want and hi == want
+    y.fill_(0.0)
+    y[-3:] = 1.0  # dy of the last rows alone, so that their sum is exact
+    dx, dg, db = torch.full((R, 1), math.nan, device="cuda"), out(1), out(1)
+    bd.stacklstm_norm_backward(op, y, x, None, mean, rstd, dx, dg, db)
+    bd.stacklstm_op_status(op)
+    lo, hi = torch.aminmax(dx)
+    assert lo == 0 and hi == 0 and dg.item() == 0 and db.item() == 3
