@@ -411,6 +411,9 @@ const char *stacklstm_op_last_error(stacklstm_op_t op);
  *   float outputs (NULL if no backward follows); eps >= 0.
  * backward: dy [rows, N] float; x, gamma, mean, rstd as in the forward; outputs (each
  *   nullable, overwritten) dx [rows, N], dgamma, dbeta [N]. rows = 0 gives zero sums.
+ * The sums' workspace is allocated at create where rows fit registers (N to 4096, in multiples of
+ * 16 bytes to 8192 of bf16), 10 MB at most; for wider rows by the first backward that wants dgamma
+ * or dbeta, 8 N bytes for each of up to four CTAs an SM, 4 GiB at most.
  */
 sl_status stacklstm_norm_create(stacklstm_op_t *out, int R, int N, sl_dtype dtype, int device, void *stream);
 sl_status stacklstm_norm_forward(stacklstm_op_t op, int rows, const void *x, const float *gamma, const float *beta,

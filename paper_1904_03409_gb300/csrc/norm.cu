@@ -380,6 +380,8 @@ norm_reduce(const float *__restrict__ part, int n, int N, float *__restrict__ dg
 struct NormPlan {
     int vec, ch, tpr, grid;
 };
+constexpr size_t kMostSumBytes = (size_t)4 << 30;  // of the CTAs' column sums: fewer CTAs from rows of 883011 on
+inline size_t norm_sum_bytes(const stacklstm_op *op, const NormPlan &p) { return (size_t)p.grid * 2 * op->N * 4; }
 NormPlan norm_plan(const stacklstm_op *op, int rows, bool bwd)
 {
     const int vmax = op->dt == SL_BF16 ? 8 : 4, N = op->N;
@@ -393,6 +395,7 @@ NormPlan norm_plan(const stacklstm_op *op, int rows, bool bwd)
     const int per_sm = !p.ch ? 4 : bwd ? (p.tpr == 32 || p.ch * p.vec > 16 ? 1 : 2) : norm_ctas(p.tpr, p.ch * p.vec);
     const int rpb = !p.ch ? 1 : (bwd ? norm_bwd_threads(p.tpr, p.ch * p.vec) : norm_threads(p.tpr)) / p.tpr;
     p.grid = (int)std::min<size_t>(ceil_div((size_t)rows, (size_t)rpb), (size_t)op->num_sms * per_sm);
+    if (bwd) p.grid = (int)std::min<size_t>(p.grid, std::max<size_t>(1, kMostSumBytes / ((size_t)N * 8)));
     return p;
 }
 
@@ -461,9 +464,10 @@ sl_status stacklstm_norm_create(stacklstm_op_t *out, int R, int N, sl_dtype dtyp
     op->R = R;
     op->N = N;
     OpDevice guard(device);
-    // the column sums of every CTA of a backward
-    const size_t ctas = std::min<size_t>((size_t)R, (size_t)op->num_sms * 4);
-    if (op_workspace(op, 0, ctas * 2 * (size_t)N * 4) != cudaSuccess) {
+    // the column sums of a backward's CTAs: 10 MB at most; for the wide kernels, where they are gigabytes,
+    // the first backward that wants them allocates them
+    const NormPlan p = norm_plan(op, R, true);
+    if (p.ch && op_workspace(op, 0, norm_sum_bytes(op, p)) != cudaSuccess) {
         stacklstm_op_destroy(op);
         return SL_ERR_OOM;
     }
@@ -507,8 +511,9 @@ sl_status stacklstm_norm_backward(stacklstm_op_t op, int rows, const float *dy, 
     c.op = op; c.rows = rows; c.x = x; c.gamma = gamma; c.mean = const_cast<float *>(mean);
     c.rstd = const_cast<float *>(rstd); c.dy = dy; c.dx = dx;
     const bool sums = dgamma || dbeta;
-    c.part = sums ? (float *)op->ws[0] : nullptr;
     const NormPlan p = norm_plan(op, rows, true);
+    if (sums && (e = op_workspace(op, 0, norm_sum_bytes(op, p)))) return op_cuda(op, e, "stacklstm_norm_backward");
+    c.part = sums ? (float *)op->ws[0] : nullptr;
     e = op->dt == SL_BF16 ? run_norm<__nv_bfloat16>(c, p) : run_norm<float>(c, p);
     if (!e && sums)
         e = launch_after(norm_reduce, ceil_div(2 * (size_t)op->N, 32), 1024, 0, op->stream, (const float *)op->ws[0], p.grid, op->N,

@@ -7,6 +7,7 @@ import numpy as np
 import pytest
 import torch
 
+import test_gpu_output_layers as base
 from oracle import output_layers as ol
 from paper_1904_03409_gb300 import binding as bd
 from paper_1904_03409_gb300 import output_layers as om
@@ -223,3 +224,10 @@ def test_norm_of_the_most_rows():
     bd.stacklstm_op_status(op)
     lo, hi = torch.aminmax(dx)
     assert lo == 0 and hi == 0 and dg.item() == 0 and db.item() == 3
+
+
+@TYPES
+@pytest.mark.parametrize("R,N", [(12000, 40), (20000, 33), (3000, 1024), (900, 4096), (2000, 1025), (1300, 4099)])
+def test_norm_of_more_rows_than_run_at_once(dt, R, N):
+    """Every kernel's loop over rows, the wide one's too."""
+    base.test_norm(dt, R, N)

@@ -195,3 +195,32 @@ def test_create_rejects_bad_sizes(real, kind, args, want):
 def test_null_handles(real):
     assert real.stacklstm_op_status(None) == ARG and real.stacklstm_op_set_stream(None, None) == ARG
     assert real.stacklstm_op_destroy(None) == OK and real.stacklstm_op_last_error(None) == b"null handle"
+
+
+def test_norm_workspace(lib):
+    """Nothing for wide rows until a backward wants their column sums, and those within a bound; all of
+    it at create for rows that fit registers, so that no call allocates."""
+    lib.cudaMalloc.argtypes = [ctypes.POINTER(vp), ctypes.c_size_t]
+
+    def allocated(f):  # (the stand-in's addresses follow one another)
+        a, b = vp(), vp()
+        lib.cudaMalloc(ctypes.byref(a), 0)
+        r = f()
+        lib.cudaMalloc(ctypes.byref(b), 0)
+        return r, b.value - a.value
+
+    P = t(8)
+    for dtype in (FP32, BF16):
+        h, n = allocated(lambda: create(lib, "norm", dtype, (1 << 16, 1 << 24)))
+        assert n < 1 << 20
+        assert allocated(lambda: lib.stacklstm_norm_forward(h, 1 << 16, *P[:3], 1e-5, *P[3:6]))[1] < 1 << 20
+        assert allocated(lambda: lib.stacklstm_norm_backward(h, 1 << 16, *P[:6], None, None))[1] < 1 << 20
+        st, n = allocated(lambda: lib.stacklstm_norm_backward(h, 1 << 16, *P))
+        assert st == OK and 8 << 24 <= n <= (4 << 30) + (1 << 20)
+        lib.stacklstm_op_destroy(h)
+        for N in (100, 1024, 4095, 4096):
+            h, n = allocated(lambda: create(lib, "norm", dtype, (1 << 16, N)))
+            assert 152 * 8 * N <= n < 11 << 20
+            st, n = allocated(lambda: lib.stacklstm_norm_backward(h, 1 << 16, *P))
+            assert st == OK and n < 1 << 20
+            lib.stacklstm_op_destroy(h)
