@@ -231,3 +231,56 @@ def test_norm_of_the_most_rows():
 def test_norm_of_more_rows_than_run_at_once(dt, R, N):
     """Every kernel's loop over rows, the wide one's too."""
     base.test_norm(dt, R, N)
+
+
+# ------------------------------------------------------------------ fp32 numbers as parts
+def one_a_row(rng, R, n, values):
+    """[R, n] with one value a row, in different columns while there are as many."""
+    a = np.zeros((R, n), np.float32)
+    a[np.arange(R), rng.permutation(np.resize(rng.permutation(n), R))] = values
+    return a
+
+
+def odd(rng, bits, *s):
+    """Numbers in [1, 2) of so many significant bits, the last one set."""
+    return (1 + (2 * rng.integers(0, 2 ** (bits - 2), s) + 1) / 2 ** (bits - 1)).astype(np.float32)
+
+
+# Products of 24 significant bits are exact in fp32, and so is every sum of their partial products:
+# a part or a partial product that were left out would show. (significant bits of the factors; a bf16
+# factor has 8 at most)
+EXACT = pytest.mark.parametrize("bits", [(24, 1), (1, 24), (12, 12), (16, 8), (8, 16)])
+
+
+def factor(rng, bits, *s):
+    return 2.0 ** rng.integers(-3, 4, s) if bits == 1 else odd(rng, bits, *s)
+
+
+@EXACT
+@pytest.mark.parametrize("R,K,N", [(5, 70, 33), (64, 200, 100), (130, 75, 300)])
+def test_linear_forward_takes_every_bit(bits, R, K, N):
+    rng = np.random.default_rng(R + K + sum(bits))
+    x, W = one_a_row(rng, R, K, factor(rng, bits[0], R)), np.float32(factor(rng, bits[1], N, K))
+    op = bd.stacklstm_linear_create(R, K, N, FP)
+    y = out(R, N)
+    bd.stacklstm_linear_forward(op, up(x), up(W), None, None, y)
+    assert np.array_equal(y.double().cpu().numpy(), x.astype(np.float64) @ W.T.astype(np.float64))
+
+
+@TYPES
+@EXACT
+@pytest.mark.parametrize("R,K,N", [(20, 70, 33), (60, 75, 200), (290, 140, 300)])
+def test_linear_backward_takes_every_bit(dt, bits, R, K, N):
+    """dz is in three parts, x and W of fp32 too."""
+    if dt == BF and bits[1] > 8:
+        pytest.skip("not a bf16 number")
+    rng = np.random.default_rng(R + K + sum(bits))
+    dy = one_a_row(rng, R, N, factor(rng, bits[0], R))  # (no column of it has two values: R <= N)
+    x, W = np.float32(factor(rng, bits[1], R, K)), np.float32(factor(rng, bits[1], N, K))
+    op = bd.stacklstm_linear_create(R, K, N, dt)
+    dx, dW, db = out(R, K), out(N, K), out(N)
+    bd.stacklstm_linear_backward(op, up(dy), up(x, tdt(dt)), up(W, tdt(dt)), None, None, dx, dW, db)
+    dy = dy.astype(np.float64)
+    assert np.array_equal(dx.double().cpu().numpy(), dy @ W.astype(np.float64))
+    assert np.array_equal(dW.double().cpu().numpy(), dy.T @ x.astype(np.float64))
+    assert np.array_equal(db.double().cpu().numpy(), dy.sum(0))
