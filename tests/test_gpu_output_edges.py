@@ -284,3 +284,85 @@ def test_linear_backward_takes_every_bit(dt, bits, R, K, N):
     assert np.array_equal(dx.double().cpu().numpy(), dy @ W.astype(np.float64))
     assert np.array_equal(dW.double().cpu().numpy(), dy.T @ x.astype(np.float64))
     assert np.array_equal(db.double().cpu().numpy(), dy.sum(0))
+
+
+# ------------------------------------------------------------------ more than 2^32 elements
+def test_norm_offsets_beyond_32_bits():
+    """The first and the last rows of 2^32 elements and more."""
+    N = 1024
+    R = (1 << 32) // N + 5
+    x = torch.empty(R, N, dtype=torch.bfloat16, device="cuda").normal_()
+    dy, dx = torch.zeros(R, N, device="cuda"), torch.full((R, N), math.nan, device="cuda")
+    dy[-3:].normal_()
+    y, mean, rstd, dg, db = torch.zeros_like(x), out(R), out(R), out(N), out(N)
+    op = bd.stacklstm_norm_create(R, N, BF)
+    bd.stacklstm_norm_forward(op, x, None, None, 1e-5, y, mean, rstd)
+    bd.stacklstm_norm_backward(op, dy, x, None, mean, rstd, dx, dg, db)
+    ends = torch.tensor([0, 1, R - 3, R - 2, R - 1], device="cuda")
+    at = lambda t: base.f64(t[ends])
+    wy, wm, wr = ol.norm_forward(at(x), None, None, 1e-5)
+    # bounds as for smaller tensors, with |x| < 8 and 1 / 2 < rstd < 2 in these rows
+    n = 2 * base.U * (N + 16)
+    base.within(at(mean), wm, n * 8, "mean")
+    base.within(at(rstd), wr, 2 * n * 17 * wr, "rstd")
+    base.within(at(y), wy, 40 * n * (1 + np.abs(wy)) + 2.0 ** -8 * np.abs(wy), "y")
+    wdx, wdg, wdb = ol.norm_backward(at(dy), at(x), None, at(mean), at(rstd))
+    base.within(at(dx), wdx, 40 * n * (1 + np.abs(at(dy)).max()), "dx")
+    base.within(base.f64(dg), wdg, 2.0 ** -20 * np.abs(at(dy) * 8).sum(0), "dgamma")
+    base.within(base.f64(db), wdb, 2.0 ** -20 * np.abs(at(dy)).sum(0), "dbeta")
+    assert not dx[:-3].any()
+
+
+@TYPES
+def test_linear_offsets_beyond_32_bits(dt):
+    K, N = 64, 32003
+    R = (1 << 32) // N + 7
+    rng = np.random.default_rng(0)
+    W, Wd = base.rounded(rng, dt, N, K, scale=1 / 8)
+    xd = torch.empty(R, K, device="cuda").normal_().to(tdt(dt))
+    op = bd.stacklstm_linear_create(R, K, N, dt)
+    y = torch.zeros(R, N, dtype=tdt(dt), device="cuda")
+    bd.stacklstm_linear_forward(op, xd, Wd, None, None, y)
+    bd.stacklstm_op_status(op)
+    ends = torch.tensor([0, 1, R - 3, R - 2, R - 1], device="cuda")
+    x = base.f64(xd[ends])
+    want = x @ W.T
+    base.within(y[ends], want, 2 * base.U * (K + 16) * (np.abs(x) @ np.abs(W).T) + base.out_tol(dt, want), "y")
+    assert y.count_nonzero(1).ge(N // 2).all()  # every row is written
+    del y
+    dy = torch.zeros(R, N, device="cuda")
+    dy[-3:].normal_()
+    dx, dW, db = torch.full((R, K), math.nan, device="cuda"), out(N, K), out(N)
+    bd.stacklstm_linear_backward(op, dy, xd, Wd, None, None, dx, dW, db)
+    bd.stacklstm_op_status(op)
+    d = base.f64(dy[-3:])
+    wx, wW, wb, _ = ol.linear_backward(d, x[-3:], W, None, None, "none")
+    base.within(dx[-3:], wx, 2 * base.U * (N + 16) * (np.abs(d) @ np.abs(W)) + 4 * base.U * np.abs(wx), "dx")
+    # (zeros add nothing: sums of three terms, in parts)
+    base.within(dW, wW, 2.0 ** -19 * (np.abs(d).T @ np.abs(x[-3:])), "dW")
+    base.within(db, wb, 2.0 ** -20 * np.abs(d).sum(0), "dbias")
+    assert not dx[:-3].any()
+
+
+@TYPES
+@pytest.mark.parametrize("R,K,N", [(20, 70, 33), (130, 75, 300), (300, 136, 264)])
+def test_linear_infinities_and_nan_stay_where_they_enter(dt, R, K, N):
+    rng = np.random.default_rng(R)
+    x, W, dy = base.rounded(rng, dt, R, K)[1], base.rounded(rng, dt, N, K)[1], up(rng.normal(size=(R, N)))
+    x[3, 5], x[R - 1, K - 1], W[N - 1, 2], dy[7, 11] = math.inf, math.nan, -math.inf, math.nan
+    op = bd.stacklstm_linear_create(R, K, N, dt)
+    y, dx, dW, db = out(R, N, dtype=tdt(dt)), out(R, K), out(N, K), out(N)
+    bd.stacklstm_linear_forward(op, x, W, None, None, y)
+    bd.stacklstm_linear_backward(op, dy, x, W, None, None, dx, dW, db)
+    bd.stacklstm_op_status(op)
+
+    def only(t, rows, cols):
+        bad = torch.zeros(t.shape, dtype=torch.bool, device="cuda")
+        bad[rows] = True
+        bad[..., cols] = True
+        assert torch.equal(~t.isfinite(), bad)
+
+    only(y, [3, R - 1], [N - 1])
+    only(dx, [7], [2])
+    only(dW, [11], [5, K - 1])
+    assert (~db.isfinite()).nonzero().flatten().tolist() == [11]
