@@ -390,7 +390,8 @@ const char *stacklstm_head_last_error(stacklstm_head_t h);
  * (SL_ERR_ARG otherwise). Calls are ordered on the handle's stream and return after
  * enqueueing; stacklstm_op_status reports what the device detected. `rows` may be anything
  * from 0 to the R of create. A handle's workspace grows to the largest call so far (the first
- * such call allocates and, where it replaces a smaller buffer, waits for the stream).
+ * such call allocates and, where it replaces a smaller buffer, waits for the stream; a call that
+ * is to be captured in a graph is made once before).
  */
 typedef struct stacklstm_op *stacklstm_op_t;
 
@@ -435,10 +436,14 @@ typedef enum { SL_ACT_NONE = 0, SL_ACT_RELU = 1, SL_ACT_TANH = 2, SL_ACT_GELU = 
  *   nullable, overwritten) dx [rows, K], dW [N, K], dbias [N]. The residual's gradient is dy.
  * The contractions run on the tensor cores with fp32 accumulation. fp32 numbers (x and W of
  * SL_FP32, dz always) enter as three bf16 parts each, 24 significant bits, and products below
- * 2^-23 of the leading one are left out: results have fp32 accuracy. A value that is not
+ * 2^-23 of the leading one are left out. The tensor cores' additions cut where fp32 ones round to
+ * nearest: fp32 results (gradients, SL_FP32 outputs) are up to 6e-7 of their size off, whatever the
+ * contraction's length; a plain fp32 sum is 1.6e-7 off for contractions of tens and 3e-6 for
+ * tens of thousands. bf16 results have 1.7e-8 K / 16 before their rounding. A value that is not
  * finite makes the outputs it enters not finite (inf may become NaN).
- * The first backward allocates 6 rows N bytes of workspace (and 4 rows N / 64 for dbias);
- * SL_FP32 6 (rows + N) K for the parts. Where the outputs are few and the contraction long, a
+ * The first backward allocates 6 rows N bytes of workspace (and 4 rows N / 64 for dbias); the first
+ * call of either kind 6 (rows + N) K for the parts of an SL_FP32 x and W, or 2 (rows + N) K for copies
+ * of bf16 ones whose K is not a multiple of 8. Where the outputs are few and the contraction long, a
  * call splits it and allocates the splits' partial sums, 4 bytes an output and split, 1 GiB at most.
  */
 sl_status stacklstm_linear_create(stacklstm_op_t *out, int R, int K, int N, sl_dtype dtype, sl_act act, int device,

@@ -161,7 +161,7 @@ struct Row {
 };
 
 // Rows of up to 4 pieces a lane: TPR lanes (8 or 32) to a row, NP pieces a lane in registers, as
-// they lie in memory. A call of 11840 x 83 fp32 with 8 entries a row is 6.3 us, bound by the call.
+// they lie in memory. A call of 11840 x 83 fp32 with 8 entries a row is 6.4 us, bound by the call.
 template <typename T, int TPR, int NP>
 __global__ void __launch_bounds__(256, 5)
 distill_narrow(const __grid_constant__ DistillArgs a)

@@ -56,9 +56,10 @@ __device__ __forceinline__ float act_f(float z, int act)
 }
 // The same for a result that is rounded to bf16. Phi(z) = 1 - h / 2 (z >= 0), h / 2 (z < 0) with
 // h = erfc(|z| / sqrt 2) = t (a1 + t (a2 + ...)) exp(-z^2 / 2), t = 1 / (1 + p |z| / sqrt 2), by formula
-// 7.1.26 of Abramowitz and Stegun's Handbook of Mathematical Functions (error 1.5e-7), a third of
-// erff's instructions, which bounded the layer; the sigmoid by the hardware's exponential and
-// quotient (2^-21).
+// 7.1.26 of Abramowitz and Stegun's Handbook of Mathematical Functions (of erf, error 1.5e-7: of gelu
+// 2e-7 in all, below bf16 rounding down to z = -5; relative to what is left of it there, 2e-3 at -5,
+// 2e-2 at -10), a third of erff's instructions, which bounded the layer; the sigmoid by the hardware's
+// exponential and quotient (2^-21; the quotient is 0 below z = -87.3, where silu is above -1.1e-36).
 __device__ __forceinline__ float act_f_bf16(float z, int act)
 {
     if (act == kActGelu) {
@@ -711,8 +712,13 @@ __device__ __forceinline__ void prefetch_map(const void *tmap)
 // A part is loaded once a chunk, whatever number of products it is in, small products first.
 // MN-major operands: blocks of 64 columns, each 64 rows of 128 bytes.
 // Bound by the tensor cores where the contraction is long: both products of the backward at 4096 x
-// 1024 x 32003 bf16, with the 245 us of their parts, 1287 us, as pairs of CTAs on 256 x 256 tiles.
-// Bound by shared memory where it is short: forward 65536 x 1024 x 1024, gelu, residual and pre, 145 us.
+// 1024 x 32003 bf16, with the 245 us of their parts, 1280 us, as pairs of CTAs on 256 x 256 tiles.
+// Bound by its output warps where it is short: forward 65536 x 1024 x 1024, gelu, residual and pre, 146
+// us, 15 rounds of tiles of 19 thousand cycles each, of which the MMAs take 8. Nothing is saturated there
+// (16384 rows: tensor pipe 34 %, issue 42 %, shared memory's data banks 12 %): the warps wait, for
+// loads most of all (2.8 of 11.9 cycles an instruction), then for instructions (1.6).
+// bf16 results come from one accumulator, whatever K is: 1.7e-8 of it an MMA, 16 of K (2^-11.8 at K =
+// 2^18, where a bf16 result is rounded by 2^-9).
 template <int BN, bool A_MN, bool B_MN, int PA, int PB, int EPI, int CG>
 __global__ void __launch_bounds__(gemm_threads(EPI), EPI == 4 ? 2 : 1)
 gemm_parts(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
