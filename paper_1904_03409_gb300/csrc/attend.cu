@@ -574,7 +574,8 @@ attend_forward(const __grid_constant__ Maps<NP> tm, const __grid_constant__ FwdA
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
-        for (uint64_t *bar = full_k; bar <= done; ++bar) tc::mbar_init(bar, bar >= z_read && bar < o_full ? 4 : 1);
+        // (empty_v: the MMAs and warp 2, which has to have seen every tile of a place before the next one's load ends)
+        for (uint64_t *bar = full_k; bar <= done; ++bar) tc::mbar_init(bar, bar >= z_read && bar < o_full ? 4 : bar >= empty_v && bar < q_full ? 2 : 1);
         init_items(ring, 6);
         *abort = 0;
         tc::fence_mbar_init();
@@ -737,6 +738,7 @@ attend_forward(const __grid_constant__ Maps<NP> tm, const __grid_constant__ FwdA
                 for (int i = 0; i < n; ++i, ++m) {
                     const int s = m % NS, rows = w.len - (lo + i) * kKeys;
                     if (!warp_wait(&full_v[s], (uint32_t)(m / NS) & 1, limit, abort)) return false;
+                    if (lane == 0) tc::mbar_arrive(&empty_v[s]);  // (a wait by parity must not miss a load: this warp may be late)
                     if (rows >= kKeys) continue;
                     for (int k = 0; k < NP * DB; ++k)
                         zero_shared(sm + Sh::kV0 + s * Sh::kKV + k * kKBlock + rows * 128, kKBlock - rows * 128, lane, 32);
@@ -1553,7 +1555,8 @@ attend_grad_queries(const __grid_constant__ BwdMaps<NP> tm, const __grid_constan
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
-        for (uint64_t *bar = full_k; bar <= done; ++bar) tc::mbar_init(bar, bar == z_read || bar == z_ready ? 4 : 1);
+        // (empty_k: the MMAs and warp 2, as empty_v of the forward)
+        for (uint64_t *bar = full_k; bar <= done; ++bar) tc::mbar_init(bar, bar == z_read || bar == z_ready ? 4 : bar >= empty_k && bar < empty_v ? 2 : 1);
         init_items(ring, 6);
         *abort = 0;
         tc::fence_mbar_init();
@@ -1735,6 +1738,7 @@ attend_grad_queries(const __grid_constant__ BwdMaps<NP> tm, const __grid_constan
                 for (int i = 0; i < n; ++i, ++m) {
                     const int s = m % NS, rows = w.len - (lo + i) * kKeys;
                     if (!warp_wait(&full_k[s], (uint32_t)(m / NS) & 1, limit, abort)) return false;
+                    if (lane == 0) tc::mbar_arrive(&empty_k[s]);
                     if (rows >= kKeys) continue;
                     for (int k = 0; k < NP * DB; ++k)
                         zero_shared(sm + Sh::kK0 + s * Sh::kK + k * kKBlock + rows * 128, kKBlock - rows * 128, lane, 32);
