@@ -526,9 +526,9 @@ sl_status stacklstm_beam_push(stacklstm_op_t op, const int8_t *ops, const void *
  *   of a sentence without states: y = 0, lse = -inf.
  * backward: dy float; q, k, v, lengths, scale as in the forward; lse its output; ctx its ctx (SL_FP32:
  *   its y); outputs (float, each nullable, overwritten) dq, dk, dv; 0 behind a sentence's end.
- * SL_BF16 without ctx rounds the weights exp(z - largest z) to bf16 (y is then within 2^-8 of its
- * rounded value's size or so); with ctx, and in every gradient, weights and dy enter as three bf16 parts:
- * fp32 accuracy. A length outside its range counts as the nearest one and is reported
+ * SL_BF16 without ctx takes the weights exp(z - largest z) as two bf16 parts (2^-15 of them at most is left
+ * out, before y is rounded by up to 2^-8); with ctx, and in every gradient, weights and dy enter as three: fp32
+ * accuracy. A length outside its range counts as the nearest one and is reported
  * (SL_ERR_ARG). Workspace: q, k, v as parts (6 bytes an element of SL_FP32; 2 of SL_BF16 with D not a
  * multiple of 8), dy as parts (6) and 4 bytes a query and head; where there are few sentences, heads and
  * tiles the sums of splits: 4 bytes an element of y, of dk and dv, or of dq, and split (32 at most).

@@ -362,6 +362,23 @@ __device__ __forceinline__ float2 less_upper2(float2 v)
     return __fadd2_rn(v, make_float2(-__uint_as_float(__float_as_uint(v.x) & 0xffff0000u), -__uint_as_float(__float_as_uint(v.y) & 0xffff0000u)));
 }
 
+// acc += D columns of a lane, so many at a time.
+template <int DP, int STEP>
+__device__ __forceinline__ void add_columns(uint32_t at, int D, float2 (&acc)[DP / 2])
+{
+#pragma unroll
+    for (int i = 0; i < DP; i += STEP)
+        if (i < D) {  // (what is past D is not used)
+            uint32_t v[STEP / 16][16];
+#pragma unroll
+            for (int j = 0; j < STEP / 16; ++j) tc::tmem_ld16_async(at + i + 16 * j, v[j]);
+            tc::tmem_wait_ld();
+#pragma unroll
+            for (int j = 0; j < STEP / 2; ++j)
+                acc[i / 2 + j] = __fadd2_rn(acc[i / 2 + j], make_float2(__uint_as_float(v[j / 8][2 * j % 16]), __uint_as_float(v[j / 8][2 * j % 16 + 1])));
+        }
+}
+
 __device__ __forceinline__ void zero_shared(uint32_t at, uint32_t bytes, int thread, int threads)
 {
     const uint32_t z[4] = {0, 0, 0, 0};
@@ -497,7 +514,9 @@ attend_pack(const __grid_constant__ Packs a)
 constexpr int kRows = 128, kKeys = 64;  // of a tile
 constexpr uint32_t kQBlock = kRows * 128, kKBlock = kKeys * 128;  // bytes of 64 columns of a tile
 
-// NP: parts of q, k and v; PP: of w (one for a bf16 result, three for an fp32 one).
+// NP: parts of q, k and v; PP: of w. Three of them are w; two (the second rounded) leave out at most 2^-15 of it, which a
+// bf16 result, rounded by up to 2^-8, does not show: 4 x 2048 x 4096, heads of 128, is 1.66e-3 off 64 bits, the rounding
+// alone, in 130 us (of one part 2.3e-3, 107 us; of three 281 us, sums in registers).
 template <int NP, int PP, int DP>
 struct FwdShape {
     static constexpr int DB = DP / 64;
@@ -510,12 +529,14 @@ struct FwdShape {
     static constexpr uint32_t kBars = (5 * kStages + 2 * kQs + 7) * 8 + 16;
     static constexpr uint32_t kSmem = 1024 + kMain + kBars;
     // tensor memory: z, w, w v; where that is more than an SM's half, w over z's second half (which is read first). A
-    // bf16 result's sum of w v stays there, with two places for w in turn; an fp32 result's is added up in
-    // registers, tile by tile
-    static constexpr bool kSums = PP == 1;
+    // bf16 result's sum of w v stays there, with two places for w in turn where there is room; an fp32 result's is added
+    // up in registers, tile by tile. (w over the tile's own z, two places of both in turn, with heads of 128: 4 x 2048 x 4096
+    // 191 us of equal sentences, 173 so.)
+    static constexpr bool kSums = PP == 2;
     static constexpr bool kOver = kCtas == 2 && kKeys + PP * kKeys / 2 + DP > 256;
-    static constexpr uint32_t kWs = kSums ? 2 : 1;  // places for w
+    static constexpr uint32_t kWs = kSums && DP == 64 ? 2 : 1;  // places for w
     static constexpr uint32_t kColW = kOver ? kKeys / 2 : kKeys, kColO = kColW + kWs * PP * kKeys / 2;
+    static __device__ uint32_t col_w(int tile, int part) { return kColW + ((uint32_t)tile % kWs * PP + part) * (kKeys / 2); }
     static constexpr uint32_t kCols = kColO + DP <= 256 ? 256 : 512;
     static_assert(kSmem + sizeof(ItemRing) <= (kCtas == 2 ? 113 : 227) * 1024 && (kCtas == 1 || kCols == 256), "tensor and shared memory of a CTA");
 };
@@ -551,9 +572,8 @@ __device__ __forceinline__ void key_tiles(const FwdArgs &g, const Item &w, int &
 // clears what lies behind a sentence's last state, and a thread of warps 4 to 7 has a query: 32 z of a tile at a time
 // in registers, and an fp32 result's sum of w v.
 // Bound by a tile's chain of MMA, reading z, exponentials and writing w, which two CTAs an SM and z one tile ahead hide
-// in part: 64 x 256 x 256, 16 heads of 64, bf16, 44 us (issue 43 %, tensor pipe 19 %), 72 for an fp32 result too; 4 x
-// 2048 x 4096, 8 heads of 128 over 2, 105 us (580 TFLOP/s). Eight queries over 4096 states of 64 x 16 heads of 64: by HBM,
-// 189 us, 5.7 TB/s.
+// in part: 64 x 256 x 256, 16 heads of 64, bf16, 52 us, 72 for an fp32 result too; 4 x 2048 x 4096, 8 heads
+// of 128 over 2, 130 us (470 TFLOP/s).
 template <int NP, int PP, int DP>
 __global__ void __launch_bounds__(256, FwdShape<NP, PP, DP>::kCtas)
 attend_forward(const __grid_constant__ Maps<NP> tm, const __grid_constant__ FwdArgs g)
@@ -597,7 +617,7 @@ attend_forward(const __grid_constant__ Maps<NP> tm, const __grid_constant__ FwdA
     };
 
     if (warp < 4) {
-        if constexpr (Sh::kCtas == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PP == 1 ? 80 : 48));
+        if constexpr (Sh::kCtas == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Sh::kSums ? 80 : 48));
         const bool issues = elect_one();
         if (warp == 0) {
             int m = 0, nv = 0, j = 0;  // loads of k, of v, of queries
@@ -696,7 +716,7 @@ attend_forward(const __grid_constant__ Maps<NP> tm, const __grid_constant__ FwdA
                     for (int p = 0; p < PO.n; ++p)
 #pragma unroll
                         for (int k = 0; k < kKeys / 16; ++k)
-                            mma_ts(tmem + Sh::kColO, tmem + Sh::kColW + ((uint32_t)m % Sh::kWs + PO.a[p]) * (kKeys / 2) + k * 8,
+                            mma_ts(tmem + Sh::kColO, tmem + Sh::col_w(m, PO.a[p]) + k * 8,
                                    av + desc_lower(kKBlock) + ((Sh::kV0 + PO.b[p] * DB * kKBlock) >> 4) + k * 128, id_o, p || k || (Sh::kSums && !starts));
                     tc::mma_commit(&empty_v[s]);
                     tc::mma_commit(&o_full[(uint32_t)m % Sh::kWs]);
@@ -752,7 +772,7 @@ attend_forward(const __grid_constant__ Maps<NP> tm, const __grid_constant__ FwdA
         }
         __syncwarp();
     } else {
-        if constexpr (Sh::kCtas == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(PP == 1 ? 176 : 208));  // (of 256 x 128 in all)
+        if constexpr (Sh::kCtas == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Sh::kSums ? 176 : 208));  // (of 256 x 128 in all)
         const int q = warp & 3, r = q * 32 + lane;
         const int t_in = r / g.G, head_in = r % g.G;
         const uint32_t at = tmem + ((uint32_t)(q * 32) << 16), stage = sm + Sh::kStage0 + q * kStageBytes;
@@ -771,7 +791,7 @@ attend_forward(const __grid_constant__ Maps<NP> tm, const __grid_constant__ FwdA
             const int t = w.tile * g.tq + t_in, head = w.kvh * g.G + head_in, len = w.len;
             const bool there = r < g.tq * g.G && t < g.T, here = there && t < w.q_len;
             const bool busy = __any_sync(0xffffffffu, here);  // a warp of no queries only keeps the count
-            float2 o[DP / 2];
+            float2 o[Sh::kSums ? 1 : DP / 2];
             if constexpr (!Sh::kSums)
 #pragma unroll
                 for (int i = 0; i < DP / 2; ++i) o[i] = make_float2(0.0f, 0.0f);
@@ -903,7 +923,7 @@ attend_forward(const __grid_constant__ Maps<NP> tm, const __grid_constant__ FwdA
 #pragma unroll
                             for (int j = 0; j < CZ / 2; ++j) {
                                 float2 &a = z[j];
-                                if constexpr (PP == 1) {
+                                if (PP == 2 && p == 1) {  // (rounded, so that sums have no bias)
                                     const __nv_bfloat162 x = __floats2bfloat162_rn(a.x, a.y);
                                     wp[j] = *(const uint32_t *)&x;
                                 } else {
@@ -911,7 +931,7 @@ attend_forward(const __grid_constant__ Maps<NP> tm, const __grid_constant__ FwdA
                                     if (p < PP - 1) a = less_upper2(a);
                                 }
                             }
-                            tmem_st(at + Sh::kColW + ((uint32_t)mi % Sh::kWs + p) * (kKeys / 2) + CZ / 2 * h, wp);
+                            tmem_st(at + Sh::col_w(mi, p) + CZ / 2 * h, wp);
                         }
                     }
                     sum[0] = __fadd2_rn(sum[0], sum[1]);
@@ -926,12 +946,8 @@ attend_forward(const __grid_constant__ Maps<NP> tm, const __grid_constant__ FwdA
             }
             m0 += n;
             if (n > 0 && !summed(m0 - 1)) return false;
-            if constexpr (Sh::kSums) {
-#pragma unroll
-                for (int i = 0; i < DP / 2; ++i) o[i] = make_float2(0.0f, 0.0f);
-                alpha = 0.0f;
-            }
-            if (n > 0 && busy) add_o();
+            if constexpr (!Sh::kSums)
+                if (n > 0 && busy) add_o();
             if (!__any_sync(0xffffffffu, there)) return true;
             const bool some = here && n > 0;
             const float by = some ? 1.0f / l : 0.0f;
@@ -940,12 +956,28 @@ attend_forward(const __grid_constant__ Maps<NP> tm, const __grid_constant__ FwdA
             const float lse = some ? (l == INFINITY ? l : fmaf(m, g.scale, fmaf(-kLn2, off, logf(l)))) : -INFINITY;
             const size_t row = (size_t)w.b * g.q_b + (size_t)t * g.q_t + head;
             const bool pieces = g.D % 8 == 0;
-            if (g.part) {
-                put_rows<float, DP>(stage, some ? g.part + (w.sp * g.rows + row) * g.Dp : nullptr, o, g.Dp, by, false, true);
+            // CD of the outputs' columns, from d0 on
+            auto put = [&](auto &v, int d0) __attribute__((always_inline)) {
+                constexpr int CD = 2 * (sizeof v / sizeof v[0]);
+                if (g.part) {
+                    put_rows<float, CD>(stage, some ? g.part + (w.sp * g.rows + row) * g.Dp + d0 : nullptr, v, min(g.Dp - d0, CD), by, false, true);
+                } else {
+                    using T = typename Sh::Out;
+                    put_rows<T, CD>(stage, there ? (T *)g.y + row * g.D + d0 : nullptr, v, min(g.D - d0, CD), by, !some, pieces);
+                    if (PP == 3 && g.ctx) put_rows<float, CD>(stage, there ? g.ctx + row * g.D + d0 : nullptr, v, min(g.D - d0, CD), by, !some, pieces);
+                }
+            };
+            if constexpr (Sh::kSums) {  // 64 columns at a time (all 128: 0.7 KB of spills)
+#pragma unroll 1
+                for (int d0 = 0; d0 < g.D; d0 += 64) {
+                    float2 v[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = make_float2(0.0f, 0.0f);
+                    if (n > 0 && busy) add_columns<64, 32>(at + Sh::kColO + d0, g.D - d0, v);
+                    put(v, d0);
+                }
             } else {
-                using T = typename Sh::Out;
-                put_rows<T, DP>(stage, there ? (T *)g.y + row * g.D : nullptr, o, g.D, by, !some, pieces);
-                if (PP == 3 && g.ctx) put_rows<float, DP>(stage, there ? g.ctx + row * g.D : nullptr, o, g.D, by, !some, pieces);
+                put(o, 0);
             }
             float *const lses = g.part ? g.part_lse + w.sp * g.rows : g.lse;
             if (lses && there) lses[row] = lse;
@@ -1084,23 +1116,6 @@ __device__ __forceinline__ void read32(uint32_t at, float2 (&z)[16])
 #pragma unroll
     for (int j = 0; j < 16; ++j) z[j] = pair_of(v, j);
 }
-// acc += D columns of a lane, so many at a time.
-template <int DP, int STEP>
-__device__ __forceinline__ void add_columns(uint32_t at, int D, float2 (&acc)[DP / 2])
-{
-#pragma unroll
-    for (int i = 0; i < DP; i += STEP)
-        if (i < D) {  // (what is past D is not used)
-            uint32_t v[STEP / 16][16];
-#pragma unroll
-            for (int j = 0; j < STEP / 16; ++j) tc::tmem_ld16_async(at + i + 16 * j, v[j]);
-            tc::tmem_wait_ld();
-#pragma unroll
-            for (int j = 0; j < STEP / 2; ++j)
-                acc[i / 2 + j] = __fadd2_rn(acc[i / 2 + j], make_float2(__uint_as_float(v[j / 8][2 * j % 16]), __uint_as_float(v[j / 8][2 * j % 16 + 1])));
-        }
-}
-
 // ---- the states' gradients. For a tile of KT states and one of 64 query rows, states in the lanes of tensor memory:
 //   z^T = k q^T,  (dw)^T = v dy^T  [KT][64];   dv += w^T dy,  dk += (dz)^T q  [KT][D]
 template <int NP, int DP>
@@ -2158,7 +2173,7 @@ sl_status stacklstm_attend_forward(stacklstm_op_t op, int T, int S, const void *
         else if (ctx)
             e = wide ? launch_forward<1, 3, 128>(op, c, o, g) : launch_forward<1, 3, 64>(op, c, o, g);
         else
-            e = wide ? launch_forward<1, 1, 128>(op, c, o, g) : launch_forward<1, 1, 64>(op, c, o, g);
+            e = wide ? launch_forward<1, 2, 128>(op, c, o, g) : launch_forward<1, 2, 64>(op, c, o, g);
     }
     return e ? op_cuda(op, e, "stacklstm_attend_forward") : SL_OK;
 }

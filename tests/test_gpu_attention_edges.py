@@ -1,10 +1,12 @@
 """Calls of the attention, the log probabilities, the dropout and the attentive layers at the ends of what they take:
 late warps, long memories, shifted logits, large scores, padding. Tolerances as in test_gpu_attention.py."""
+import numpy as np
 import pytest
 import torch
 
+from oracle import attention as at
 from paper_1904_03409_gb300 import binding as bd
-from test_gpu_attention import BF, FP, TYPES, empty, tdt
+from test_gpu_attention import BF, FP, TYPES, U, Case, empty, tdt, within
 
 pytestmark = pytest.mark.gpu
 
@@ -33,3 +35,20 @@ def test_many_short_sentences_with_broken_tiles(dt, D):
         assert not any(torch.isnan(t).any() for t in out)
         assert first is None or all(torch.equal(a, b) for a, b in zip(out, first))
         first = first or out
+
+
+@pytest.mark.parametrize("B,T,S,nh,nk,D", [(1, 8, 40, 5, 5, 40), (2, 64, 65, 2, 2, 63), (1, 65, 128, 1, 1, 128), (1, 129, 129, 2, 1, 72),
+                                           (1, 127, 300, 4, 2, 100), (1, 2, 1100, 6, 2, 32), (2, 5, 3000, 4, 1, 64)])
+def test_a_bf16_result_alone_keeps_its_weights(B, T, S, nh, nk, D):
+    """Without ctx as with it: y is what the weights in fp32 give, rounded once. Two bf16 parts of a weight, the first cut (which
+    leaves less than 2^-7 of it) and the second rounded by up to 2^-8 of that, leave out 2^-15; of each tile of 64 states eight additions
+    cut, each by less than 2^-23 of the sum so far (which is at most the sum of magnitudes)."""
+    c = Case(BF, B, T, S, nh, nk, D)
+    want, _, w = at.attend(*c.x, c.q_len, c.kv_len, float(c.scale))
+    of = np.arange(nh) * nk // nh
+    zmag = float(c.scale) * np.einsum("tbhd,sbhd->bhts", np.abs(c.x[0]), np.abs(c.x[1])[:, :, of])
+    rel = 2 * (2 * U * (D + 8) + 4 * U) * zmag.max(3) + 4 * U * (S + 16) + 2.0 ** -20  # of a weight, as in Case.check
+    wv = np.einsum("bhts,sbhd->tbhd", w, np.abs(c.x[2])[:, :, of])
+    tol = (2 * rel.transpose(2, 0, 1)[..., None] + 2.0 ** -15 + 8 * 2.0 ** -23 * (S / 64 + 1)) * wv
+    _, y, _, _ = c.forward(c.handle(), False)
+    within(c.back(y, nh), want, tol * (1 + 2.0 ** -7) + 2.0 ** -8 * np.abs(want), "y")
