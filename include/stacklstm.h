@@ -531,7 +531,8 @@ sl_status stacklstm_beam_push(stacklstm_op_t op, const int8_t *ops, const void *
  * accuracy. A length outside its range counts as the nearest one and is reported
  * (SL_ERR_ARG). Workspace: q, k, v as parts (6 bytes an element of SL_FP32; 2 of SL_BF16 with D not a
  * multiple of 8), dy as parts (6) and 4 bytes a query and head; where there are few sentences, heads and
- * tiles the sums of splits: 4 bytes an element of y, of dk and dv, or of dq, and split (32 at most).
+ * tiles the sums of splits: 4 bytes an element of y, of dk and dv, or of dq, and split (32 at most); 4 bytes an
+ * element of a bf16 y without ctx over more than 4096 states.
  */
 typedef enum { SL_TIME_MAJOR = 0, SL_BATCH_MAJOR = 1 } sl_layout;
 sl_status stacklstm_attend_create(stacklstm_op_t *out, int T, int S, int B, int heads, int kv_heads, int D, sl_dtype dtype,

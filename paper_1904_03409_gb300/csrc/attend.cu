@@ -13,8 +13,9 @@
 // A bf16 tensor is one operand; an fp32 number is the sum of three bf16 parts (8 + 8 + 8 significant
 // bits) and the product of two of them six partial products, of one with a bf16 number three (what is
 // left out is below 2^-23 of it). So gradients, which are fp32, have fp32's accuracy whatever the
-// inputs' type: dy, w and dz enter as three parts. The tensor cores' additions cut, so no accumulator
-// takes more than one tile's products: threads add the tiles up in registers, in fp32.
+// inputs' type: dy, w and dz enter as three parts. The tensor cores' additions cut, so that an accumulator's error
+// grows with what it takes: one tile's products (threads add the tiles up in registers, in fp32), or for a bf16
+// result those of kRun tiles.
 //
 // Queries of the heads that share a state's head lie side by side: row r of a tile is query
 // t0 + r / G of head r % G of the G, so that a tile reads the states once for all of them, and their
@@ -533,6 +534,9 @@ struct FwdShape {
     // up in registers, tile by tile. (w over the tile's own z, two places of both in turn, with heads of 128: 4 x 2048 x 4096
     // 191 us of equal sentences, 173 so.)
     static constexpr bool kSums = PP == 2;
+    // Tiles whose w v are summed in tensor memory before the sum goes to memory, where it is added up in fp32: 8 additions a
+    // tile that cut by less than 2^-23 of the sum each, 2^-14 in all. (Of 2^20 states in one sum y was 0.9 % too small.)
+    static constexpr int kRun = 64;
     static constexpr bool kOver = kCtas == 2 && kKeys + PP * kKeys / 2 + DP > 256;
     static constexpr uint32_t kWs = kSums && DP == 64 ? 2 : 1;  // places for w
     static constexpr uint32_t kColW = kOver ? kKeys / 2 : kKeys, kColO = kColW + kWs * PP * kKeys / 2;
@@ -549,6 +553,7 @@ struct FwdArgs {
     void *y;
     float *lse, *ctx;
     float *part, *part_lse;   // [split][rows][Dp] and [split][rows], or null
+    float *sums;              // [split][rows][Dp], part or a buffer by itself: a bf16 result's sums of the runs before
     int split, per;           // splits of the key tiles, key tiles of a split
     int tq, tiles, items;     // queries of a tile, tiles; all items
     size_t rows;              // B T heads
@@ -673,7 +678,7 @@ attend_forward(const __grid_constant__ Maps<NP> tm, const __grid_constant__ FwdA
             const int steps = (g.D + 15) / 16;
             int m = -1, j = 0;   // the tile whose w v is next; items begun
             uint32_t cut = 0;    // cleared tiles of each place, modulo 2
-            bool starts = false, partial = false;  // of tile m: is it its item's first, are states of it cleared
+            bool starts = false, partial = false;  // of tile m: does it begin a sum, are states of it cleared
             auto scores = [&](int m, bool first, bool last) {  // z of tile m of item j (first, last: of the item)
                 const int s = m % NS, qs = j % QS;
                 if (first && !warp_wait(&q_full[qs], (uint32_t)(j / QS) & 1, limit, abort)) return false;
@@ -738,7 +743,7 @@ attend_forward(const __grid_constant__ Maps<NP> tm, const __grid_constant__ FwdA
                     held = true;
                     ++m;
                     if (i == n - 1) ++j;
-                    starts = i == 0;
+                    starts = i % Sh::kRun == 0;
                     partial = (lo + i + 1) * kKeys > w.len;
                 }
                 return true;
@@ -799,6 +804,9 @@ attend_forward(const __grid_constant__ Maps<NP> tm, const __grid_constant__ FwdA
             // result's sum in tensor memory is scaled anew only where that has grown by more than 2^8, a factor
             // that neither w nor the sums mind
             float m = -INFINITY, l = 0.0f, alpha = 1.0f;  // w = 2^(c z - base2), base2 = c m as rounded
+            float kept2 = 0.0f;  // base2 of the sums in memory
+            const size_t row = (size_t)w.b * g.q_b + (size_t)t * g.q_t + head;
+            auto kept = [&](int d) { return (float4 *)(g.sums + (w.sp * g.rows + row) * g.Dp + d); };  // four of them
             auto add_o = [&]() {  // o = o alpha + the last tile's w v
                 const float2 al = make_float2(alpha, alpha);
 #pragma unroll
@@ -811,6 +819,21 @@ attend_forward(const __grid_constant__ Maps<NP> tm, const __grid_constant__ FwdA
                         for (int j = 0; j < 8; ++j)
                             o[i / 2 + j] = __ffma2_rn(o[i / 2 + j], al, make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])));
                     }
+                }
+            };
+            // the sum in tensor memory, times `by`, to the one in memory (first: it is the first), times `old`
+            auto keep_sum = [&](float by, float old, bool first) {
+#pragma unroll 1
+                for (int i = 0; i < g.Dp; i += 8) {
+                    float v[8];
+                    tc::tmem_ld8(at + Sh::kColO + i, v);
+                    if (here)
+#pragma unroll
+                        for (int j = 0; j < 8; j += 4) {
+                            const float4 x = first ? make_float4(0, 0, 0, 0) : *kept(i + j);
+                            *kept(i + j) = make_float4(fmaf(v[j], by, x.x * old), fmaf(v[j + 1], by, x.y * old), fmaf(v[j + 2], by, x.z * old),
+                                                       fmaf(v[j + 3], by, x.w * old));
+                        }
                 }
             };
             auto scale_o = [&](float by) {  // the sum in tensor memory
@@ -891,7 +914,12 @@ attend_forward(const __grid_constant__ Maps<NP> tm, const __grid_constant__ FwdA
                 if (i >= kBack && !summed(mi - kBack)) return false;
                 if (busy) {
                     if constexpr (Sh::kSums) {
-                        if (__any_sync(0xffffffffu, i > 0 && now != 1.0f)) {
+                        if (i > 0 && i % Sh::kRun == 0) {
+                            if (!summed(mi - 1)) return false;
+                            const bool first = i == Sh::kRun;
+                            keep_sum(now, first ? 0.0f : exp2_hw(kept2 - base2), first);
+                            kept2 = base2;
+                        } else if (__any_sync(0xffffffffu, i > 0 && now != 1.0f)) {
                             if (!summed(mi - 1)) return false;
                             scale_o(now);
                         }
@@ -954,7 +982,6 @@ attend_forward(const __grid_constant__ Maps<NP> tm, const __grid_constant__ FwdA
             // l is against base2, not c m: an lse that left the difference out was 8e-7 off (2221 states), with it 3e-7
             const float off = m == -INFINITY ? 0.0f : fmaf(m, c, -__fmul_rn(m, c));
             const float lse = some ? (l == INFINITY ? l : fmaf(m, g.scale, fmaf(-kLn2, off, logf(l)))) : -INFINITY;
-            const size_t row = (size_t)w.b * g.q_b + (size_t)t * g.q_t + head;
             const bool pieces = g.D % 8 == 0;
             // CD of the outputs' columns, from d0 on
             auto put = [&](auto &v, int d0) __attribute__((always_inline)) {
@@ -974,6 +1001,16 @@ attend_forward(const __grid_constant__ Maps<NP> tm, const __grid_constant__ FwdA
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] = make_float2(0.0f, 0.0f);
                     if (n > 0 && busy) add_columns<64, 32>(at + Sh::kColO + d0, g.D - d0, v);
+                    if (n > Sh::kRun && here) {
+                        const float old = exp2_hw(kept2 - (m == -INFINITY ? 0.0f : __fmul_rn(m, c)));
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2)
+                            if (d0 + 2 * i < g.Dp) {
+                                const float4 x = *kept(d0 + 2 * i);
+                                v[i] = __ffma2_rn(make_float2(x.x, x.y), make_float2(old, old), v[i]);
+                                v[i + 1] = __ffma2_rn(make_float2(x.z, x.w), make_float2(old, old), v[i + 1]);
+                            }
+                    }
                     put(v, d0);
                 }
             } else {
@@ -2029,8 +2066,12 @@ cudaError_t launch_forward(stacklstm_op *op, const Call &c, const Operand (&o)[3
         e = op_workspace(op, kWsPart, (size_t)g.split * g.rows * g.Dp * 4);
         if (!e) e = op_workspace(op, kWsPartLse, (size_t)g.split * g.rows * 4);
         if (e) return e;
-        g.part = (float *)op->ws[kWsPart];
+        g.part = g.sums = (float *)op->ws[kWsPart];
         g.part_lse = (float *)op->ws[kWsPartLse];
+    }
+    if (Sh::kSums && g.split == 1 && g.per > Sh::kRun) {
+        if ((e = op_workspace(op, kWsPart, g.rows * g.Dp * 4))) return e;
+        g.sums = (float *)op->ws[kWsPart];
     }
     g.items = (int)(ctas * g.split);
     g.sorted = few_each(g.items, room, g.B, g.kv_len);

@@ -52,3 +52,65 @@ def test_a_bf16_result_alone_keeps_its_weights(B, T, S, nh, nk, D):
     tol = (2 * rel.transpose(2, 0, 1)[..., None] + 2.0 ** -15 + 8 * 2.0 ** -23 * (S / 64 + 1)) * wv
     _, y, _, _ = c.forward(c.handle(), False)
     within(c.back(y, nh), want, tol * (1 + 2.0 ** -7) + 2.0 ** -8 * np.abs(want), "y")
+
+
+def long_reference(q, k, v, kv_len, scale, nk):
+    """y of q [T, B, nk D] and the sum of magnitudes sum w |v| in fp64, some heads at a time, with the bound on a weight's error
+    (as in Case.check)."""
+    T, B, S, D = q.shape[0], q.shape[1], k.shape[0], k.shape[2] // nk
+    y, mag, rel = (torch.empty(T, B, nk, d, device="cuda", dtype=torch.float64) for d in (D, D, 1))
+    step = max(1, 2 ** 28 // (S * D))
+    for b in range(B):
+        n = S if kv_len is None else int(kv_len[b])
+        for h in range(0, nk, step):
+            cut = lambda x, n: x[:n, b].view(n, nk, D)[:, h:h + step].double()
+            qq, kk, vv = cut(q, T), cut(k, n), cut(v, n)
+            w = torch.softmax(scale * torch.einsum("tnd,snd->nts", qq, kk), -1)
+            zmag = scale * torch.einsum("tnd,snd->nts", qq.abs(), kk.abs()).amax(2)
+            y[:, b, h:h + step] = torch.einsum("nts,snd->tnd", w, vv)
+            mag[:, b, h:h + step] = torch.einsum("nts,snd->tnd", w, vv.abs())
+            rel[:, b, h:h + step, 0] = (2 * (2 * U * (D + 8) + 4 * U) * zmag + 4 * U * 4096 + 2.0 ** -20).t()
+    return y, mag, rel
+
+
+@pytest.mark.parametrize("B,T,S,nk,D,ragged", [(1, 1, 9000, 320, 16, False), (2, 2, 8300, 160, 24, True), (1, 3, 5000, 320, 72, False),
+                                               (1, 2, 300000, 2, 24, False), (3, 130, 4200, 110, 8, True)])
+def test_memories_of_several_sums(B, T, S, nk, D, ragged):
+    """More than 4096 states to an item, in several sums that are joined in fp32: scores that grow along the states, so that
+    each sum has a base of its own; whole and broken ends; a few long sentences, split as well. Cuts of 8 additions a tile
+    and 64 tiles at most, weights in two parts, and an fp32 sum (4 u a term) of the runs."""
+    g = torch.Generator(device="cuda").manual_seed(S)
+    r = lambda n: torch.randn(n, B, nk * D, device="cuda", generator=g)
+    grow = torch.linspace(0, 20, S, device="cuda")[:, None, None]
+    q, k, v = r(T).abs().bfloat16(), (0.5 * r(S) + grow / D ** 0.5).bfloat16(), r(S).bfloat16()
+    kv_len = torch.tensor([S, 4097, 64][:B], dtype=torch.int32, device="cuda") if ragged else None
+    op = bd.stacklstm_attend_create(T, S, B, nk, nk, D, BF)
+    y = empty(*q.shape, dtype=torch.bfloat16)
+    scale = float(np.float32(D ** -0.5))
+    bd.stacklstm_attend_forward(op, q, k, v, None, kv_len, scale, y)
+    bd.stacklstm_op_status(op)
+    want, mag, rel = long_reference(q, k, v, kv_len, scale, nk)
+    tol = (2 * rel + 2.0 ** -15 + 512 * 2.0 ** -23 + 8 * U * (S / 4096 + 33)) * mag
+    within(y.view_as(want), want.cpu().numpy(), (tol * (1 + 2.0 ** -7) + 2.0 ** -8 * want.abs()).cpu().numpy(), "y")
+
+
+def test_the_longest_memory():
+    """2^20 states of values of one sign, not split (320 heads): no bias from additions that cut. Of a result's mean relative error
+    rounding to bf16 leaves 2^-8 / sqrt(3 n) of n results whose sizes spread over an octave (four of those), the cuts of one sum of
+    4096 states 2^-14 at most."""
+    S, nk, D = 1 << 20, 320, 8
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q = torch.randn(1, 1, nk * D, device="cuda", generator=g).bfloat16()
+    k = torch.randn(S, 1, nk * D, device="cuda", generator=g, dtype=torch.bfloat16)
+    v = torch.rand(S, 1, nk * D, device="cuda", generator=g, dtype=torch.bfloat16)
+    v += 1
+    v *= torch.exp2(torch.rand(nk * D, device="cuda", generator=g)).bfloat16()
+    op = bd.stacklstm_attend_create(1, S, 1, nk, nk, D, BF)
+    y = empty(1, 1, nk * D, dtype=torch.bfloat16)
+    bd.stacklstm_attend_forward(op, q, k, v, None, None, D ** -0.5, y)
+    bd.stacklstm_op_status(op)
+    want, mag, rel = long_reference(q, k, v, None, D ** -0.5, nk)
+    off = y.view_as(want).double() / want - 1
+    assert abs(float(off.mean())) <= 2.0 ** -14 + 4 * 2.0 ** -8 / (3 * nk * D) ** 0.5
+    tol = 2 * rel + 2.0 ** -15 + 2.0 ** -14 + 8 * U * 289
+    assert bool((off.abs() <= tol * (1 + 2.0 ** -7) + 2.0 ** -8).all())
