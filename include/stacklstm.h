@@ -558,9 +558,9 @@ sl_status stacklstm_attend_backward(stacklstm_op_t op, int T, int S, const float
  *   G = dlogp (0 without a target) + sum of dtop_j over the classes there are;
  *   dlogits [rows, V] float, overwritten; logits, target, entropy, lse, top_idx as the forward has them
  *   (target needed with dlogp, entropy with dentropy, top_idx with dtop). A class listed twice counts twice.
- *   A row of -inf alone has gradient 0.
+ *   A row of -inf alone has gradient 0. The p_v are divided by their own sum: lse's rounding, 2^-25 of it, does not enter.
  * k <= 64 (0: no alternatives). An index outside its range is skipped and reported (SL_ERR_ARG).
- * Workspace: few rows (at most four times the SMs) are over several CTAs each, 16 + 8 k bytes a row and CTA.
+ * Workspace: few rows (at most four times the SMs) are over several CTAs each, 16 + 8 k bytes a row and CTA, 4 in the backward.
  */
 sl_status stacklstm_logprob_create(stacklstm_op_t *out, int R, int V, int k, sl_dtype dtype, int device, void *stream);
 sl_status stacklstm_logprob_forward(stacklstm_op_t op, int rows, const void *logits, const int32_t *target, float *logp,

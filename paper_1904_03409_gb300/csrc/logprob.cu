@@ -6,6 +6,9 @@
 // (x and e x are exact where a class is the best; z sum-by-sum would cancel). For gradients g of the target's
 // lp, g_j of alternative i_j's and h of H, with G = g + sum g_j,
 //   dz_v = g [v = target] + sum_j g_j [v = i_j] - p_v (G + h (lp_v + H)).
+// lse as a float is off by half a step, 2^-25 of it, and p = exp(z - lse) by a factor that the whole row shares: 1.4e-5 for
+// logits shifted by 300, and V for a row of V times -1e9. So the backward takes lse only for a first base and makes
+// f = sum_v exp(z_v - lse) itself: p_v = exp(z_v - lse - ln f). (lse is at most 21 off, the logarithm of the most classes.)
 // Bound by HBM: a row is read once, and by the backward once more, which writes 4 bytes a class.
 #include "select.cuh"
 
@@ -355,7 +358,10 @@ struct GradArgs {
     const float *entropy, *lse, *dlogp, *dentropy, *dtop;
     float *dz;
     int32_t *err;
+    // rows over several CTAs:
     int split;                 // CTAs a row
+    int sums;                  // parts of a row whose sums of exponentials are in
+    float *part;               //  [rows][sums]
 };
 
 // The row's classes that have a gradient of their own: the target and the alternatives (c: class or -1).
@@ -380,87 +386,198 @@ __device__ __forceinline__ void read_entry(const GradArgs &a, size_t r, int j, i
 }
 
 struct Grad {
-    float lse, all, h;  // all = G + h H
+    float lse, rest, all, h;  // lp = z - lse - rest; all = G + h H
     bool none;
+    // (the entries read, f of the row known)
+    __device__ __forceinline__ Grad(const GradArgs &a, size_t r, const float *w, float lse_, float f) : lse(lse_), rest(logf(f))
+    {
+        none = lse == -INFINITY;
+        h = a.dentropy ? a.dentropy[r] : 0.0f;
+        all = 0.0f;
+        for (int j = 0; j <= a.k; ++j) all += w[j];
+        if (a.dentropy) all = fmaf(h, a.entropy[r], all);
+    }
     __device__ __forceinline__ float operator()(float z) const
     {
-        const float lp = z - lse, p = exp2_hw(lp * kLog2e);
+        const float lp = (z - lse) - rest, p = exp2_hw(lp * kLog2e);
         return none ? 0.0f : -p * fmaf(h, fmaxf(lp, -1e4f), all);  // (p is 0 below -104: no inf x 0)
     }
 };
-
-// TPR lanes (8, 32) to a row, several rows a CTA, or a CTA of 256 threads to a range of a row's pieces. The
-// few classes of the entries are written once more after the CTA's pieces: the first entry of each class
-// takes the sum of the class's weights in entry order, so repeated classes need no atomics.
-// Bound by HBM: 4096 x 32003 bf16 157 us, 5.0 TB/s (6 bytes a class).
-template <typename T, int TPR>
-__global__ void __launch_bounds__(256)
-logprob_grad(const __grid_constant__ GradArgs a)
+// A piece's share of f (what is outside the row is -inf, and counts 0).
+template <typename T>
+__device__ __forceinline__ float piece_sum(const uint4 &q, float lse)
 {
-    constexpr int E = RowVec<T>::E, RPC = TPR <= 32 ? 256 / TPR : 1, U = 4;
-    extern __shared__ __align__(16) uint8_t dyn[];
-    after_previous();
-    const int k1 = a.k + 1, sub = TPR <= 32 ? threadIdx.x / TPR : 0, t = threadIdx.x % TPR;
-    int *c = (int *)dyn + sub * k1;
-    float *w = (float *)(dyn + (size_t)RPC * k1 * 4) + sub * k1;
-    const size_t r = TPR <= 32 ? (size_t)blockIdx.x * RPC + sub : blockIdx.x / a.split;
-    const int part = TPR <= 32 ? 0 : (int)(blockIdx.x % a.split);
-    const bool here = r < (size_t)a.rows;
+    float v[RowVec<T>::E], s = 0.0f;
+    unpack<T>(q, v);
+#pragma unroll
+    for (int i = 0; i < RowVec<T>::E; ++i) s += exp2_hw((v[i] - lse) * kLog2e);
+    return s;
+}
+// Pieces p_lo .. n of a row are written: the few classes of the entries among them are once more. The first entry of each
+// class takes the sum of the class's weights in entry order, so repeated classes need no atomics.
+template <typename T, int TPR>
+__device__ __forceinline__ void put_entries(const GradArgs &a, const Grad &g, const RowVec<T> &row, int p_lo, int n, const int *c, const float *w, int t)
+{
     const T *z = (const T *)a.z;
-    const RowVec<T> row(r, a.V);
-    const int pieces = here ? row.pieces() : 0;
-    const int p_lo = (int)((long long)pieces * part / a.split), n = (int)((long long)pieces * (part + 1) / a.split);
-    // the first pieces are on their way while the entries are read
-    uint4 q[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-        if (p_lo + u * TPR + t < n) q[u] = row.load(z, p_lo + u * TPR + t);
-    if (here)
-        for (int j = t; j < k1; j += TPR) read_entry(a, r, j, c, w);
-    if constexpr (TPR <= 32)
-        __syncwarp();
-    else
-        __syncthreads();
-    if (!here) return;
-    Grad g;
-    g.lse = a.lse[r];
-    g.none = g.lse == -INFINITY;
-    g.h = a.dentropy ? a.dentropy[r] : 0.0f;
-    g.all = 0.0f;
-    for (int j = 0; j < k1; ++j) g.all += w[j];
-    if (a.dentropy) g.all = fmaf(g.h, a.entropy[r], g.all);
-    const bool aligned = on_32(a.dz);
-    for (int p = p_lo + t; p < n; p += U * TPR) {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (p + u * TPR < n) {
-                float v[E], d[E];
-                unpack<T>(q[u], v);
-#pragma unroll
-                for (int i = 0; i < E; ++i) d[i] = g(v[i]);
-                row.store_f32(a.dz, aligned, p + u * TPR, d);
-            }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (p + (U + u) * TPR < n) q[u] = row.load(z, p + (U + u) * TPR);
-    }
-    if constexpr (TPR <= 32)
-        __syncwarp(TPR == 32 ? 0xffffffffu : 0xffu << (threadIdx.x & 24));
-    else
-        __syncthreads();
     const int c_lo = row.column(p_lo), c_hi = row.column(n);
-    for (int j = t; j < k1; j += TPR) {
+    for (int j = t; j <= a.k; j += TPR) {
         const int v = c[j];
         if (v < c_lo || v >= c_hi || v < 0 || g.none) continue;
         bool first = true;
         float sum = w[j];
-        for (int i = 0; i < k1; ++i)
+        for (int i = 0; i <= a.k; ++i)
             if (c[i] == v) {
                 if (i < j) first = false;
                 if (i > j) sum += w[i];
             }
         if (first) a.dz[row.first() + v] = g(to_f32(z[row.first() + v])) + sum;
     }
+}
+
+// A row's pieces read once for f and for the gradient, NP a thread in registers: TPR lanes (8, 32) to a row, several rows a CTA,
+// or a CTA of TPR threads; what 1024 threads do not hold they read again, in part from L2.
+// Bound by HBM: 4096 x 32003 bf16 133 us, 5.9 TB/s (6 bytes a class). (A row over a cluster of CTAs, 2000 x 70001: 222 us, 169 so.)
+template <typename T, int TPR, int NP>
+__global__ void __launch_bounds__(row_cta(TPR), TPR <= 32 ? 1 : row_ctas_per_sm(TPR))
+logprob_grad(const __grid_constant__ GradArgs a)
+{
+    constexpr int RPC = rows_per_cta(TPR);
+    __shared__ float sm[TPR <= 32 ? 1 : TPR / 32];
+    extern __shared__ __align__(16) uint8_t dyn[];
+    after_previous();
+    const int k1 = a.k + 1, sub = TPR <= 32 ? threadIdx.x / TPR : 0, t = threadIdx.x % TPR;
+    int *c = (int *)dyn + sub * k1;
+    float *w = (float *)(dyn + (size_t)RPC * k1 * 4) + sub * k1;
+    const size_t r = (size_t)blockIdx.x * RPC + sub;
+    const bool here = r < (size_t)a.rows;  // (lanes of a row past the end stay for the joins)
+    const T *z = (const T *)a.z;
+    const RowVec<T> row(r, a.V);
+    const int n = here ? row.pieces() : 0;
+    // the pieces are on their way while the entries are read
+    uint4 q[NP];
+#pragma unroll
+    for (int u = 0; u < NP; ++u)
+        if (u * TPR + t < n) q[u] = row.load(z, u * TPR + t);
+    if (here)
+        for (int j = t; j < k1; j += TPR) read_entry(a, r, j, c, w);
+    const float lse = here ? a.lse[r] : 0.0f;
+    float f[1] = {0.0f};
+#pragma unroll
+    for (int u = 0; u < NP; ++u)
+        if (u * TPR + t < n) f[0] += piece_sum<T>(q[u], lse);
+    constexpr int U = 4;  // of a longer row's pieces at a time
+    if constexpr (TPR == 1024)
+        for (int p = NP * TPR + t; p < n; p += U * TPR) {
+            uint4 x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (p + u * TPR < n) x[u] = row.load(z, p + u * TPR);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (p + u * TPR < n) f[0] += piece_sum<T>(x[u], lse);
+        }
+    row_join<false, TPR>(f, sm);  // (and the entries are written, of a row over a CTA)
+    if constexpr (TPR <= 32) __syncwarp();
+    if (!here) return;
+    const Grad g(a, r, w, lse, f[0]);
+    const bool aligned = on_32(a.dz);
+    auto put = [&](const uint4 &x, int p) {
+        float v[RowVec<T>::E];
+        unpack<T>(x, v);
+#pragma unroll
+        for (int i = 0; i < RowVec<T>::E; ++i) v[i] = g(v[i]);
+        row.store_f32(a.dz, aligned, p, v);
+    };
+#pragma unroll
+    for (int u = 0; u < NP; ++u)
+        if (u * TPR + t < n) put(q[u], u * TPR + t);
+    if constexpr (TPR == 1024)
+        for (int p = NP * TPR + t; p < n; p += U * TPR) {
+            uint4 x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (p + u * TPR < n) x[u] = row.load(z, p + u * TPR);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (p + u * TPR < n) put(x[u], p + u * TPR);
+        }
+    if constexpr (TPR <= 32)
+        __syncwarp(TPR == 32 ? 0xffffffffu : 0xffu << (threadIdx.x & 24));
+    else
+        __syncthreads();
+    put_entries<T, TPR>(a, g, row, 0, n, c, w, t);
+}
+
+// Long rows, too few to fill the GPU with a CTA each: f in parts first, a CTA of 256 threads each, ... (8 x 32003 bf16 both
+// launches as long as 100 rows of a CTA each.)
+template <typename T>
+__global__ void __launch_bounds__(256)
+logprob_sum(const __grid_constant__ GradArgs a)
+{
+    constexpr int U = 4;
+    __shared__ float sm[8];
+    after_previous();
+    const size_t r = blockIdx.x / a.sums;
+    const int part = (int)(blockIdx.x % a.sums), t = threadIdx.x;
+    const RowVec<T> row(r, a.V);
+    const int pieces = row.pieces(), p_lo = (int)((long long)pieces * part / a.sums), n = (int)((long long)pieces * (part + 1) / a.sums);
+    const float lse = a.lse[r];
+    float f[1] = {0.0f};
+    for (int p = p_lo + t; p < n; p += U * 256) {
+        uint4 q[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (p + u * 256 < n) q[u] = row.load((const T *)a.z, p + u * 256);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (p + u * 256 < n) f[0] += piece_sum<T>(q[u], lse);
+    }
+    row_join<false, 256>(f, sm);
+    if (t == 0) a.part[r * a.sums + part] = f[0];
+}
+// ... and then the gradient, a CTA to a range of a row's pieces, which adds the parts up in their order.
+template <typename T>
+__global__ void __launch_bounds__(256)
+logprob_grad_range(const __grid_constant__ GradArgs a)
+{
+    constexpr int U = 4;
+    __shared__ float sm[8];
+    extern __shared__ __align__(16) uint8_t dyn[];
+    after_previous();
+    const int t = threadIdx.x;
+    int *c = (int *)dyn;
+    float *w = (float *)(dyn + (size_t)(a.k + 1) * 4);
+    const size_t r = blockIdx.x / a.split;
+    const int part = (int)(blockIdx.x % a.split);
+    const T *z = (const T *)a.z;
+    const RowVec<T> row(r, a.V);
+    const int pieces = row.pieces(), p_lo = (int)((long long)pieces * part / a.split), n = (int)((long long)pieces * (part + 1) / a.split);
+    uint4 q[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (p_lo + u * 256 + t < n) q[u] = row.load(z, p_lo + u * 256 + t);
+    for (int j = t; j <= a.k; j += 256) read_entry(a, r, j, c, w);
+    float f[1] = {0.0f};
+    for (int i = t; i < a.sums; i += 256) f[0] += a.part[r * a.sums + i];
+    row_join<false, 256>(f, sm);
+    const Grad g(a, r, w, a.lse[r], f[0]);
+    const bool aligned = on_32(a.dz);
+    for (int p = p_lo + t; p < n; p += U * 256) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (p + u * 256 < n) {
+                float v[RowVec<T>::E];
+                unpack<T>(q[u], v);
+#pragma unroll
+                for (int i = 0; i < RowVec<T>::E; ++i) v[i] = g(v[i]);
+                row.store_f32(a.dz, aligned, p + u * 256, v);
+            }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (p + (U + u) * 256 < n) q[u] = row.load(z, p + (U + u) * 256);
+    }
+    __syncthreads();
+    put_entries<T, 256>(a, g, row, p_lo, n, c, w, t);
 }
 
 template <typename T>
@@ -507,20 +624,27 @@ cudaError_t launch_logprob(stacklstm_op *op, LogpArgs &a)
 }
 
 template <typename T>
-cudaError_t launch_grad(const stacklstm_op *op, GradArgs &a)
+cudaError_t launch_grad(stacklstm_op *op, GradArgs &a)
 {
     int tpr, np;
     row_plan<T>(a.V, &tpr, &np);
-    a.split = 1;
-    if (tpr <= 32) {
-        const unsigned grid = ceil_div(a.rows, 256 / tpr);
-        const size_t smem = (size_t)(256 / tpr) * (a.k + 1) * 8;
-        return tpr == 8 ? launch_after(logprob_grad<T, 8>, grid, 256, smem, op->stream, a)
-                        : launch_after(logprob_grad<T, 32>, grid, 256, smem, op->stream, a);
+    if (tpr <= 32 || a.rows >= op->num_sms / 2) {
+        const size_t smem = (size_t)rows_per_cta(tpr) * (a.k + 1) * 8;
+        const dim3 grid(ceil_div(a.rows, rows_per_cta(tpr)));
+#define SL_GRAD(TPR, NP) \
+    if (tpr == TPR && np && np <= NP) return launch_after(logprob_grad<T, TPR, NP>, grid, row_cta(TPR), smem, op->stream, a);
+        SL_GRAD(8, 1) SL_GRAD(8, 2) SL_GRAD(8, 4) SL_GRAD(32, 2) SL_GRAD(32, 4) SL_GRAD(128, 2) SL_GRAD(128, 4) SL_GRAD(128, 8)
+        SL_GRAD(512, 4) SL_GRAD(512, 8)
+        return launch_after(logprob_grad<T, 1024, 8>, grid, 1024, smem, op->stream, a);
+#undef SL_GRAD
     }
     const size_t pieces = ((size_t)a.V + RowVec<T>::E - 1) / RowVec<T>::E + 1;
     a.split = (int)std::max<size_t>(1, std::min<size_t>(ceil_div(pieces, 1024), (1u << 30) / (size_t)a.rows));
-    return launch_after(logprob_grad<T, 256>, dim3((unsigned)((size_t)a.rows * a.split)), 256, (size_t)(a.k + 1) * 8, op->stream, a);
+    a.sums = std::min(a.split, 256);
+    if (cudaError_t e = op_workspace(op, 3, (size_t)a.rows * a.sums * 4)) return e;
+    a.part = (float *)op->ws[3];
+    if (cudaError_t e = launch_after(logprob_sum<T>, dim3((unsigned)((size_t)a.rows * a.sums)), 256, 0, op->stream, a)) return e;
+    return launch_after(logprob_grad_range<T>, dim3((unsigned)((size_t)a.rows * a.split)), 256, (size_t)(a.k + 1) * 8, op->stream, a);
 }
 
 }  // namespace

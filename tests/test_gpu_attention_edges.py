@@ -114,3 +114,48 @@ def test_the_longest_memory():
     assert abs(float(off.mean())) <= 2.0 ** -14 + 4 * 2.0 ** -8 / (3 * nk * D) ** 0.5
     tol = 2 * rel + 2.0 ** -15 + 2.0 ** -14 + 8 * U * 289
     assert bool((off.abs() <= tol * (1 + 2.0 ** -7) + 2.0 ** -8).all())
+
+
+@TYPES
+@pytest.mark.parametrize("R,V,k", [(5, 7, 2), (9, 83, 5), (40, 432, 3), (6, 2500, 4), (160, 2500, 4), (3, 32003, 2), (90, 32003, 2), (2, 70001, 3),
+                                   (40, 70001, 1), (2, 300007, 0)])
+@pytest.mark.parametrize("kind", [300, 3000, -1e5, "rows of -1e9", "rows of the lowest"])
+def test_the_logits_gradient_does_not_depend_on_a_shift(dt, R, V, k, kind):
+    """Logits far from 0, and finite rows masked throughout. Errors, relative to p times what it is multiplied by: the sum of
+    exponentials of up to 64 terms a thread and its joins, 96 u; exponents, by 8 u of them (of their mean in the sum) and
+    of ln f, which is what half a step of lse leaves, 21 at most; two exponentials, 2^-21 each; the weights' sum, 2 u a
+    term. Nothing grows with the logits."""
+    rng = np.random.default_rng(R + V)
+    z = 3 * rng.normal(size=(R, V)) + (kind if not isinstance(kind, str) else 0.0)
+    if isinstance(kind, str):
+        z[::2] = -1e9 if kind.endswith("9") else float(torch.finfo(tdt(dt)).min)
+    zd = torch.from_numpy(z).to(tdt(dt)).cuda()
+    z = zd.double().cpu().numpy()
+    target = rng.integers(-1, V, R).astype(np.int32)
+    op = bd.stacklstm_logprob_create(R, V, k, dt)
+    up = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    logp, ent, lse, idx, top = empty(R), empty(R), empty(R), empty(R, k, dtype=torch.int32), empty(R, k)
+    bd.stacklstm_logprob_forward(op, zd, up(target), logp, ent, lse, idx if k else None, top if k else None)
+    g, h, gt = (rng.normal(size=s).astype(np.float32) for s in (R, R, (R, k)))
+    x = z.max(1, keepdims=True) - z
+    e = np.exp(-x)
+    p = e / e.sum(1, keepdims=True)
+    mean = (p * np.minimum(x, 200)).sum(1, keepdims=True)
+    rest = np.minimum(21, U * np.abs(lse.double().cpu().numpy()))[:, None]
+    rel = U * (min(V, 64) + 32) + 2.0 ** -20 + 8 * U * (np.minimum(x, 200) + mean + rest + 4) + 2 * U * (k + 2)
+    _, we, _, wi, _ = at.logprob(z, target, k)
+    hits = np.zeros_like(z)
+    for r in range(R):
+        for c in [target[r], *wi[r]]:
+            if c >= 0:
+                hits[r, c] = np.abs(g[r]) + np.abs(gt[r]).sum()
+    d = empty(R, V)
+    for a in ((g, None, gt), (g, h, gt), (None, h, None)):
+        bd.stacklstm_logprob_backward(op, zd, up(target), ent, lse, idx if k else None, up(a[0]) if a[0] is not None else None,
+                                      up(a[1]) if a[1] is not None else None, up(gt) if k and a[2] is not None else None, d)
+        bd.stacklstm_op_status(op)
+        want = at.logprob_backward(z, target, wi, *a)
+        mag = sum(np.abs(v).reshape(R, -1).sum(1, keepdims=True) for v in (a[0], a[2]) if v is not None) if a[0] is not None else 0.0
+        if a[1] is not None:  # (the entropy, of its own sums, enters here as well)
+            mag = mag + np.abs(h)[:, None] * (x + np.abs(we)[:, None] + np.log(V) + 1)
+        within(d, want, p * np.where(p > 0, mag, 0) * 2 * rel + 2 * U * (k + 4) * hits + 1e-37, "dlogits")
