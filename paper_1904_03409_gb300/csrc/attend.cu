@@ -552,7 +552,8 @@ struct FwdArgs {
     float scale;
     void *y;
     float *lse, *ctx;
-    float *part, *part_lse;   // [split][rows][Dp] and [split][rows], or null
+    float *part;              // [split][rows][Dp], or null
+    float2 *part_stats;       // [split][rows]: the largest z, the sum of exponentials against it (0: no states)
     float *sums;              // [split][rows][Dp], part or a buffer by itself: a bf16 result's sums of the runs before
     int split, per;           // splits of the key tiles, key tiles of a split
     int tq, tiles, items;     // queries of a tile, tiles; all items
@@ -981,7 +982,6 @@ attend_forward(const __grid_constant__ Maps<NP> tm, const __grid_constant__ FwdA
             const float by = some ? 1.0f / l : 0.0f;
             // l is against base2, not c m: an lse that left the difference out was 8e-7 off (2221 states), with it 3e-7
             const float off = m == -INFINITY ? 0.0f : fmaf(m, c, -__fmul_rn(m, c));
-            const float lse = some ? (l == INFINITY ? l : fmaf(m, g.scale, fmaf(-kLn2, off, logf(l)))) : -INFINITY;
             const bool pieces = g.D % 8 == 0;
             // CD of the outputs' columns, from d0 on
             auto put = [&](auto &v, int d0) __attribute__((always_inline)) {
@@ -1016,8 +1016,12 @@ attend_forward(const __grid_constant__ Maps<NP> tm, const __grid_constant__ FwdA
             } else {
                 put(o, 0);
             }
-            float *const lses = g.part ? g.part_lse + w.sp * g.rows : g.lse;
-            if (lses && there) lses[row] = lse;
+            if (there) {
+                if (g.part)
+                    g.part_stats[w.sp * g.rows + row] = some ? make_float2(m, l * exp2f(-off)) : make_float2(-INFINITY, 0.0f);
+                else if (g.lse)
+                    g.lse[row] = some ? (l == INFINITY ? l : fmaf(m, g.scale, fmaf(-kLn2, off, logf(l)))) : -INFINITY;
+            }
             return true;
         });
         if (!ok && lane == 0) fail();
@@ -1028,7 +1032,8 @@ attend_forward(const __grid_constant__ Maps<NP> tm, const __grid_constant__ FwdA
     if (tid == 0) items_done(g.next);
 }
 
-// The splits' outputs of each query row joined: a warp a row, a lane a split's weight, then four columns.
+// The splits' outputs of each query row joined: a warp a row, a lane a split's weight, then four columns. A weight is made of
+// differences of z, as those of states are: of lses, rounded by 2^-25 of them, y was 1.2e-5 off where they are 3200.
 constexpr int kMostSplits = 32;
 template <typename T>
 __global__ void __launch_bounds__(256)
@@ -1038,12 +1043,12 @@ attend_join(const __grid_constant__ FwdArgs g)
     const size_t row = (size_t)blockIdx.x * 8 + threadIdx.x / 32;
     const int lane = threadIdx.x & 31, d = lane * 4;
     if (row >= g.rows) return;
-    const float e = lane < g.split ? g.part_lse[lane * g.rows + row] : -INFINITY;
-    float m = e;
+    const float2 e = lane < g.split ? g.part_stats[lane * g.rows + row] : make_float2(-INFINITY, 0.0f);
+    float m = e.x;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    const bool there = e != -INFINITY;  // (else the split had no states, and wrote nothing)
-    const float w = !there ? 0.0f : m == INFINITY ? NAN : expf(e - m);
+    const bool there = e.y != 0.0f;  // (else the split had no states, and wrote nothing)
+    const float w = there ? e.y * exp2f((e.x - m) * (g.scale * kLog2e)) : 0.0f;
     const float sum = warp_sum(w);
     const unsigned have = __ballot_sync(0xffffffffu, there);
     float v[4] = {};
@@ -1066,7 +1071,7 @@ attend_join(const __grid_constant__ FwdArgs g)
             ((T *)g.y)[row * g.D + d + j] = from_f32<T>(v[j] * by);
             if (g.ctx) g.ctx[row * g.D + d + j] = v[j] * by;
         }
-    if (lane == 0 && g.lse) g.lse[row] = have ? m + logf(sum) : -INFINITY;
+    if (lane == 0 && g.lse) g.lse[row] = have ? fmaf(m, g.scale, logf(sum)) : -INFINITY;
 }
 
 // ------------------------------------------------------------------ backward
@@ -1928,7 +1933,7 @@ attend_sum(const __grid_constant__ SumArgs a)
 }
 
 // ------------------------------------------------------------------ host side
-enum { kWsQ = 0, kWsK, kWsV, kWsDy, kWsDelta, kWsPart, kWsPartLse };  // workspace buffers
+enum { kWsQ = 0, kWsK, kWsV, kWsDy, kWsDelta, kWsPart, kWsPartStats };  // workspace buffers
 
 // q, k, v, y or dy: B sentences of n rows of `heads` heads; D elements a head, or in the workspace Dp.
 struct Rows {
@@ -2064,10 +2069,10 @@ cudaError_t launch_forward(stacklstm_op *op, const Call &c, const Operand (&o)[3
     g.split = (int)ceil_div(tiles, g.per);
     if (g.split > 1) {
         e = op_workspace(op, kWsPart, (size_t)g.split * g.rows * g.Dp * 4);
-        if (!e) e = op_workspace(op, kWsPartLse, (size_t)g.split * g.rows * 4);
+        if (!e) e = op_workspace(op, kWsPartStats, (size_t)g.split * g.rows * 8);
         if (e) return e;
         g.part = g.sums = (float *)op->ws[kWsPart];
-        g.part_lse = (float *)op->ws[kWsPartLse];
+        g.part_stats = (float2 *)op->ws[kWsPartStats];
     }
     if (Sh::kSums && g.split == 1 && g.per > Sh::kRun) {
         if ((e = op_workspace(op, kWsPart, g.rows * g.Dp * 4))) return e;

@@ -159,3 +159,30 @@ def test_the_logits_gradient_does_not_depend_on_a_shift(dt, R, V, k, kind):
         if a[1] is not None:  # (the entropy, of its own sums, enters here as well)
             mag = mag + np.abs(h)[:, None] * (x + np.abs(we)[:, None] + np.log(V) + 1)
         within(d, want, p * np.where(p > 0, mag, 0) * 2 * rel + 2 * U * (k + 4) * hits + 1e-37, "dlogits")
+
+
+@TYPES
+@pytest.mark.parametrize("offset", [0, 300, 3200, -3200])
+@pytest.mark.parametrize("B,T,S,nh,nk,D", [(2, 40, 1300, 2, 2, 64), (1, 2, 5000, 6, 2, 128), (3, 30, 90, 4, 4, 40)])
+def test_results_of_large_scores(dt, offset, B, T, S, nh, nk, D):
+    """Scores around `offset` that fp32 holds exactly (products of whole numbers of few bits), in splits and whole: y in fp32 as exact as
+    around 0. Of a weight, independent of one another: its exponent's rounding, at most 11 u in each of two operations, the
+    exponential 2^-21, its sum and the division 4 u, cut sums of 12 products of parts 12 x 1.7e-8, a split's weight the same
+    again: sqrt(2 (2 x 0.66^2 + 0.48^2 + 0.24^2) + 0.2^2) = 1.5e-6 at most. lse: by half a step and 2^-20."""
+    g = torch.Generator(device="cuda").manual_seed(S + D)
+    r = lambda n, h: torch.randint(-1, 2, (n, B, h, D), device="cuda", generator=g).float()
+    q, k, v = r(T, nh), r(S, nk), torch.randn(S, B, nk, D, device="cuda", generator=g)
+    q[..., 0], k[..., 0] = 25.0, offset / 6.25  # (of a quarter: `offset` itself)
+    q, k, v = (t.to(tdt(dt)).flatten(2) for t in (q, k, v))
+    kv_len = torch.tensor([S, S // 2, 70][:B], device="cuda").int()
+    h = lambda x: x.double().view(x.shape[0], B, nk, -1, D)
+    see = torch.arange(S, device="cuda")[None] < kv_len[:, None]
+    z = (0.25 * torch.einsum("tbngd,sbnxd->bngts", h(q), h(k))).masked_fill(~see.view(B, 1, 1, 1, S), -float("inf"))
+    want = torch.einsum("bngts,sbnxd->tbngd", torch.softmax(z, -1), h(v))
+    op = bd.stacklstm_attend_create(T, S, B, nh, nk, D, dt)
+    y, lse, ctx = empty(*q.shape, dtype=tdt(dt)), empty(T, B, nh), empty(*q.shape)
+    bd.stacklstm_attend_forward(op, q, k, v, None, kv_len, 0.25, y, lse, ctx)
+    bd.stacklstm_op_status(op)
+    assert float((ctx.double().view(want.shape) - want).norm()) <= 1.5e-6 * float(want.norm())
+    wl = torch.logsumexp(z, -1).permute(3, 0, 1, 2).reshape(T, B, nh)
+    assert bool(((lse.double() - wl).abs() <= U * wl.abs() + 2.0 ** -20).all())
