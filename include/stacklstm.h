@@ -525,12 +525,13 @@ sl_status stacklstm_beam_push(stacklstm_op_t op, const int8_t *ops, const void *
  *   y before its rounding, float (a backward of SL_BF16 needs it; else NULL). Queries behind q_len and
  *   of a sentence without states: y = 0, lse = -inf.
  * backward: dy float; q, k, v, lengths, scale as in the forward; lse its output; ctx its ctx (SL_FP32:
- *   its y); outputs (float, each nullable, overwritten) dq, dk, dv; 0 behind a sentence's end.
+ *   its y); outputs (float, each nullable, overwritten) dq, dk, dv; 0 behind a sentence's end. A row's weights
+ *   are divided by their own sum: lse's rounding, 2^-25 of it, does not enter (dk and dv alone take as long as with dq).
  * SL_BF16 without ctx takes the weights exp(z - largest z) as two bf16 parts (2^-15 of them at most is left
  * out, before y is rounded by up to 2^-8); with ctx, and in every gradient, weights and dy enter as three: fp32
  * accuracy. A length outside its range counts as the nearest one and is reported
  * (SL_ERR_ARG). Workspace: q, k, v as parts (6 bytes an element of SL_FP32; 2 of SL_BF16 with D not a
- * multiple of 8), dy as parts (6) and 4 bytes a query and head; where there are few sentences, heads and
+ * multiple of 8), dy as parts (6) and 8 bytes a query and head; where there are few sentences, heads and
  * tiles the sums of splits: 4 bytes an element of y, of dk and dv, or of dq, and split (32 at most); 4 bytes an
  * element of a bf16 y without ctx over more than 4096 states.
  */

@@ -7,7 +7,7 @@
 //   dv_s = sum_t w_ts dy_t,   dz_ts = w_ts (dy_t . v_s - dy_t . y_t),   dq_t = c sum_s dz_ts k_s,   dk_s = c sum_t dz_ts q_t.
 // Neither z nor w is ever in memory: the forward goes over the states in tiles of 64 and keeps, for
 // each query, the largest z so far, the sum of exponentials and the weighted sum of v against it; the
-// backward makes w again from lse.
+// backward makes w again from lse, and from f_t = sum_s exp(z_ts - lse_t), 1 but for what lse's rounding lost.
 //
 // All products run on the tensor cores (tcgen05, bf16 operands, fp32 accumulators in tensor memory).
 // A bf16 tensor is one operand; an fp32 number is the sum of three bf16 parts (8 + 8 + 8 significant
@@ -1091,6 +1091,9 @@ struct BwdArgs {
     const int32_t *q_len, *kv_len;
     float scale;
     const float *lse, *delta;
+    float *norm;              // [B][heads][T] log2 f: made with dq, read for dk and dv
+    float *part_norm;         // [split][B][heads][T] f of splits
+    size_t rows;              // B T heads
     float *dq, *dk, *dv;
     int tq, tiles;            // queries of a tile, tiles of queries (dq) or of states (dk, dv)
     int split, per;           // splits of the other's tiles, tiles of a split: each has sums of its own
@@ -1104,7 +1107,9 @@ struct BwdArgs {
 
 // w = exp(scale z - lse) as 2^(c (z - pivot) - rest), c = scale log2 e: where w counts z is near the pivot, so that
 // the rounding of the product and of c is that of a small number. (Of c z - lse log2 e it is that of lse, 12 for 2221
-// states, for all of a row's w: gradients 1.5e-6 off 64 bits, 6e-7 so.)
+// states, for all of a row's w: gradients 1.5e-6 off 64 bits, 6e-7 so.) lse itself is off by half a step, 2^-25 of it, and
+// with it all w of a row by one factor, 1.5e-5 where lse is 300: the kernel that makes dq sums a row's w, divides dq by
+// that sum f, and leaves log2 f for the kernel that makes dk and dv, whose rest it is added to.
 struct RowBase {
     float pivot, rest;
 };
@@ -1117,6 +1122,9 @@ __device__ __forceinline__ RowBase row_base(float lse, float scale)
     }
     return {p, fmaf(-p, scale, lse) * kLog2e};
 }
+
+// Where a row's f lies: a warp's rows are next to one another (as they lie in lse stores cost 14 us of 256 x 256 x 256).
+__device__ __forceinline__ size_t norm_at(const BwdArgs &g, int b, int head, int t) { return ((size_t)b * (g.nk * g.G) + head) * g.T + t; }
 
 // Columns of part p of the 16 fp32 numbers c of a lane (of 64 numbers) as an operand in tensor memory, made in the
 // place of the numbers (64 columns and 32 more): the first two parts lie in the 16 numbers' own columns.
@@ -1407,6 +1415,7 @@ attend_grad_states(const __grid_constant__ BwdMaps<NP> tm, const __grid_constant
                 if (r < g.tq * g.G && t < w.q_len) {
                     const size_t row = (size_t)w.b * g.q_b + (size_t)t * g.q_t + w.kvh * g.G + r % g.G;
                     from = row_base(g.lse[row], g.scale);
+                    from.rest += g.norm[norm_at(g, w.b, w.kvh * g.G + r % g.G, t)];
                     delta = g.delta[row];
                 }
                 // (the place's statistics of NS tiles ago were read before its gradients were made)
@@ -1830,7 +1839,7 @@ attend_grad_queries(const __grid_constant__ BwdMaps<NP> tm, const __grid_constan
             const RowBase from = here ? row_base(g.lse[row], g.scale) : RowBase{0.0f, 0.0f};
             const float2 pivot = make_float2(-from.pivot, -from.pivot), rest = make_float2(-from.rest, -from.rest);
             const float delta = here ? g.delta[row] : 0.0f;
-            float2 acc[DP / 2];
+            float2 acc[DP / 2], f2 = make_float2(0.0f, 0.0f);
 #pragma unroll
             for (int i = 0; i < DP / 2; ++i) acc[i] = make_float2(0.0f, 0.0f);
 #pragma unroll 1
@@ -1864,14 +1873,23 @@ attend_grad_queries(const __grid_constant__ BwdMaps<NP> tm, const __grid_constan
                         read16(at + Sh::kColD + 16 * h, dz);
 #pragma unroll
                         for (int j = 0; j < 8; ++j) dz[j] = __fmul2_rn(wv[h / 2][h % 2 * 8 + j], __fadd2_rn(dz[j], make_float2(-delta, -delta)));
-                        if (left < kKeys || len == 1) {
-                            // (one state has weight 1 whatever z is: dz is 0, not what rounding leaves of it)
+                        float2 *const w = &wv[h / 2][h % 2 * 8];
+                        if (left < kKeys) {
 #pragma unroll
                             for (int j = 0; j < 8; ++j) {
-                                if (16 * h + 2 * j >= left || len == 1) dz[j].x = 0.0f;
-                                if (16 * h + 2 * j + 1 >= left || len == 1) dz[j].y = 0.0f;
+                                if (16 * h + 2 * j >= left) dz[j].x = w[j].x = 0.0f;
+                                if (16 * h + 2 * j + 1 >= left) dz[j].y = w[j].y = 0.0f;
                             }
+                            // (one state has weight 1 whatever z is: dz is 0, not what rounding leaves of it)
+                            if (h == 0 && len == 1) dz[0].x = 0.0f;
                         }
+                        float2 s2 = __fadd2_rn(w[0], w[1]), u2 = __fadd2_rn(w[2], w[3]);
+#pragma unroll
+                        for (int j = 4; j < 8; j += 2) {
+                            s2 = __fadd2_rn(s2, w[j]);
+                            u2 = __fadd2_rn(u2, w[j + 1]);
+                        }
+                        f2 = __fadd2_rn(f2, __fadd2_rn(s2, u2));
                         put_parts16(at + Sh::kColD, h, dz);
                     }
                     tmem_wait_st();
@@ -1885,7 +1903,15 @@ attend_grad_queries(const __grid_constant__ BwdMaps<NP> tm, const __grid_constan
                 if (busy) add_columns<DP, (DP == 64 ? 32 : 16)>(at + Sh::kColQ, g.D, acc);
             }
             if (n == 0 && g.split > 1) return true;  // (the sum knows which splits have none)
-            if (__any_sync(0xffffffffu, there)) put_rows<float, DP>(stage, there ? g.dq + w.sp * g.plane + row * g.D : nullptr, acc, g.D, g.scale, !here || n == 0, g.D % 8 == 0);
+            const float f = f2.x + f2.y;
+            if (here && n > 0) {
+                if (g.split > 1)
+                    g.part_norm[w.sp * g.rows + norm_at(g, w.b, head, t)] = f;
+                else
+                    g.norm[norm_at(g, w.b, head, t)] = log2f(f);
+            }
+            if (g.dq && __any_sync(0xffffffffu, there))
+                put_rows<float, DP>(stage, there ? g.dq + w.sp * g.plane + row * g.D : nullptr, acc, g.D, g.split > 1 ? g.scale : g.scale / f, !here || n == 0, g.D % 8 == 0);
             return true;
         });
         if (!ok && lane == 0) fail();
@@ -1901,6 +1927,8 @@ attend_grad_queries(const __grid_constant__ BwdMaps<NP> tm, const __grid_constan
 struct SumArgs {
     const float *part[2];
     float *out[2];           // (each may be null)
+    const float *part_norm;  // of dq's rows f of each split, or null
+    float *norm;             //  and log2 f
     size_t plane, rows;
     int n, B, heads, D, r_t, r_b;        // the rows' tensor
     const int32_t *len, *other_len;      // of the rows, and of what they were split over
@@ -1919,6 +1947,14 @@ attend_sum(const __grid_constant__ SumArgs a)
     const int t = a.n == 1 ? 0 : by_time || a.B == 1 ? (int)(line / a.B) : (int)(line % a.n);
     const int len = a.len ? min(max(a.len[b], 0), a.n) : a.n, other = a.other_len ? min(max(a.other_len[b], 0), a.other) : a.other;
     const int tiles = (other + a.tile - 1) / a.tile, n = t < len ? min(a.split, (tiles + a.per - 1) / a.per) : 0;
+    float by = 1.0f;
+    if (a.part_norm && n > 0) {
+        const size_t at = ((size_t)b * a.heads + row % a.heads) * a.n + t;
+        float f = 0.0f;
+        for (int i = 0; i < n; ++i) f += a.part_norm[i * a.rows + at];
+        by = 1.0f / f;
+        if (lane == 0) a.norm[at] = log2f(f);
+    }
 #pragma unroll
     for (int o = 0; o < 2; ++o) {
         if (!a.out[o]) continue;
@@ -1927,13 +1963,13 @@ attend_sum(const __grid_constant__ SumArgs a)
             float v = 0.0f;
 #pragma unroll 4
             for (int i = 0; i < n; ++i) v += p[i * a.plane];
-            a.out[o][row * a.D + d] = v;
+            a.out[o][row * a.D + d] = v * by;
         }
     }
 }
 
 // ------------------------------------------------------------------ host side
-enum { kWsQ = 0, kWsK, kWsV, kWsDy, kWsDelta, kWsPart, kWsPartStats };  // workspace buffers
+enum { kWsQ = 0, kWsK, kWsV, kWsDy, kWsDelta, kWsPart, kWsPartStats, kWsNorm };  // workspace buffers
 
 // q, k, v, y or dy: B sentences of n rows of `heads` heads; D elements a head, or in the workspace Dp.
 struct Rows {
@@ -2106,13 +2142,32 @@ cudaError_t launch_backward(stacklstm_op *op, const Call &c, const Operand (&o)[
         g.split = (int)ceil_div(tiles, g.per);
         g.items = (int)(items * g.split);
     };
-    auto sum = [&](const Rows &r, const int32_t *len, const int32_t *other_len, int other, int tile, const float *p0, const float *p1, float *o0, float *o1) {
+    auto sum = [&](const Rows &r, const int32_t *len, const int32_t *other_len, int other, int tile, const float *p0, const float *p1, float *o0, float *o1,
+                   const float *part_norm) {
         const size_t rows = (size_t)r.n * r.B * r.heads;
-        const SumArgs a = {{p0, p1}, {o0, o1}, g.plane, rows, r.n, r.B, r.heads, r.D, r.t(), r.b(), len, other_len, other, tile, g.per, g.split};
+        const SumArgs a = {{p0, p1}, {o0, o1}, part_norm, g.norm, g.plane, rows, r.n, r.B, r.heads, r.D, r.t(), r.b(), len, other_len, other, tile, g.per, g.split};
         return launch_after(attend_sum, dim3(ceil_div(rows, 8)), 256, 0, op->stream, a);
     };
     float *const dq = g.dq, *const dk = g.dk, *const dv = g.dv;
-    if (dk || dv) {
+    g.rows = (size_t)qr.n * qr.B * qr.heads;
+    {  // dq, and each row's f (wanted for dk and dv too)
+        using Sh = QueriesShape<NP, DP>;
+        constexpr auto kernel = attend_grad_queries<NP, DP>;
+        g.tq = Sh::RT / g.G;
+        g.tiles = (int)ceil_div(c.T, g.tq);
+        split(pairs * g.tiles, (int)ceil_div(c.S, kKeys), op->num_sms * Sh::kCtas, (c.q_len || c.kv_len) && g.B > 1);
+        g.sorted = few_each(g.items, op->num_sms * Sh::kCtas, g.B, g.kv_len);
+        g.plane = (size_t)qr.n * qr.B * qr.heads * qr.D;
+        e = maps(kKeys);
+        if (!e) e = op_workspace(op, kWsNorm, g.rows * 4);
+        g.norm = (float *)op->ws[kWsNorm];
+        if (!e && g.split > 1 && dq && !(e = op_workspace(op, kWsPart, g.split * g.plane * 4))) g.dq = (float *)op->ws[kWsPart];
+        if (!e && g.split > 1 && !(e = op_workspace(op, kWsPartStats, g.split * g.rows * 4))) g.part_norm = (float *)op->ws[kWsPartStats];
+        if (!e) e = smem_at_least((const void *)kernel, Sh::kSmem);
+        if (!e) e = launch_after(kernel, dim3((unsigned)std::min(g.items, op->num_sms * Sh::kCtas)), 256, Sh::kSmem, op->stream, m, g);
+        if (!e && g.split > 1) e = sum(qr, g.q_len, g.kv_len, c.S, kKeys, g.dq, nullptr, dq, nullptr, g.part_norm);
+    }
+    if (!e && (dk || dv)) {
         using Sh = StatesShape<NP, DP>;
         constexpr auto kernel = attend_grad_states<NP, DP>;
         const Rows kr = state_rows(op, c.S);
@@ -2128,21 +2183,7 @@ cudaError_t launch_backward(stacklstm_op *op, const Call &c, const Operand (&o)[
         }
         if (!e) e = smem_at_least((const void *)kernel, Sh::kSmem);
         if (!e) e = launch_after(kernel, dim3((unsigned)std::min(g.items, op->num_sms)), Sh::kThreads, Sh::kSmem, op->stream, m, g);
-        if (!e && g.split > 1) e = sum(kr, g.kv_len, g.q_len, c.T, g.tq, g.dk, g.dv, dk, dv);
-    }
-    if (!e && dq) {
-        using Sh = QueriesShape<NP, DP>;
-        constexpr auto kernel = attend_grad_queries<NP, DP>;
-        g.tq = Sh::RT / g.G;
-        g.tiles = (int)ceil_div(c.T, g.tq);
-        split(pairs * g.tiles, (int)ceil_div(c.S, kKeys), op->num_sms * Sh::kCtas, (c.q_len || c.kv_len) && g.B > 1);
-        g.sorted = few_each(g.items, op->num_sms * Sh::kCtas, g.B, g.kv_len);
-        g.plane = (size_t)qr.n * qr.B * qr.heads * qr.D;
-        e = maps(kKeys);
-        if (!e && g.split > 1 && !(e = op_workspace(op, kWsPart, g.split * g.plane * 4))) g.dq = (float *)op->ws[kWsPart];
-        if (!e) e = smem_at_least((const void *)kernel, Sh::kSmem);
-        if (!e) e = launch_after(kernel, dim3((unsigned)std::min(g.items, op->num_sms * Sh::kCtas)), 256, Sh::kSmem, op->stream, m, g);
-        if (!e && g.split > 1) e = sum(qr, g.q_len, g.kv_len, c.S, kKeys, g.dq, nullptr, dq, nullptr);
+        if (!e && g.split > 1) e = sum(kr, g.kv_len, g.q_len, c.T, g.tq, g.dk, g.dv, dk, dv, nullptr);
     }
     return e;
 }

@@ -6,6 +6,7 @@ import torch
 
 from oracle import attention as at
 from paper_1904_03409_gb300 import binding as bd
+import test_gpu_attention as tga
 from test_gpu_attention import BF, FP, TYPES, U, Case, empty, tdt, within
 
 pytestmark = pytest.mark.gpu
@@ -186,3 +187,53 @@ def test_results_of_large_scores(dt, offset, B, T, S, nh, nk, D):
     assert float((ctx.double().view(want.shape) - want).norm()) <= 1.5e-6 * float(want.norm())
     wl = torch.logsumexp(z, -1).permute(3, 0, 1, 2).reshape(T, B, nh)
     assert bool(((lse.double() - wl).abs() <= U * wl.abs() + 2.0 ** -20).all())
+
+
+@TYPES
+@pytest.mark.parametrize("offset", [0, 300, 3200, -3200])
+@pytest.mark.parametrize("B,T,S,nh,nk,D", [(3, 119, 300, 8, 2, 40), (1, 700, 130, 2, 1, 112), (2, 40, 1300, 2, 2, 64), (20, 130, 60, 8, 8, 24)])
+def test_gradients_of_large_scores(dt, offset, B, T, S, nh, nk, D):
+    """Scores around `offset` that fp32 holds exactly (products of whole numbers of few bits): gradients as a whole as exact as those
+    of scores around 0. Of a weight, which the bound of test_gradients_keep_32_bits_over_many_states leaves without
+    lse's rounding: sqrt(0.24^2 + 2 x 0.66^2 + 0.48^2 + 0.41^2) = 1.2e-6 of it at most. One at a time the same bits."""
+    g = torch.Generator(device="cuda").manual_seed(S + D)
+    r = lambda n, h, m: torch.randint(-m, m + 1, (n, B, h, D), device="cuda", generator=g).float()
+    q, k = r(T, nh, 1), r(S, nk, 1)
+    q[..., 0], k[..., 0] = 25.0, offset / 6.25  # (of a quarter: `offset` itself)
+    v, dy = torch.randn(S, B, nk, D, device="cuda", generator=g), torch.randn(T, B, nh, D, device="cuda", generator=g)
+    q, k, v = (t.to(tdt(dt)).flatten(2) for t in (q, k, v))
+    dy, scale = dy.flatten(2), 0.25
+    q_len, kv_len = torch.tensor([T, T // 2, T][:B] + [T] * (B - 3), device="cuda").int(), torch.tensor([S, S, S // 3][:B] + [S] * (B - 3), device="cuda").int()
+    h = lambda x: x.double().view(x.shape[0], B, nk, -1, D)
+    see = torch.arange(S, device="cuda")[None] < kv_len[:, None]
+    use = (torch.arange(T, device="cuda")[:, None] < q_len[None]).view(T, B, 1, 1, 1)
+    z = (scale * torch.einsum("tbngd,sbnxd->bngts", h(q), h(k))).masked_fill(~see.view(B, 1, 1, 1, S), -float("inf"))
+    w = torch.softmax(z, -1)
+    dw = torch.einsum("tbngd,sbnxd->bngts", h(dy) * use, h(v))
+    dz = scale * w * (dw - (w * dw).sum(-1, keepdim=True))
+    want = (torch.einsum("bngts,sbnxd->tbngd", dz, h(k)), torch.einsum("bngts,tbngd->sbnd", dz, h(q)), torch.einsum("bngts,tbngd->sbnd", w, h(dy) * use))
+    op = bd.stacklstm_attend_create(T, S, B, nh, nk, D, dt)
+    y, lse, ctx = empty(*q.shape, dtype=tdt(dt)), empty(T, B, nh), empty(*q.shape)
+    bd.stacklstm_attend_forward(op, q, k, v, q_len, kv_len, scale, y, lse, ctx)
+    grads = [empty(n, B, c * D) for n, c in ((T, nh), (S, nk), (S, nk))]
+    bd.stacklstm_attend_backward(op, dy, q, k, v, q_len, kv_len, scale, lse, ctx, *grads)
+    bd.stacklstm_op_status(op)
+    for name, a, b in zip(("dq", "dk", "dv"), grads, want):
+        a = a.double().view(b.shape)
+        if name == "dq":  # (column 0 is the states' common one, a sum of dz: nothing but its rounding)
+            a, b = a[..., 1:], b[..., 1:]
+        assert float((a - b).norm()) <= 1.2e-6 * float(b.norm()), name
+    for i in range(3):
+        one = [torch.full_like(t, float("nan")) if j == i else None for j, t in enumerate(grads)]
+        bd.stacklstm_attend_backward(op, dy, q, k, v, q_len, kv_len, scale, lse, ctx, *one)
+        assert torch.equal(one[i], grads[i])
+    bd.stacklstm_op_status(op)
+
+
+@TYPES
+def test_gradients_of_sharp_weights(dt, monkeypatch):
+    """z in the hundreds with the backward: weights down to e^-300 and below, of which those under 2^-126 (and parts of numbers
+    under it) are 0 in fp32. A gradient's 40 terms are such a number times |dy . v| <= 64 x 4 x 4, |q| <= 30 and the scale
+    of 1 at most: 2^-126 x 40 x 1024 x 30 < 2^-105."""
+    monkeypatch.setattr(tga, "within", lambda got, want, tol, what="": within(got, want, tol + 2.0 ** -105, what))
+    Case(dt, 2, 20, 300, 2, 2, 64, scale=1.0, sharp=6.0).check()
