@@ -806,6 +806,7 @@ attend_forward(const __grid_constant__ Maps<NP> tm, const __grid_constant__ FwdA
             // that neither w nor the sums mind
             float m = -INFINITY, l = 0.0f, alpha = 1.0f;  // w = 2^(c z - base2), base2 = c m as rounded
             float kept2 = 0.0f;  // base2 of the sums in memory
+            float only = 0.0f;   // z of a single state, which is taken from itself
             const size_t row = (size_t)w.b * g.q_b + (size_t)t * g.q_t + head;
             auto kept = [&](int d) { return (float4 *)(g.sums + (w.sp * g.rows + row) * g.Dp + d); };  // four of them
             auto add_o = [&]() {  // o = o alpha + the last tile's w v
@@ -871,6 +872,10 @@ attend_forward(const __grid_constant__ Maps<NP> tm, const __grid_constant__ FwdA
                         for (int j = 0; j < CZ / 2; ++j) {
                             if (CZ * h + 2 * j >= left) z[j].x = -INFINITY;
                             if (CZ * h + 2 * j + 1 >= left) z[j].y = -INFINITY;
+                        }
+                        if (len == 1 && h == 0) {  // its weight is 1, not 2^(what rounding leaves of z's exponent)
+                            only = z[0].x;
+                            z[0].x -= only;
                         }
                     }
                 };
@@ -981,7 +986,8 @@ attend_forward(const __grid_constant__ Maps<NP> tm, const __grid_constant__ FwdA
             const bool some = here && n > 0;
             const float by = some ? 1.0f / l : 0.0f;
             // l is against base2, not c m: an lse that left the difference out was 8e-7 off (2221 states), with it 3e-7
-            const float off = m == -INFINITY ? 0.0f : fmaf(m, c, -__fmul_rn(m, c));
+            if (len == 1) m = only;
+            const float off = m == -INFINITY || len == 1 ? 0.0f : fmaf(m, c, -__fmul_rn(m, c));
             const bool pieces = g.D % 8 == 0;
             // CD of the outputs' columns, from d0 on
             auto put = [&](auto &v, int d0) __attribute__((always_inline)) {
@@ -1516,6 +1522,13 @@ attend_grad_states(const __grid_constant__ BwdMaps<NP> tm, const __grid_constant
 #pragma unroll
                         for (int k = 0; k < 8; ++k)
                             if (!live) wv[h][k] = make_float2(0.0f, 0.0f);
+                    // (one state has weight 1, whatever z is: not what rounding leaves of it. 0 stays 0, a NaN one)
+                    if (w.len == 1)
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            if (wv[h][k].x > 0.0f) wv[h][k].x = 1.0f;
+                            if (wv[h][k].y > 0.0f) wv[h][k].y = 1.0f;
+                        }
                 }
                 if (n > 0) {  // w's place is free; the last tile's dv (dk) is there, which the next one's takes the place of
                     if (!warp_wait(v_full, (uint32_t)(n - 1) & 1, limit, abort)) return false;

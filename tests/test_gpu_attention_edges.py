@@ -237,3 +237,32 @@ def test_gradients_of_sharp_weights(dt, monkeypatch):
     of 1 at most: 2^-126 x 40 x 1024 x 30 < 2^-105."""
     monkeypatch.setattr(tga, "within", lambda got, want, tol, what="": within(got, want, tol + 2.0 ** -105, what))
     Case(dt, 2, 20, 300, 2, 2, 64, scale=1.0, sharp=6.0).check()
+
+
+@pytest.mark.parametrize("S,nk,D", [(1, 1, 16), (1, 2, 21), (300, 1, 64), (70, 2, 100)])
+@pytest.mark.parametrize("scale", [1.0, 40.0])
+def test_a_single_state_has_weight_1(S, nk, D, scale):
+    """Whatever its score is: y = v and dv the sum of dy, finite also at the largest numbers (three parts of a number, of sums that
+    may cut: 4 u), dq = dk = 0; sentences of one state among others."""
+    T, B = 3, 3
+    big = float(torch.finfo(torch.float32).max)
+    g = torch.Generator(device="cuda").manual_seed(D)
+    r = lambda n, h: torch.randn(n, B, h * D, device="cuda", generator=g)
+    q, k, v, dy = r(T, nk), r(S, nk), r(S, nk), r(T, nk)
+    v[..., ::3], v[..., 4] = big, -big
+    dy[1:] = 0  # (a sum of one)
+    dy[0, :, 1::2], dy[0, :, 2] = big, 2.0 ** -126
+    kv_len = torch.tensor([1, S, 1], device="cuda").int()
+    if S > 1:  # (a mean of the largest numbers is its own concern)
+        v[:, 1], dy[:, 1] = r(S, nk)[:, 1], r(T, nk)[:, 1]
+    op = bd.stacklstm_attend_create(T, S, B, nk, nk, D, FP)
+    y, lse, grads = empty(T, B, nk * D), empty(T, B, nk), [empty(n, B, nk * D) for n in (T, S, S)]
+    bd.stacklstm_attend_forward(op, q, k, v, None, kv_len, scale, y, lse)
+    bd.stacklstm_attend_backward(op, dy, q, k, v, None, kv_len, scale, lse, y, *grads)
+    bd.stacklstm_op_status(op)
+    for b in (0, 2):
+        for got, want in ((y[:, b], v[:1, b].expand(T, -1)), (grads[2][:1, b], dy[:1, b])):
+            assert torch.isfinite(got).all() and bool(((got - want).abs().double() <= 4 * U * want.abs().double()).all())
+        assert not grads[0][:, b].any() and not grads[1][:, b].any() and not grads[2][1:, b].any()
+    z = scale * (q[:, 0].double() * k[:1, 0].double()).view(T, nk, D).sum(-1)
+    assert bool(((lse[:, 0].double() - z).abs() <= 2 * U * scale * (D + 9) * (q[:, 0].abs() * k[:1, 0].abs()).view(T, nk, D).sum(-1)).all())
