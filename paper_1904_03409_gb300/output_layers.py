@@ -190,14 +190,18 @@ class AttentiveLayers:
         return self.logits[:r]
 
     def learn(self, y, target, dlogp, dentropy, q_len=None):
-        """Forward with dropout of the tops y [T B, H] (q_len [B] of them in each sentence), and the gradients of the
-        objective whose gradient with respect to each row's log probability of its target (-1: none) and entropy is
-        dlogp, dentropy [T B]: the layers' (``grads``), the tops' dy [T B, H] and the states' dstates [s B, E].
-        Returns (logp, entropy, dy, dstates)."""
+        """Forward with dropout of the tops y [T B, H] (q_len [B] of them in each sentence, the others finite), and the
+        gradients of the objective whose gradient with respect to each row's log probability of its target (-1: none) and
+        entropy is dlogp, dentropy [T B] (whatever they are behind a sentence's end: those rows have no part in it): the
+        layers' (``grads``), the tops' dy [T B, H] and the states' dstates [s B, E]. Returns (logp, entropy, dy, dstates)."""
+        import torch
         self._on_current_stream()
         self._have_memory()
         r, p, g, s = self.rows, self.params, self.grads, self.s
         T, B, H = self.T, self.B, self.H
+        if q_len is not None:
+            behind = (torch.arange(T, device=y.device)[:, None] >= q_len[None]).view(r)
+            dlogp, dentropy = (None if d is None else d.masked_fill(behind, 0.0) for d in (dlogp, dentropy))
         at = lambda x: x[:r].view(T, B, H)
         kk, vv, lens = self.kk[:s], self.vv[:s], (q_len, self.kv_len)
         self._tops(y, True, lambda: bd.stacklstm_attend_forward(self.attend, at(self.q), kk, vv, *lens, self.scale, at(self.u), self.lse, self.ctx))
@@ -240,7 +244,7 @@ def train_step(hd, ins: dict, out: dict, layers: OutputLayers, t_idx, t_logit, g
 def policy_step(hd, ins: dict, out: dict, layers: AttentiveLayers, target, dlogp, dentropy, q_len=None):
     """One training step of a StackLSTM under ``layers`` as a policy over its classes (their ``memory`` set):
     target, dlogp, dentropy [T B] as in ``AttentiveLayers.learn`` (for a step along the gradient of
-    sum(weight logp + c entropy): -weight and -c). Returns (logp, entropy, dstates); the gradients are in
+    sum(weight logp + c entropy) over each sentence's q_len rows: -weight and -c). Returns (logp, entropy, dstates); the gradients are in
     ``layers.grads`` and ``out``. Streams as in ``train_step``."""
     def learn(y):
         logp, entropy, dy, dstates = layers.learn(y, target, dlogp, dentropy, q_len)

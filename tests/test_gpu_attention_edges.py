@@ -6,6 +6,7 @@ import torch
 
 from oracle import attention as at
 from paper_1904_03409_gb300 import binding as bd
+from paper_1904_03409_gb300 import output_layers as om
 import test_gpu_attention as tga
 from test_gpu_attention import BF, FP, TYPES, U, Case, empty, tdt, within
 
@@ -266,3 +267,26 @@ def test_a_single_state_has_weight_1(S, nk, D, scale):
         assert not grads[0][:, b].any() and not grads[1][:, b].any() and not grads[2][1:, b].any()
     z = scale * (q[:, 0].double() * k[:1, 0].double()).view(T, nk, D).sum(-1)
     assert bool(((lse[:, 0].double() - z).abs() <= 2 * U * scale * (D + 9) * (q[:, 0].abs() * k[:1, 0].abs()).view(T, nk, D).sum(-1)).all())
+
+
+@TYPES
+def test_rows_behind_a_sentences_end_have_no_part_in_the_objective(dt):
+    """A constant weight of the entropy, and anything in dlogp: the same gradients as with zeros there."""
+    T, B, S, H, E, V, heads = 7, 4, 9, 24, 16, 13, 2
+    rng = np.random.default_rng(3)
+    up = lambda a, t=None: torch.from_numpy(np.ascontiguousarray(a)).cuda().to(t or torch.float32)
+    q_len = up([7, 3, 1, 0], torch.int32)
+    inside = torch.arange(T, device="cuda")[:, None] < q_len[None]
+    y, mem = up(rng.normal(size=(T * B, H)), tdt(dt)), up(rng.normal(size=(S, B, E)), tdt(dt))
+    target, g = up(rng.integers(0, V, T * B), torch.int32), up(rng.normal(size=T * B)).view(T, B)
+    out = []
+    for dlogp, dent in ((torch.where(inside, g, float("nan")), torch.full((T, B), 0.1, device="cuda")),
+                        (torch.where(inside, g, 0.0), torch.where(inside, 0.1, 0.0))):
+        layers = om.AttentiveLayers(T, B, S, H, E, V, heads, p=0.2, dtype=dt, seed=5)
+        layers.memory(mem)
+        _, _, dy, dstates = layers.learn(y, target, dlogp.reshape(-1), dent.reshape(-1), q_len)
+        layers.status()
+        out.append([t.clone() for t in (dy, dstates, *layers.grads.values())])
+        assert torch.isfinite(dy).all() and not dy.view(T, B, H)[~inside].any()
+        layers.destroy()
+    assert all(torch.equal(a, b) for a, b in zip(*out))
