@@ -22,8 +22,8 @@ struct DropArgs {
     int all;
     float by;
     const long long *step;
-    int copies;                // uses of each mask element, of which a thread takes
-    int per;                   //  so many
+    unsigned copies;           // uses of each mask element (2^31 - 1 at most), of which a thread takes
+    unsigned per;              //  so many
 };
 
 __device__ __forceinline__ void philox7(uint32_t (&c)[4], uint32_t k0, uint32_t k1)
@@ -100,8 +100,8 @@ dropout(const __grid_constant__ DropArgs a)
     T *y = (T *)a.y;
     if (MANY && first >= pieces) return;
     const uint32_t mine = MANY ? kept(a, first, s0, s1) : 0;
-    const int c_lo = MANY ? blockIdx.y * a.per : 0, c_hi = MANY ? min(c_lo + a.per, a.copies) : kInFlight;
-    for (int c0 = c_lo; c0 < c_hi; c0 += kInFlight) {
+    const unsigned c_lo = MANY ? blockIdx.y * a.per : 0, c_hi = MANY ? min(c_lo + a.per, a.copies) : kInFlight;
+    for (unsigned c0 = c_lo; c0 < c_hi; c0 += kInFlight) {
         size_t at[kInFlight];
         Eight<T> q[kInFlight], w[kInFlight];
         bool here[kInFlight];
@@ -157,9 +157,8 @@ cudaError_t launch_dropout(const stacklstm_op *op, DropArgs &a)
     // as few uses a thread as fill the GPU with threads, kInFlight at least
     const size_t ctas = ceil_div(pieces, 256);
     const size_t groups = std::max<size_t>(1, (size_t)op->num_sms * 8 / ctas);
-    a.per = (int)std::max<size_t>(kInFlight, ceil_div(a.copies, groups));
+    a.per = (unsigned)std::max<size_t>(kInFlight, std::max(ceil_div(a.copies, groups), ceil_div(a.copies, 65535)));
     a.per = (a.per + kInFlight - 1) / kInFlight * kInFlight;
-    a.per = std::max(a.per, (int)ceil_div(a.copies, 65535));
     const dim3 grid((unsigned)ctas, ceil_div(a.copies, a.per));
     return whole ? launch_after(dropout<T, true, true>, grid, 256, 0, op->stream, a)
                  : launch_after(dropout<T, false, true>, grid, 256, 0, op->stream, a);
@@ -181,7 +180,7 @@ sl_status run(stacklstm_op *op, int rows, const void *x, const void *residual, d
     const int period = mask_rows == 0 || mask_rows > rows ? rows : mask_rows;
     a.total = (size_t)rows * op->N;
     a.period = (size_t)period * op->N;
-    a.copies = (rows + period - 1) / period;
+    a.copies = ((unsigned)rows + (unsigned)period - 1) / (unsigned)period;
     a.x = x; a.residual = residual; a.y = y; a.step = (const long long *)step;
     a.k0 = (uint32_t)seed; a.k1 = (uint32_t)(seed >> 32);
     const unsigned long long least = (unsigned long long)nearbyint(p * 4294967296.0);  // kept from this word on

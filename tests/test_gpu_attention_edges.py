@@ -290,3 +290,17 @@ def test_rows_behind_a_sentences_end_have_no_part_in_the_objective(dt):
         assert torch.isfinite(dy).all() and not dy.view(T, B, H)[~inside].any()
         layers.destroy()
     assert all(torch.equal(a, b) for a, b in zip(*out))
+
+
+@pytest.mark.parametrize("rows,mask_rows", [(1500000000, 1000000000), (2 ** 31 - 1, 1), (2 ** 31 - 1, 2 ** 31 - 2)])
+def test_dropout_of_rows_and_mask_rows_beyond_31_bits(rows, mask_rows):
+    op = bd.stacklstm_dropout_create(rows, 1, BF)
+    x = torch.ones(rows, 1, device="cuda", dtype=torch.bfloat16)
+    bd.stacklstm_dropout_forward(op, x, None, 0.5, 5, None, mask_rows, x)
+    bd.stacklstm_op_status(op)
+    keep = at.keep(min(mask_rows, 1000), 1, 0, 0.5, 5, 0)
+    assert ((x[: len(keep), 0].double().cpu().numpy() == 2) == keep).all()
+    if mask_rows == 1:
+        assert bool((x == x[0]).all())
+    else:
+        assert torch.equal(x[mask_rows:], x[: rows - mask_rows]) and bool(((x == 0) | (x == 2)).all())
