@@ -156,6 +156,8 @@ class AttentiveLayers:
     def memory(self, states, kv_len=None):
         """The encoder's states [s, B, E] (s up to S; kv_len [B] int32 of them in each sentence, the others finite)
         that the following calls look at."""
+        if states.dim() != 3 or states.shape[0] > self.S or states.shape[1:] != (self.B, self.E):
+            raise ValueError("states must be [s, %d, %d] of at most %d states" % (self.B, self.E, self.S))
         self._on_current_stream()
         s = states.shape[0]
         flat, kv = states.reshape(s * self.B, self.E), (self.kk[:s].view(s * self.B, -1), self.vv[:s].view(s * self.B, -1))
@@ -195,6 +197,8 @@ class AttentiveLayers:
         entropy is dlogp, dentropy [T B] (whatever they are behind a sentence's end: those rows have no part in it): the
         layers' (``grads``), the tops' dy [T B, H] and the states' dstates [s B, E]. Returns (logp, entropy, dy, dstates)."""
         import torch
+        if y.shape != (self.rows, self.H):
+            raise ValueError("y must be [%d, %d]: the tops of every step of every sentence" % (self.rows, self.H))
         self._on_current_stream()
         self._have_memory()
         r, p, g, s = self.rows, self.params, self.grads, self.s
@@ -277,15 +281,17 @@ def _stack_step(hd, ins: dict, out: dict, learn):
 
 
 def beam_decode(layers, W, bias, emb, ops, h0, c0, K: int, steps: int, end: int = -1):
-    """(``layers``: OutputLayers, or AttentiveLayers whose ``memory`` holds the sentences' states.)
-    The K best sequences of up to ``steps`` classes for each of the B sentences whose stacks start
-    at h0, c0 [B, H]. Class v pushes, pops or holds (ops [V] int8) with the input emb[v] (emb
+    """The K best sequences of up to ``steps`` classes for each of the B sentences whose stacks start
+    at h0, c0 [B, H] under ``layers``: OutputLayers, or AttentiveLayers of B sentences whose ``memory``
+    holds their states. Class v pushes, pops or holds (ops [V] int8) with the input emb[v] (emb
     [V, I]); a pop of an empty stack is no candidate; class ``end`` ends a sequence. W, bias: the
     StackLSTM's. Returns (scores [B, K], classes [B, K, steps], -1 after an end), best first; where
     there are fewer than K sequences, -inf and -1."""
     import torch
     B, H = h0.shape
     V, I = emb.shape
+    if isinstance(layers, AttentiveLayers) and (layers.B != B or K > layers.beam):
+        raise ValueError("the layers look at the states of %d sentences, for beams of at most %d" % (layers.B, layers.beam))
     N, S, dt, dev = B * K, steps + 1, h0.dtype, h0.device
     f = lambda *s: torch.empty(*s, dtype=torch.float32, device=dev)
     i32 = lambda *s: torch.empty(*s, dtype=torch.int32, device=dev)

@@ -304,3 +304,29 @@ def test_dropout_of_rows_and_mask_rows_beyond_31_bits(rows, mask_rows):
         assert bool((x == x[0]).all())
     else:
         assert torch.equal(x[mask_rows:], x[: rows - mask_rows]) and bool(((x == 0) | (x == 2)).all())
+
+
+def test_sizes_that_the_attentive_layers_refuse():
+    """Sentences other than those whose states they look at (4 rows were taken for 4 sentences of one hypothesis where they were 2
+    of two), tops of fewer or more steps, states of another width."""
+    B, S, H, E, V, I = 4, 5, 16, 8, 7, 8
+    layers = om.AttentiveLayers(2, B, S, H, E, V, 2, beam=2, dtype=FP)
+    x = lambda *s: torch.randn(*s, device="cuda")
+    for shape in ((S + 1, B, E), (S, B + 1, E), (S, 2 * B, E // 2), (S, B * E)):
+        with pytest.raises(ValueError):
+            layers.memory(x(*shape))
+    layers.memory(x(S, B, E))
+    ops = torch.ones(V, device="cuda", dtype=torch.int8)
+    for n, K in ((2, 2), (B, 3)):
+        with pytest.raises(ValueError):
+            om.beam_decode(layers, x(I + H, 4 * H), x(4 * H), x(V, I), ops, x(n, H), x(n, H), K, 3)
+    score, _ = om.beam_decode(layers, x(I + H, 4 * H), x(4 * H), x(V, I), ops, x(B, H), x(B, H), 2, 3)
+    assert torch.isfinite(score).all()
+    grads = [g.fill_(7.0) for g in layers.grads.values()]
+    zero = torch.zeros(2 * B, device="cuda")
+    for rows in (2 * B - 1, B, 2 * B + 1):
+        with pytest.raises(ValueError):
+            layers.learn(x(rows, H), zero.int(), zero, zero)
+    assert all(bool((g == 7.0).all()) for g in grads) and int(layers.step) == 0
+    layers.status()
+    layers.destroy()
