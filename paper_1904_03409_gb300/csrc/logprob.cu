@@ -369,33 +369,39 @@ __device__ __forceinline__ void read_entry(const GradArgs &a, size_t r, int j, i
 {
     int v = -1;
     float g = 0.0f;
-    if (j < a.k) {
-        v = a.top_idx && a.dtop ? a.top_idx[r * a.k + j] : -1;
-        g = v != -1 ? a.dtop[r * a.k + j] : 0.0f;
-    } else {
-        v = a.target && a.dlogp ? a.target[r] : -1;
-        g = v != -1 ? a.dlogp[r] : 0.0f;
+    if (j < a.k) {  // (k is 0 without dtop)
+        v = a.top_idx[r * a.k + j];
+        g = a.dtop[r * a.k + j];
+    } else if (a.target && a.dlogp) {
+        v = a.target[r];
+        g = a.dlogp[r];
     }
     if (v < -1 || v >= a.V) {
         atomicCAS(a.err, 0, (int)SL_ERR_ARG);  // skipped
         v = -1;
-        g = 0.0f;
     }
+    if (v < 0) g = 0.0f;
     c[j] = v;
     w[j] = g;
 }
 
 struct Grad {
-    float lse, rest, all, h;  // lp = z - lse - rest; all = G + h H
+    float lse, h, entropy;
+    float rest, all;          // lp = z - lse - rest; all = G + h H
     bool none;
-    // (the entries read, f of the row known)
-    __device__ __forceinline__ Grad(const GradArgs &a, size_t r, const float *w, float lse_, float f) : lse(lse_), rest(logf(f))
+    __device__ __forceinline__ Grad(const GradArgs &a, size_t r)
     {
-        none = lse == -INFINITY;
+        lse = a.lse[r];
         h = a.dentropy ? a.dentropy[r] : 0.0f;
+        entropy = a.dentropy ? a.entropy[r] : 0.0f;
+        none = lse == -INFINITY;
+    }
+    __device__ __forceinline__ void join(int k, const float *w, float f)  // the entries' weights, f of the row
+    {
+        rest = logf(f);
         all = 0.0f;
-        for (int j = 0; j <= a.k; ++j) all += w[j];
-        if (a.dentropy) all = fmaf(h, a.entropy[r], all);
+        for (int j = 0; j <= k; ++j) all += w[j];
+        all = fmaf(h, entropy, all);
     }
     __device__ __forceinline__ float operator()(float z) const
     {
@@ -414,11 +420,17 @@ __device__ __forceinline__ float piece_sum(const uint4 &q, float lse)
     return s;
 }
 // Pieces p_lo .. n of a row are written: the few classes of the entries among them are once more. The first entry of each
-// class takes the sum of the class's weights in entry order, so repeated classes need no atomics.
-template <typename T, int TPR>
-__device__ __forceinline__ void put_entries(const GradArgs &a, const Grad &g, const RowVec<T> &row, int p_lo, int n, const int *c, const float *w, int t)
+// class takes the sum of the class's weights in entry order, so repeated classes need no atomics. (mine: entry t's logit,
+// where each thread has one at most)
+template <typename T>
+__device__ __forceinline__ float entry_logit(const GradArgs &a, const RowVec<T> &row, const int *c, int t)
 {
-    const T *z = (const T *)a.z;
+    return t <= a.k && c[t] >= 0 ? to_f32(((const T *)a.z)[row.first() + c[t]]) : 0.0f;
+}
+template <typename T, int TPR>
+__device__ __forceinline__ void put_entries(const GradArgs &a, const Grad &g, const RowVec<T> &row, int p_lo, int n, const int *c, const float *w, int t,
+                                            float mine)
+{
     const int c_lo = row.column(p_lo), c_hi = row.column(n);
     for (int j = t; j <= a.k; j += TPR) {
         const int v = c[j];
@@ -430,13 +442,14 @@ __device__ __forceinline__ void put_entries(const GradArgs &a, const Grad &g, co
                 if (i < j) first = false;
                 if (i > j) sum += w[i];
             }
-        if (first) a.dz[row.first() + v] = g(to_f32(z[row.first() + v])) + sum;
+        if (first) a.dz[row.first() + v] = g(TPR > 64 ? mine : entry_logit<T>(a, row, c, j)) + sum;
     }
 }
 
 // A row's pieces read once for f and for the gradient, NP a thread in registers: TPR lanes (8, 32) to a row, several rows a CTA,
 // or a CTA of TPR threads; what 1024 threads do not hold they read again, in part from L2.
-// Bound by HBM: 4096 x 32003 bf16 133 us, 5.9 TB/s (6 bytes a class). (A row over a cluster of CTAs, 2000 x 70001: 222 us, 169 so.)
+// Bound by HBM: 4096 x 32003 bf16 with 8 alternatives 138 us, 5.7 TB/s (6 bytes a class), 121 without; 148 and 128 where what a
+// row needs of entropy, weights and entries' logits was read after its sum. (A row over a cluster of CTAs, 2000 x 70001: 222 us, 169 so.)
 template <typename T, int TPR, int NP>
 __global__ void __launch_bounds__(row_cta(TPR), TPR <= 32 ? 1 : row_ctas_per_sm(TPR))
 logprob_grad(const __grid_constant__ GradArgs a)
@@ -460,11 +473,11 @@ logprob_grad(const __grid_constant__ GradArgs a)
         if (u * TPR + t < n) q[u] = row.load(z, u * TPR + t);
     if (here)
         for (int j = t; j < k1; j += TPR) read_entry(a, r, j, c, w);
-    const float lse = here ? a.lse[r] : 0.0f;
+    Grad g(a, here ? r : 0);
     float f[1] = {0.0f};
 #pragma unroll
     for (int u = 0; u < NP; ++u)
-        if (u * TPR + t < n) f[0] += piece_sum<T>(q[u], lse);
+        if (u * TPR + t < n) f[0] += piece_sum<T>(q[u], g.lse);
     constexpr int U = 4;  // of a longer row's pieces at a time
     if constexpr (TPR == 1024)
         for (int p = NP * TPR + t; p < n; p += U * TPR) {
@@ -474,12 +487,13 @@ logprob_grad(const __grid_constant__ GradArgs a)
                 if (p + u * TPR < n) x[u] = row.load(z, p + u * TPR);
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (p + u * TPR < n) f[0] += piece_sum<T>(x[u], lse);
+                if (p + u * TPR < n) f[0] += piece_sum<T>(x[u], g.lse);
         }
     row_join<false, TPR>(f, sm);  // (and the entries are written, of a row over a CTA)
     if constexpr (TPR <= 32) __syncwarp();
     if (!here) return;
-    const Grad g(a, r, w, lse, f[0]);
+    g.join(a.k, w, f[0]);
+    const float mine = TPR > 64 ? entry_logit<T>(a, row, c, t) : 0.0f;
     const bool aligned = on_32(a.dz);
     auto put = [&](const uint4 &x, int p) {
         float v[RowVec<T>::E];
@@ -505,7 +519,7 @@ logprob_grad(const __grid_constant__ GradArgs a)
         __syncwarp(TPR == 32 ? 0xffffffffu : 0xffu << (threadIdx.x & 24));
     else
         __syncthreads();
-    put_entries<T, TPR>(a, g, row, 0, n, c, w, t);
+    put_entries<T, TPR>(a, g, row, 0, n, c, w, t, mine);
 }
 
 // Long rows, too few to fill the GPU with a CTA each: f in parts first, a CTA of 256 threads each, ... (8 x 32003 bf16 both
@@ -557,10 +571,12 @@ logprob_grad_range(const __grid_constant__ GradArgs a)
     for (int u = 0; u < U; ++u)
         if (p_lo + u * 256 + t < n) q[u] = row.load(z, p_lo + u * 256 + t);
     for (int j = t; j <= a.k; j += 256) read_entry(a, r, j, c, w);
+    Grad g(a, r);
     float f[1] = {0.0f};
     for (int i = t; i < a.sums; i += 256) f[0] += a.part[r * a.sums + i];
     row_join<false, 256>(f, sm);
-    const Grad g(a, r, w, a.lse[r], f[0]);
+    g.join(a.k, w, f[0]);
+    const float mine = entry_logit<T>(a, row, c, t);
     const bool aligned = on_32(a.dz);
     for (int p = p_lo + t; p < n; p += U * 256) {
 #pragma unroll
@@ -577,7 +593,7 @@ logprob_grad_range(const __grid_constant__ GradArgs a)
             if (p + (U + u) * 256 < n) q[u] = row.load(z, p + (U + u) * 256);
     }
     __syncthreads();
-    put_entries<T, 256>(a, g, row, p_lo, n, c, w, t);
+    put_entries<T, 256>(a, g, row, p_lo, n, c, w, t, mine);
 }
 
 template <typename T>
