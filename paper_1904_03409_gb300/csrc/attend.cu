@@ -2080,11 +2080,12 @@ bool few_each(long long items, long long ctas, int B, const int32_t *len)
 }
 
 // In how many splits (`most` at most) items of `tiles` tiles each go over the `room` CTAs there are. An item's begin and
-// end cost `ends` tiles, the join of the splits `join`. Where the sentences differ (uneven) CTAs take what there is, several
+// end cost `ends` tiles, the join of the splits `join`. Where the sentences differ (uneven) CTAs take what there is, `few`
 // items each, so that their work evens out; else the splits are those that end first: 64 x 8 over 4096 states, 16 heads
-// of 64 over 4, 256 items for 304 CTAs, in one go 51 us and in three splits each 65; of lengths from 1365 to 4096, 50 us in
-// four splits, 62 where a sentence's splits were begun together, 58 in six. Backward, 1 x 1194 x 3442 fp32, 2 heads of 31,
-// 91 us with two items a CTA, 76 so.
+// of 64 over 4, 256 items for 304 CTAs, in one go 51 us and in three splits each 65. Of lengths from a third of it on, with
+// 2, 3, 4, 6 items a CTA: 57, 53, 54, 61 us; 32 x 1 over 8192, 8 heads of 128 over 2: 54, 56, 57, 60; 40 x 8 over 3000, 8 of 128
+// over 4: 54, 51, 52, 55; 8 x 16 over 4096, 16 of 64 over 8: 27, 29, 31, 30. Backward, 1 x 1194 x 3442 fp32, 2 heads of 31, 91
+// us with two items a CTA, 76 so.
 int few_splits(long long items, long long room, int tiles, int most, bool uneven, int few, int ends, int join)
 {
     if (items >= room || most < 2) return 1;
@@ -2113,7 +2114,7 @@ cudaError_t launch_forward(stacklstm_op *op, const Call &c, const Operand (&o)[3
     const long long ctas = (long long)g.tiles * g.nk * g.B, room = (long long)op->num_sms * Sh::kCtas;
     const int tiles = (int)ceil_div(c.S, kKeys), rows = std::min(c.T * g.G, kRows);
     const int least = std::max(4, 8 * rows / kKeys);
-    g.split = few_splits(ctas, room, tiles, std::min(tiles / least, kMostSplits), c.kv_len && g.B > 1, 4, 3, 4);
+    g.split = few_splits(ctas, room, tiles, std::min(tiles / least, kMostSplits), c.kv_len && g.B > 1, 3, 3, 4);
     g.per = (int)ceil_div(tiles, g.split);
     g.split = (int)ceil_div(tiles, g.per);
     if (g.split > 1) {
