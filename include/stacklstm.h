@@ -395,7 +395,8 @@ const char *stacklstm_head_last_error(stacklstm_head_t h);
  * from 0 to the R of create. A handle's workspace grows to the largest call so far (the first
  * such call allocates and, where it replaces a smaller buffer, waits for the stream; a call that
  * is to be captured in a graph is made once before, and the handle's larger ones too: they would free
- * what the graph's kernels use).
+ * what the graph's kernels use). A replay is a call on the stream it runs on: calls and replays of one handle
+ * share its workspace and do not run at the same time.
  */
 typedef struct stacklstm_op *stacklstm_op_t;
 

@@ -498,7 +498,7 @@ __device__ __forceinline__ void pack_block(const Pack &a, unsigned cta, int32_t 
 }
 
 // Bound by HBM and, nearly as much, by instructions: 4 bytes read and 6 written an element (dy: 8 and 6); dy of
-// 64 x 256 x 1024 in 42 us, 5.6 TB/s.
+// 64 x 256 x 1024 in 36 us, 6.5 TB/s.
 __global__ void __launch_bounds__(256)
 attend_pack(const __grid_constant__ Packs a)
 {
@@ -534,8 +534,8 @@ struct FwdShape {
     // up in registers, tile by tile. (w over the tile's own z, two places of both in turn, with heads of 128: 4 x 2048 x 4096
     // 191 us of equal sentences, 173 so.)
     static constexpr bool kSums = PP == 2;
-    // Tiles whose w v are summed in tensor memory before the sum goes to memory, where it is added up in fp32: 8 additions a
-    // tile that cut by less than 2^-23 of the sum each, 2^-14 in all. (Of 2^20 states in one sum y was 0.9 % too small.)
+    // Tiles whose w v are summed in tensor memory before the sum goes to memory, where it is added up in fp32: 8 MMAs a
+    // tile, each of which loses 2^-23.8 of the sum (2^20 values of one sign in one sum: y 0.9 % too small), 2^-14.8 in all.
     static constexpr int kRun = 64;
     static constexpr bool kOver = kCtas == 2 && kKeys + PP * kKeys / 2 + DP > 256;
     static constexpr uint32_t kWs = kSums && DP == 64 ? 2 : 1;  // places for w
@@ -578,8 +578,8 @@ __device__ __forceinline__ void key_tiles(const FwdArgs &g, const Item &w, int &
 // clears what lies behind a sentence's last state, and a thread of warps 4 to 7 has a query: 32 z of a tile at a time
 // in registers, and an fp32 result's sum of w v.
 // Bound by a tile's chain of MMA, reading z, exponentials and writing w, which two CTAs an SM and z one tile ahead hide
-// in part: 64 x 256 x 256, 16 heads of 64, bf16, 52 us, 72 for an fp32 result too; 4 x 2048 x 4096, 8 heads
-// of 128 over 2, 130 us (470 TFLOP/s).
+// in part: 64 x 256 x 256, 16 heads of 64, bf16, 52 us (issue 42 %, tensor pipe 23 %), 71 for an fp32 result too; 8 x 1024 x
+// 1024, 8 heads of 128, 57 us (tensor pipe 46 %), 112; 4 x 2048 x 4096, 8 heads of 128 over 2, 134 us (455 TFLOP/s).
 template <int NP, int PP, int DP>
 __global__ void __launch_bounds__(256, FwdShape<NP, PP, DP>::kCtas)
 attend_forward(const __grid_constant__ Maps<NP> tm, const __grid_constant__ FwdArgs g)
@@ -1223,7 +1223,7 @@ __device__ __forceinline__ bool each_tile(const BwdArgs &g, ItemRing &ring, vola
 // has a state's row and a quarter or half of the queries; heads of 64: eight warps filled 31 % of the issue slots and
 // took 480 us where sixteen take 410) and add up dv (the first half of them) and dk of the tile before. Tile n's MMAs are
 // issued as dv(n), z(n + 1), dk(n), dw(n + 1): w(n + 1) is made while dk(n) and dw(n + 1) run.
-// Bound by the chain z, w, dv, dw, dz, dk of a tile: 64 x 256 x 256, 16 heads of 64, bf16, 145 us, 770 TFLOP/s in 13
+// Bound by the chain z, w, dv, dw, dz, dk of a tile: 64 x 256 x 256, 16 heads of 64, bf16, 146 us, 765 TFLOP/s in 13
 // products of parts (tensor pipe 34 %, issue 53 %).
 template <int NP, int DP>
 __global__ void __launch_bounds__(StatesShape<NP, DP>::kThreads, 1)
@@ -1612,7 +1612,7 @@ struct QueriesShape {
 // CTAs take items one after the other: a tile of query rows of one sentence and state's head. Warp 0 loads (TMA), warp 1 issues
 // the MMAs, warp 2 clears what lies behind a sentence's last state, and a thread of warps 4 to 7 has a query. Tile
 // m's MMAs are issued as z(m + 1), dq(m), dw(m + 1).
-// Bound by the chain z, w, dw, dz of a tile, as above: 64 x 256 x 256, 16 heads of 64, bf16, 87 us, 690 TFLOP/s in 7
+// Bound by the chain z, w, dw, dz of a tile, as above: 64 x 256 x 256, 16 heads of 64, bf16, 89 us, 680 TFLOP/s in 7
 // products of parts (tensor pipe 31 %, issue 36 %; two CTAs an SM).
 template <int NP, int DP>
 __global__ void __launch_bounds__(256, QueriesShape<NP, DP>::kCtas)

@@ -180,7 +180,7 @@ logprob_narrow(const __grid_constant__ LogpArgs a)
 // segment is read for the threads' sums and largest logits alone; the few threads whose best makes the bound read
 // their pieces again, from the caches. Where a row is over several CTAs, the last of them to end joins their
 // statistics and best keys.
-// 4096 x 32003 bf16: 53 us without alternatives (4.9 TB/s), 88 with 8 of them (3.0 TB/s: the search, issue 54 %).
+// 4096 x 32003 bf16: 53 us without alternatives (4.9 TB/s), 84 with 8 of them (3.1 TB/s: the search, issue 54 %).
 template <typename T, int NT, int NP>
 __global__ void __launch_bounds__(NT, 1024 / NT)
 logprob_wide(const __grid_constant__ LogpArgs a)
@@ -624,9 +624,9 @@ cudaError_t launch_logprob(stacklstm_op *op, LogpArgs &a)
         a.part_key = (u64 *)op->ws[1];
         a.arrived = (int *)op->ws[2];
     }
-    // A long row's threads: 128, eight rows an SM, where the room for its best keys is small (4096 x 32003 bf16
-    // without alternatives 53 us, 60 with 256 threads and 82 with 512; with 8 of them 85, 89 and 124), else 256 (with 32
-    // 124 us, 291 with 128).
+    // A long row's threads: 128, eight rows an SM, where the room for its best keys is small, else 256. 4096 x 32003 bf16 without
+    // alternatives 53 us, 60 with 256 threads and 82 with 512; with 8 of them 84 and 89, with 12 (caches cold) 115 and 101, with
+    // 32 296 and 134; 8192 x 12000 with 8 97 and 119, 12 119 and 124, 16 144 and 128; fp32, 4096 x 32003, 8 138 and 148, 12 156 and 152.
     const int per = small ? NP : a.k <= 8 ? 4 * NP : 2 * NP;  // pieces a thread and segment
     const size_t spill = (size_t)a.k * std::max(per * RowVec<T>::E + 1, (int)kMergeItems) * 8;
     const dim3 grid((unsigned)((size_t)a.rows * a.split));

@@ -43,8 +43,8 @@ def test_many_short_sentences_with_broken_tiles(dt, D):
                                            (1, 127, 300, 4, 2, 100), (1, 2, 1100, 6, 2, 32), (2, 5, 3000, 4, 1, 64)])
 def test_a_bf16_result_alone_keeps_its_weights(B, T, S, nh, nk, D):
     """Without ctx as with it: y is what the weights in fp32 give, rounded once. Two bf16 parts of a weight, the first cut (which
-    leaves less than 2^-7 of it) and the second rounded by up to 2^-8 of that, leave out 2^-15; of each tile of 64 states eight additions
-    cut, each by less than 2^-23 of the sum so far (which is at most the sum of magnitudes)."""
+    leaves less than 2^-7 of it) and the second rounded by up to 2^-8 of that, leave out 2^-15; of each tile of 64 states eight MMAs cut
+    what they add: over 2^20 states of one sign y lost 0.9 %, 2^-23.8 of the sum an MMA, here 2^-23 of the sum of magnitudes."""
     c = Case(BF, B, T, S, nh, nk, D)
     want, _, w = at.attend(*c.x, c.q_len, c.kv_len, float(c.scale))
     of = np.arange(nh) * nk // nh
@@ -79,8 +79,8 @@ def long_reference(q, k, v, kv_len, scale, nk):
                                                (1, 2, 300000, 2, 24, False), (3, 130, 4200, 110, 8, True)])
 def test_memories_of_several_sums(B, T, S, nk, D, ragged):
     """More than 4096 states to an item, in several sums that are joined in fp32: scores that grow along the states, so that
-    each sum has a base of its own; whole and broken ends; a few long sentences, split as well. Cuts of 8 additions a tile
-    and 64 tiles at most, weights in two parts, and an fp32 sum (4 u a term) of the runs."""
+    each sum has a base of its own; whole and broken ends; a few long sentences, split as well. Cuts of 8 MMAs a tile,
+    2^-23 of the sum of magnitudes each as above, and 64 tiles at most, weights in two parts, and an fp32 sum (4 u a term) of the runs."""
     g = torch.Generator(device="cuda").manual_seed(S)
     r = lambda n: torch.randn(n, B, nk * D, device="cuda", generator=g)
     grow = torch.linspace(0, 20, S, device="cuda")[:, None, None]
